@@ -1,7 +1,7 @@
-"""Build libxl.so (HIP kernels + host planner + C ABI) for gfx950 with hipcc.
+"""Build libxl.so (HIP kernels + host planner + C ABI) and libxl_seq.so (sequence operators) for gfx950 with hipcc.
 
-Run as `python -m paper_2007_06000_amd.build`; the library lands next to this
-file so that it travels with the source tree.
+Run as `python -m paper_2007_06000_amd.build`; the libraries land next to this
+file so that they travel with the source tree.
 """
 from __future__ import annotations
 
@@ -25,6 +25,10 @@ HEADERS = [os.path.join(CSRC, "xl_internal.h"), os.path.join(CSRC, "plan.h"), os
            os.path.join(CSRC, "split_conv.h"), os.path.join(CSRC, "dw_conv.h"), os.path.join(CSRC, "chain_conv.h"),
            os.path.join(CSRC, "ksplit_conv.h"), os.path.join(CSRC, "direct_conv.h"), os.path.join(CSRC, "head_conv.h"), os.path.join(CSRC, "stem_conv.h"),
            os.path.join(ROOT, "include", "xl.h")]
+SEQ_LIB = os.path.join(HERE, "libxl_seq.so")
+SEQ_SOURCES = [("seq_api.cpp", "seq_api", []), ("seq_conv.hip", "seq_conv", []), ("seq_scan.hip", "seq_scan", []),
+               ("seq_quant.hip", "seq_quant", []), ("seq_matmul.hip", "seq_matmul", [])]
+SEQ_HEADERS = [os.path.join(CSRC, "seq_internal.h"), os.path.join(ROOT, "include", "xl_seq.h"), os.path.join(ROOT, "include", "xl.h")]
 
 # packed-fp32 instructions are switched off for all device code
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
@@ -45,11 +49,11 @@ def _filter(stderr: str) -> str:
     return "\n".join(keep)
 
 
-def _compile(item, force: bool) -> str:
+def _compile(item, headers, force: bool) -> str:
     src, name, defines = item
     obj = os.path.join(OBJ, name + ".o")
     path = os.path.join(CSRC, src)
-    newest = max(os.path.getmtime(p) for p in [path] + HEADERS)
+    newest = max(os.path.getmtime(p) for p in [path] + headers)
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= newest:
         return obj
     cmd = [_hipcc()] + HIPCC_FLAGS + defines + ["-x", "hip", "-c", path, "-o", obj]
@@ -62,18 +66,24 @@ def _compile(item, force: bool) -> str:
     return obj
 
 
-def build(force: bool = False, verbose: bool = True) -> str:
-    os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, force), SOURCES))
-    if force or not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
-        cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs
+def _link(lib: str, objs, force: bool) -> None:
+    if force or not os.path.exists(lib) or any(os.path.getmtime(o) > os.path.getmtime(lib) for o in objs):
+        cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib] + objs
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             sys.stderr.write(_filter(r.stderr) + "\n")
             raise RuntimeError("link failed")
-    if verbose:
-        print("built", LIB)
+
+
+def build(force: bool = False, verbose: bool = True) -> str:
+    os.makedirs(OBJ, exist_ok=True)
+    items = [(s, HEADERS) for s in SOURCES] + [(s, SEQ_HEADERS) for s in SEQ_SOURCES]
+    with ThreadPoolExecutor(max_workers=len(items)) as ex:
+        objs = list(ex.map(lambda item: _compile(*item, force), items))
+    for lib, part in ((LIB, objs[:len(SOURCES)]), (SEQ_LIB, objs[len(SOURCES):])):
+        _link(lib, part, force)
+        if verbose:
+            print("built", lib)
     return LIB
 
 

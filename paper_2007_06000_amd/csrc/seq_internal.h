@@ -1,0 +1,87 @@
+// What the kernels of the sequence operators share: element types, division of work, launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "xl_seq.h"
+
+namespace xls {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+static constexpr float LOG2E = 1.44269504088896340736f;
+
+// Activations in memory <-> fp32.  Conversions to 16 bits round to nearest, ties to even.
+template <int DT> struct Elem;
+template <> struct Elem<XL_F32> {
+    typedef float T;
+};
+template <> struct Elem<XL_F16> {
+    typedef _Float16 T;
+};
+template <> struct Elem<XL_BF16> {
+    typedef __bf16 T;
+};
+
+// V elements at p as fp32; VEC: p is aligned to their size together, and one load brings them.
+template <int DT, int V> __device__ __forceinline__ void load_vec(const void *p, long long at, float *out)
+{
+    typedef typename Elem<DT>::T T;
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    const Vec v = *reinterpret_cast<const Vec *>(static_cast<const T *>(p) + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = (float)v[i];
+}
+template <int DT, int V> __device__ __forceinline__ void store_vec(void *p, long long at, const float *in)
+{
+    typedef typename Elem<DT>::T T;
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    Vec v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (T)in[i];
+    *reinterpret_cast<Vec *>(static_cast<T *>(p) + at) = v;
+}
+
+// One hardware exponential (about one unit in the last place; results below the normal range are zero).
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * LOG2E); }
+
+// v * sigmoid(v)
+__device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + exp_fast(-v)); }
+
+// log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|) in (0, 1].  log(1 + e) = 2 artanh(r), r = e / (2 + e) <= 1/3, by the first seven
+// terms of artanh's series: what is left out is 1.6e-8 of the result.  (The hardware logarithm of 1 + e would lose the digits of a small e, and small
+// steps are the usual ones.)  NaN and infinities come through.
+__device__ __forceinline__ float softplus(float x)
+{
+    const float e = exp_fast(-fabsf(x));
+    const float r = e * __builtin_amdgcn_rcpf(2.f + e), q = r * r;
+    float s = 1.f / 13;
+    s = __builtin_fmaf(s, q, 1.f / 11);
+    s = __builtin_fmaf(s, q, 1.f / 9);
+    s = __builtin_fmaf(s, q, 1.f / 7);
+    s = __builtin_fmaf(s, q, 1.f / 5);
+    s = __builtin_fmaf(s, q, 1.f / 3);
+    s = __builtin_fmaf(s, q, 1.f);
+    const float m = x > 0.f ? x : x != x ? x : 0.f;
+    return __builtin_fmaf(2.f * r, s, m);
+}
+
+// The row of the states that belongs to sequence b, or -1 if it is absent.
+__device__ __forceinline__ long long slot_of(const int *slots, long long nslots, int b)
+{
+    const long long s = slots ? slots[b] : b;
+    return s >= 0 && s < nslots ? s : -1;
+}
+__device__ __forceinline__ int length_of(const int *lengths, int b, int length)
+{
+    return lengths ? min(max(lengths[b], 0), length) : length;
+}
+
+hipError_t launch_causal_conv(const xl_causal_conv_args &a, hipStream_t s);
+hipError_t launch_selective_scan(const xl_scan_args &a, hipStream_t s);
+hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t s);
+hipError_t launch_block_matmul(const xl_block_matmul_args &a, hipStream_t s);
+
+}  // namespace xls

@@ -1,0 +1,126 @@
+// Blocks of numbers to e4m3 with a scale each.
+//
+//   scale = max(max|x| / 448, 2^-126),  q = e4m3(x / scale)
+//
+// Bound by memory.  The division is a true one (about ten operations a number, hidden behind the loads): a product with the reciprocal lands on the
+// other side of a tie now and then, and q would depend on how it was computed.
+#include "seq_internal.h"
+
+namespace xls {
+
+static constexpr float E4M3_MAX = 448.f, MIN_SCALE = 1.17549435e-38f;
+
+// The largest |x| as the bits of a float: the order of the bits is the order of the numbers, infinity and then NaN above them.
+__device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
+__device__ __forceinline__ float scale_of(unsigned most)
+{
+    const float s = __builtin_bit_cast(float, most) / E4M3_MAX;
+    return s < MIN_SCALE ? MIN_SCALE : s;      // a NaN stays
+}
+
+__device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Eight numbers of a row from column k on; those past its end are zeros.
+template <int DT, bool WIDE> __device__ __forceinline__ void load8(const typename Elem<DT>::T *x, long long at, int k, int K, float *v)
+{
+    if (WIDE && k + 8 <= K) {
+        if (DT == XL_F32) {
+            load_vec<DT, 4>(x, at + k, v);
+            load_vec<DT, 4>(x, at + k + 4, v + 4);
+        } else {
+            load_vec<DT, 8>(x, at + k, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? (float)x[at + k + i] : 0.f;
+}
+
+// One row's blocks: 16 lanes a block, 8 numbers a lane.  The 16 blocks of a workgroup lie under each other, in 16 rows: their
+// scales are neighbours where a column of scales is contiguous, as the product wants them.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
+{
+    typedef typename Elem<DT>::T T;
+    const int lane = threadIdx.x % 16, K = (int)a.k, kb = blockIdx.y, k = kb * XL_SCALE_BLOCK + lane * 8;
+    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
+    if (row >= a.rows) return;
+    float v[8];
+    load8<DT, WIDE>(static_cast<const T *>(a.x), row * a.x_row, k, K, v);
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) most = max(most, (unsigned)__shfl_xor((int)most, o));
+    const float scale = scale_of(most);
+    if (lane == 0) a.scales[row * a.scale_row + kb * a.scale_block] = scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] / scale;
+    if (k < (K + 15) / 16 * 16)
+        *reinterpret_cast<u32x2 *>(static_cast<char *>(a.q) + row * a.q_row + k) = u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
+}
+
+// A block of 128 rows by 128 columns a workgroup; a thread has 8 columns of every sixteenth row.  Weights are quantised once.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
+{
+    typedef typename Elem<DT>::T T;
+    __shared__ unsigned shared_most[4];
+    const int K = (int)a.k, kb = blockIdx.y, k = kb * XL_SCALE_BLOCK + (threadIdx.x % 16) * 8;
+    const long long row0 = (long long)blockIdx.x * XL_SCALE_BLOCK + threadIdx.x / 16;
+    float v[8][8];
+    unsigned most = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const long long row = row0 + r * 16;
+        if (row < a.rows) {
+            load8<DT, WIDE>(static_cast<const T *>(a.x), row * a.x_row, k, K, v[r]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[r][i]));
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) most = max(most, (unsigned)__shfl_xor((int)most, o));
+    if (threadIdx.x % 64 == 0) shared_most[threadIdx.x / 64] = most;
+    __syncthreads();
+    most = max(max(shared_most[0], shared_most[1]), max(shared_most[2], shared_most[3]));
+    const float scale = scale_of(most);
+    if (threadIdx.x == 0) a.scales[blockIdx.x * a.scale_row + kb * a.scale_block] = scale;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const long long row = row0 + r * 16;
+        if (row < a.rows && k < (K + 15) / 16 * 16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[r][i] = v[r][i] / scale;
+            *reinterpret_cast<u32x2 *>(static_cast<char *>(a.q) + row * a.q_row + k) =
+                u32x2{e4m3x4(v[r][0], v[r][1], v[r][2], v[r][3]), e4m3x4(v[r][4], v[r][5], v[r][6], v[r][7])};
+        }
+    }
+}
+
+template <int DT> static hipError_t launch_type(const xl_quantize_args &a, hipStream_t s)
+{
+    const bool wide = ((unsigned long long)a.x | (unsigned long long)a.x_row * sizeof(typename Elem<DT>::T)) % 16 == 0;
+    const unsigned kb = (unsigned)((a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK);
+    if (a.block_rows == 1) {
+        const dim3 grid((unsigned)((a.rows + 15) / 16), kb);
+        if (wide) rows_kernel<DT, true><<<grid, 256, 0, s>>>(a);
+        else rows_kernel<DT, false><<<grid, 256, 0, s>>>(a);
+    } else {
+        const dim3 grid((unsigned)((a.rows + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK), kb);
+        if (wide) blocks_kernel<DT, true><<<grid, 256, 0, s>>>(a);
+        else blocks_kernel<DT, false><<<grid, 256, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t s)
+{
+    return a.dtype == XL_F32 ? launch_type<XL_F32>(a, s) : a.dtype == XL_F16 ? launch_type<XL_F16>(a, s) : launch_type<XL_BF16>(a, s);
+}
+
+}  // namespace xls
