@@ -113,6 +113,7 @@ xl_status xl_selective_scan(const xl_scan_args *args, void *stream)
     xl_status st = check_sequences(w, a.batch, a.length, a.channels, a.dtype, a.nslots, a.state, a.new_state, a.slots, a.lengths);
     if (st != XL_OK) return st;
     if (a.states < 1 || a.states > XL_MAX_STATES) return fail(XL_E_UNSUPPORTED, "%s: %lld states (1 to %d are covered)", w, a.states, XL_MAX_STATES);
+    if (!product_fits(a.batch, a.channels, 1, 1 << 30)) return fail(XL_E_SHAPE, "%s: batch %lld x channels %lld out of range", w, a.batch, a.channels);
     if (a.batch == 0 || a.channels == 0) return XL_OK;
     const int size = size_of(a.dtype);
     const struct { const char *name; const void *p; long long batch, token, width; bool written; } rows[] = {

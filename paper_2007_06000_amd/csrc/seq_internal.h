@@ -57,13 +57,14 @@ __device__ __forceinline__ float softplus(float x)
 {
     const float e = exp_fast(-fabsf(x));
     const float r = e * __builtin_amdgcn_rcpf(2.f + e), q = r * r;
-    float s = 0.14087329f;
-    s = __builtin_fmaf(s, q, 0.13980709f);
-    s = __builtin_fmaf(s, q, 0.20012427f);
-    s = __builtin_fmaf(s, q, 0.33333158f);
-    s = __builtin_fmaf(s, q, 1.f);
-    const float m = x > 0.f ? x : x != x ? x : 0.f;
-    return __builtin_fmaf(2.f * r, s, m);
+    float s = 2 * 0.14087329f;
+    s = __builtin_fmaf(s, q, 2 * 0.13980709f);
+    s = __builtin_fmaf(s, q, 2 * 0.20012427f);
+    s = __builtin_fmaf(s, q, 2 * 0.33333158f);
+    s = __builtin_fmaf(s, q, 2.f);
+    // max(x, 0) on the bits: what is negative as a float is so as an integer (and a NaN has come through e)
+    const float m = __builtin_bit_cast(float, max(__builtin_bit_cast(int, x), 0));
+    return __builtin_fmaf(r, s, m);
 }
 
 // The row of the states that belongs to sequence b, or -1 if it is absent.

@@ -1,27 +1,82 @@
 // Selective state-space scan.
 //
 //   h[n] <- exp(d A[n]) h[n] + d u B[n],   y = sum_n C[n] h[n] + D u,   y *= z sigmoid(z)
+#include <climits>
+#include <initializer_list>
+
 #include "seq_internal.h"
 
 namespace xls {
 
-// A token after the other: LP lanes a channel, NS states a lane, 256 / LP channels a workgroup.
-template <int DT, int LP, int NS>
+// A sequence's rows of one tensor: element [t][i] lies t * step + i elements behind `base`.  Where rows are aligned, of whole vectors and in 2 GB (`wide`) a buffer covers exactly the
+// tokens that the sequence has, so that one past its end reads as zeros and its store goes nowhere, without a comparison.
+template <typename T, int V> using Vec = T __attribute__((ext_vector_type(V)));
+struct Rows {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Rows(const void *base, long long step, int rows, int width, int size)
+    {
+        const unsigned bytes = rows > 0 ? ((rows - 1) * (unsigned)step + width) * size : 0u;
+        const unsigned long long p = (unsigned long long)base;
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)p), hi = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32));
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(((unsigned long long)hi << 32) | lo), (short)0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+    }
+    // `tile`: where the tile's first row begins (inside the buffer), `at`: this thread's place behind it, both in bytes
+    template <typename V> __device__ __forceinline__ V load(unsigned at, unsigned tile) const
+    {
+        if constexpr (sizeof(V) == 2) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, tile, 0));
+        else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, tile, 0));
+        else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, tile, 0));
+        else return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, tile, 0));
+    }
+    template <typename V> __device__ __forceinline__ void store(unsigned at, unsigned tile, V v) const
+    {
+        if constexpr (sizeof(V) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), rsrc, at, tile, 0);
+        else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rsrc, at, tile, 0);
+        else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rsrc, at, tile, 0);
+        else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rsrc, at, tile, 0);
+    }
+};
+static constexpr unsigned NOWHERE = 0x80000000u;       // past the end of every such buffer
+
+// The general case, for rows of any alignment: the first n of V elements exist, the others come out as zeros.
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_some(const T *p, int n)
+{
+    Vec<T, V> v = {};
+    if (n >= V) {
+        __builtin_memcpy(&v, p, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) v[i] = p[i];
+    }
+    return v;
+}
+template <typename T, int V> __device__ __forceinline__ void store_some(T *p, int n, Vec<T, V> v)
+{
+    if (n >= V) {
+        __builtin_memcpy(p, &v, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+
+// A token after the other: LP lanes a channel, four states (a 16-byte load) a lane, 256 / LP channels a workgroup.
+template <int DT, int LP>
 __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int groups)
 {
     typedef typename Elem<DT>::T T;
+    constexpr int NS = 4;
     const int b = blockIdx.x / groups, c = (blockIdx.x % groups) * (256 / LP) + threadIdx.x / LP, part = threadIdx.x % LP, n0 = part * NS;
     const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
     const long long slot = slot_of(a.slots, a.nslots, b);
     const int len = slot < 0 ? 0 : length_of(a.lengths, b, L);
     const bool in = c < D;
-    float A2[NS], h[NS];
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const bool live = in && n0 + i < N;
-        A2[i] = live ? a.A[(long long)c * N + n0 + i] * LOG2E : 0.f;
-        h[i] = live && a.state && slot >= 0 ? a.state[(slot * D + c) * N + n0 + i] : 0.f;
-    }
+    const int live = in ? N - n0 : 0;
+    const long long at = (slot * D + c) * N + n0;
+    const f32x4 A2 = load_some<float, NS>(a.A + (long long)c * N + n0, live) * LOG2E;
+    f32x4 h = load_some<float, NS>(a.state + at, a.state && slot >= 0 ? live : 0);
     const float bias = in && a.delta_bias ? a.delta_bias[c] : 0.f, skip = in && a.D ? a.D[c] : 0.f;
     const T *up = static_cast<const T *>(a.u) + b * a.u_batch + c, *dp = static_cast<const T *>(a.delta) + b * a.delta_batch + c;
     const T *zp = static_cast<const T *>(a.z) + b * a.z_batch + c, *Bp = static_cast<const T *>(a.B) + b * a.b_batch + n0;
@@ -33,12 +88,11 @@ __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int gro
         if (a.softplus) d = softplus(d);
         const float s = d * u;
         float y = 0.f;
+        const Vec<T, NS> B = load_some<T, NS>(Bp + t * a.b_token, N - n0), C = load_some<T, NS>(Cp + t * a.c_token, N - n0);
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            if (n0 + i < N) {
-                h[i] = __builtin_fmaf(exp2_fast(d * A2[i]), h[i], s * (float)Bp[t * a.b_token + i]);
-                y = __builtin_fmaf((float)Cp[t * a.c_token + i], h[i], y);
-            }
+            h[i] = __builtin_fmaf(exp2_fast(d * A2[i]), h[i], s * (float)B[i]);
+            y = __builtin_fmaf((float)C[i], h[i], y);
         }
 #pragma unroll
         for (int o = 1; o < LP; o *= 2) y += __shfl_xor(y, o);
@@ -50,11 +104,7 @@ __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int gro
     }
     if (part == 0 && in)
         for (int t = len; t < L; ++t) yp[t * a.y_token] = (T)0.f;
-    if (a.new_state && slot >= 0) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (in && n0 + i < N) a.new_state[(slot * D + c) * N + n0 + i] = h[i];
-    }
+    if (a.new_state && slot >= 0 && live > 0) store_some<float, NS>(a.new_state + at, live, h);
 }
 
 // Sum over the LP lanes of a channel, for LP tokens at once: lane i of the channel gets token i's.  At every step a lane keeps half of its tokens and hands the other
@@ -81,38 +131,31 @@ template <int LP> __device__ __forceinline__ float sum_over_lanes(float *p, int 
     return (up1 ? p[1] : p[0]) + from_partner<0xb1>(up1 ? p[0] : p[1]);                                             // lane ^ 1
 }
 
-// V elements at p, of which the first n exist; the others come out as zeros.
-template <typename T, int V> using Vec = T __attribute__((ext_vector_type(V)));
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_some(const T *p, int n, bool wide)
-{
-    Vec<T, V> v = {};
-    if (wide && n >= V) {
-        v = *reinterpret_cast<const Vec<T, V> *>(p);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) v[i] = p[i];
-    }
-    return v;
-}
-
 // Many tokens.  A workgroup owns CH = 64 / LP channels of a sequence and goes through it in tiles of W x TK tokens, TK of them a wave: the recurrence is linear, so a
-// wave runs its tokens from a state of zero (which gives E) and multiplies up their factors (P = exp(A sum d)); after a barrier each
-// folds the (P, E) of the waves before it into the state that it begins with, and runs its tokens again, the factors and
-// inputs still in registers, now with the outputs.
+// wave runs its tokens from a state of zero (which gives E) and multiplies up their factors (P = exp(A sum d)); then the waves exchange (P, E), each
+// folds those of the waves before it into the state that it begins with, and runs its tokens again, the factors and inputs
+// still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
+// tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 template <int DT, int LP, int NS, int W, int TK>
 __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups, bool wide, bool wide_bc)
 {
     typedef typename Elem<DT>::T T;
-    constexpr int CH = 64 / LP, NP = LP * NS, TT = W * TK, PT = TT + 4, THREADS = 64 * W;
+    constexpr int CH = 64 / LP, NP = LP * NS, TT = W * TK, PT = TK + 4;
     constexpr int PER = CH * TK / 64, VE = PER < 4 ? PER : 4, IT = PER / VE;            // a thread's part of a tile's u, delta, z and y
     constexpr int PERB = NP * TK / 64, VB = PERB < 4 ? PERB : 4, IB = PERB / VB;        // and of its B and C
-    static_assert(PER >= 1 && PERB >= 1 && TK % LP == 0 && TK % 4 == 0, "a tile divides among the threads");
-    __shared__ float dl[CH * PT], sx[CH * PT];      // steps, and step x input (later the outputs): [channel][token]
-    __shared__ float Bs[TT * NP], Cs[TT * NP];      // [token][state]
-    __shared__ Vec<float, NS> Ps[W * 64], Es[W * 64];
+    static_assert(PER >= 1 && PERB >= 1 && TK % LP == 0, "a wave's tokens divide among its lanes");
+    __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT];    // steps, and step x input (later the outputs): [channel][token]
+    __shared__ float Bs_all[W][TK * NP], Cs_all[W][TK * NP];    // [token][state]
+    __shared__ Vec<float, NS> Ps[2][W * 64], Es[2][W * 64];
 
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, c = lane / LP, part = lane % LP, n0 = part * NS;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
+    float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave], *Cs = Cs_all[wave];
     const int b = blockIdx.x / groups, c0 = (blockIdx.x % groups) * CH;
     const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
     const long long slot = slot_of(a.slots, a.nslots, b);
@@ -126,56 +169,92 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
         A2[i] = live ? a.A[(long long)(c0 + c) * N + n0 + i] * LOG2E : 0.f;
         h[i] = live && a.state && slot >= 0 ? a.state[(slot * D + c0 + c) * N + n0 + i] : 0.f;
     }
-    // this thread's numbers: VE channels of IT tokens
-    const int ec = tid % (CH / VE) * VE, et = tid / (CH / VE), nc = min(D - c0 - ec, VE);
-    const int bn = tid % (NP / VB) * VB, bt = tid / (NP / VB), nb = min(N - bn, VB);
-    constexpr int ET = THREADS * VE / CH, BT = THREADS * VB / NP;       // tokens between a thread's items
+    // this lane's numbers of its wave's tokens: VE channels of IT tokens
+    const int ec = lane % (CH / VE) * VE, et = lane / (CH / VE), nc = min(D - c0 - ec, VE), tw = wave * TK;
+    const int bn = lane % (NP / VB) * VB, bt = lane / (NP / VB), nb = min(N - bn, VB);
+    constexpr int ET = 64 * VE / CH, BT = 64 * VB / NP;         // tokens between a lane's items
     float bias[VE], skip[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
         bias[i] = a.delta_bias && i < nc ? a.delta_bias[c0 + ec + i] : 0.f;
         skip[i] = a.D && i < nc ? a.D[c0 + ec + i] : 0.f;
     }
-    const T *up = static_cast<const T *>(a.u) + b * a.u_batch + c0 + ec, *dp = static_cast<const T *>(a.delta) + b * a.delta_batch + c0 + ec;
-    const T *zp = static_cast<const T *>(a.z) + b * a.z_batch + c0 + ec;
-    const T *Bp = static_cast<const T *>(a.B) + b * a.b_batch + bn, *Cp = static_cast<const T *>(a.C) + b * a.c_batch + bn;
-    T *yp = static_cast<T *>(a.y) + b * a.y_batch + c0 + ec;
+    // the workgroup's first token of each tensor, and this lane's place in a tile
+    const T *up = static_cast<const T *>(a.u) + b * a.u_batch + c0, *dp = static_cast<const T *>(a.delta) + b * a.delta_batch + c0;
+    const T *zp = static_cast<const T *>(a.z) + b * a.z_batch + c0, *Bp = static_cast<const T *>(a.B) + b * a.b_batch, *Cp = static_cast<const T *>(a.C) + b * a.c_batch;
+    T *yp = static_cast<T *>(a.y) + b * a.y_batch + c0;
+    constexpr unsigned S = sizeof(T);
+    const unsigned u_at = nc > 0 ? ((tw + et) * (unsigned)a.u_token + ec) * S : NOWHERE, d_at = nc > 0 ? ((tw + et) * (unsigned)a.delta_token + ec) * S : NOWHERE, z_at = nc > 0 ? ((tw + et) * (unsigned)a.z_token + ec) * S : NOWHERE;
+    const unsigned y_at = nc > 0 ? ((tw + et) * (unsigned)a.y_token + ec) * S : NOWHERE, b_at = nb > 0 ? ((tw + bt) * (unsigned)a.b_token + bn) * S : NOWHERE, c_at = nb > 0 ? ((tw + bt) * (unsigned)a.c_token + bn) * S : NOWHERE;
+
+    const int tokens = wide ? len : 0, tokens_bc = wide_bc ? len : 0;
+    const int width = min(CH, D - c0);
+    const Rows urows(up, a.u_token, tokens, width, S), drows(dp, a.delta_token, tokens, width, S), zrows(zp, a.z_token, a.z ? tokens : 0, width, S);
+    const Rows yrows(yp, a.y_token, tokens, width, S), Brows(Bp, a.b_token, tokens_bc, N, S), Crows(Cp, a.c_token, tokens_bc, N, S);
+    const unsigned u_row = (unsigned)a.u_token * S, d_row = (unsigned)a.delta_token * S, z_row = a.z ? (unsigned)a.z_token * S : 0, y_row = (unsigned)a.y_token * S;
+    const unsigned b_row = (unsigned)a.b_token * S, c_row = (unsigned)a.c_token * S;
 
     Vec<T, VE> ur[IT], dr[IT], zr[IT];
     Vec<T, VB> Br[IB], Cr[IB];
     auto fetch = [&](int t0) {
+        if (wide) {
 #pragma unroll
-        for (int k = 0; k < IT; ++k) {
-            const long long t = t0 + et + k * ET;
-            const int n = t < len ? nc : 0;
-            ur[k] = load_some<T, VE>(up + t * a.u_token, n, wide);
-            dr[k] = load_some<T, VE>(dp + t * a.delta_token, n, wide);
-            if (a.z) zr[k] = load_some<T, VE>(zp + t * a.z_token, n, wide);
+            for (int k = 0; k < IT; ++k) {
+                ur[k] = urows.template load<Vec<T, VE>>(u_at + k * ET * u_row, t0 * u_row);
+                dr[k] = drows.template load<Vec<T, VE>>(d_at + k * ET * d_row, t0 * d_row);
+                zr[k] = zrows.template load<Vec<T, VE>>(z_at + k * ET * z_row, t0 * z_row);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < IT; ++k) {
+                const long long t = t0 + tw + et + k * ET;
+                const int n = t < len ? nc : 0;
+                ur[k] = load_some<T, VE>(up + t * a.u_token + ec, n);
+                dr[k] = load_some<T, VE>(dp + t * a.delta_token + ec, n);
+                zr[k] = load_some<T, VE>(zp + t * a.z_token + ec, a.z ? n : 0);
+            }
         }
+        if (wide_bc) {
 #pragma unroll
-        for (int k = 0; k < IB; ++k) {
-            const long long t = t0 + bt + k * BT;
-            const int n = t < len ? nb : 0;
-            Br[k] = load_some<T, VB>(Bp + t * a.b_token, n, wide_bc);
-            Cr[k] = load_some<T, VB>(Cp + t * a.c_token, n, wide_bc);
+            for (int k = 0; k < IB; ++k) {
+                Br[k] = Brows.template load<Vec<T, VB>>(b_at + k * BT * b_row, t0 * b_row);
+                Cr[k] = Crows.template load<Vec<T, VB>>(c_at + k * BT * c_row, t0 * c_row);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < IB; ++k) {
+                const long long t = t0 + tw + bt + k * BT;
+                const int n = t < len ? nb : 0;
+                Br[k] = load_some<T, VB>(Bp + t * a.b_token + bn, n);
+                Cr[k] = load_some<T, VB>(Cp + t * a.c_token + bn, n);
+            }
         }
     };
 
     fetch(0);
-    for (int t0 = 0; t0 < len; t0 += TT) {
+    for (int t0 = 0, set = 0; t0 < len; t0 += TT, set ^= 1) {
         Vec<T, VE> uc[IT], zc[IT];
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
             const int t = et + k * ET;
             uc[k] = ur[k];
             zc[k] = zr[k];
+            float d[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) d[i] = (float)dr[k][i] + bias[i];
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) d[i] = softplus(d[i]);
+            }
+            if (t0 + TT > len) {
+                asm volatile("");       // a branch: only the last tile has such tokens
+#pragma unroll
+                for (int i = 0; i < VE; ++i) d[i] = t0 + tw + t < len ? d[i] : 0.f;      // a token past the end changes nothing
+            }
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                float d = (float)dr[k][i] + bias[i];
-                if (a.softplus) d = softplus(d);
-                d = t0 + t < len ? d : 0.f;                     // a token past the end changes nothing
-                dl[(ec + i) * PT + t] = d;
-                sx[(ec + i) * PT + t] = d * (float)ur[k][i];
+                dl[(ec + i) * PT + t] = d[i];
+                sx[(ec + i) * PT + t] = d[i] * (float)ur[k][i];
             }
         }
 #pragma unroll
@@ -190,84 +269,88 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             *reinterpret_cast<Vec<float, VB> *>(&Cs[(bt + k * BT) * NP + bn]) = vc;
         }
         if (t0 + TT < len) fetch(t0 + TT);                      // the next tile's numbers come in the meantime
-        __syncthreads();
+        wave_sync();
 
         // the wave's tokens from a state of zero
-        float av[TK][NS], bv[TK][NS], sum = 0.f;
+        constexpr bool KEEP = TK * NS <= 64;     // the inputs too; with eight states a lane there is no room, and they are computed twice
+        float av[TK][NS], bv[KEEP ? TK : 1][NS], sum = 0.f;
         Vec<float, NS> e = {}, p;
-        const int tw = wave * TK;
 #pragma unroll
         for (int k = 0; k < TK; k += 4) {
-            const f32x4 d = *reinterpret_cast<const f32x4 *>(&dl[c * PT + tw + k]), s = *reinterpret_cast<const f32x4 *>(&sx[c * PT + tw + k]);
+            const f32x4 d = *reinterpret_cast<const f32x4 *>(&dl[c * PT + k]), s = *reinterpret_cast<const f32x4 *>(&sx[c * PT + k]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const Vec<float, NS> B = *reinterpret_cast<const Vec<float, NS> *>(&Bs[(tw + k + j) * NP + n0]);
+                const Vec<float, NS> B = *reinterpret_cast<const Vec<float, NS> *>(&Bs[(k + j) * NP + n0]);
                 sum += d[j];
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     av[k + j][i] = exp2_fast(d[j] * A2[i]);
-                    bv[k + j][i] = s[j] * B[i];
-                    e[i] = __builtin_fmaf(av[k + j][i], e[i], bv[k + j][i]);
+                    const float put = s[j] * B[i];
+                    if (KEEP) bv[KEEP ? k + j : 0][i] = put;
+                    e[i] = __builtin_fmaf(av[k + j][i], e[i], put);
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < NS; ++i) p[i] = exp2_fast(sum * A2[i]);
-        Ps[tid] = p;
-        Es[tid] = e;
+        // Two sets in turn: a wave that writes one again has passed the next tile's barrier, and so has every reader of it.
+        Ps[set][threadIdx.x] = p;
+        Es[set][threadIdx.x] = e;
         __syncthreads();
         float g[NS];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             if (w == wave) {
+                asm volatile("");       // a branch: every wave passes by W - 1 of these, and as selections they would cost it W * NS operations
 #pragma unroll
                 for (int i = 0; i < NS; ++i) g[i] = h[i];
             }
-            const Vec<float, NS> pw = Ps[w * 64 + lane], ew = Es[w * 64 + lane];
+            const Vec<float, NS> pw = Ps[set][w * 64 + lane], ew = Es[set][w * 64 + lane];
 #pragma unroll
             for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(pw[i], h[i], ew[i]);
         }
         // and again from the state that they find
 #pragma unroll
         for (int k = 0; k < TK; k += LP) {
-            float y[LP];
+            float y[LP], s[LP];
+            if (!KEEP) {
+#pragma unroll
+                for (int j = 0; j < LP; ++j) s[j] = sx[c * PT + k + j];
+            }
 #pragma unroll
             for (int j = 0; j < LP; ++j) {
-                const Vec<float, NS> C = *reinterpret_cast<const Vec<float, NS> *>(&Cs[(tw + k + j) * NP + n0]);
+                const Vec<float, NS> C = *reinterpret_cast<const Vec<float, NS> *>(&Cs[(k + j) * NP + n0]);
+                const Vec<float, NS> B = KEEP ? Vec<float, NS>{} : *reinterpret_cast<const Vec<float, NS> *>(&Bs[(k + j) * NP + n0]);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
-                    g[i] = __builtin_fmaf(av[k + j][i], g[i], bv[k + j][i]);
+                    g[i] = __builtin_fmaf(av[k + j][i], g[i], KEEP ? bv[KEEP ? k + j : 0][i] : s[j] * B[i]);
                     y[j] = i ? __builtin_fmaf(C[i], g[i], y[j]) : C[i] * g[i];
                 }
             }
-            sx[c * PT + tw + k + part] = sum_over_lanes<LP>(y, part);
+            sx[c * PT + k + part] = sum_over_lanes<LP>(y, part);
         }
-        __syncthreads();
+        wave_sync();
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
             const int t = et + k * ET;
-            if (t0 + t >= len || nc <= 0) continue;
             float out[VE];
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                out[i] = sx[(ec + i) * PT + t];
-                if (a.D) out[i] = __builtin_fmaf(skip[i], (float)uc[k][i], out[i]);
-                if (a.z) out[i] *= silu((float)zc[k][i]);
-            }
-            T *y = yp + (t0 + t) * a.y_token;
-            if (wide && nc >= VE) {
-                store_vec<DT, VE>(y, 0, out);
-            } else {
+            for (int i = 0; i < VE; ++i) out[i] = __builtin_fmaf(skip[i], (float)uc[k][i], sx[(ec + i) * PT + t]);
+            if (a.z) {
 #pragma unroll
-                for (int i = 0; i < VE; ++i)
-                    if (i < nc) y[i] = (T)out[i];
+                for (int i = 0; i < VE; ++i) out[i] *= silu((float)zc[k][i]);
             }
+            Vec<T, VE> v;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[i] = (T)out[i];
+            if (wide) yrows.store(y_at + k * ET * y_row, t0 * y_row, v);
+            else if (t0 + tw + t < len) store_some<T, VE>(yp + (t0 + tw + t) * a.y_token + ec, nc, v);
         }
     }
-    for (int t = len + et; t < L; t += ET) {
+    for (int t = len + wave * ET + et; t < L; t += W * ET) {
 #pragma unroll
         for (int i = 0; i < VE; ++i)
-            if (i < nc) yp[t * a.y_token + i] = (T)0.f;
+            if (i < nc) yp[t * a.y_token + ec + i] = (T)0.f;
     }
     if (wave == 0 && a.new_state && slot >= 0) {
 #pragma unroll
@@ -276,10 +359,10 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     }
 }
 
-template <int DT, int LP, int NS> static hipError_t launch_step(const xl_scan_args &a, hipStream_t s)
+template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, hipStream_t s)
 {
     const int per = 256 / LP, groups = (int)((a.channels + per - 1) / per);
-    step_kernel<DT, LP, NS><<<dim3((unsigned)(groups * a.batch)), 256, 0, s>>>(a, groups);
+    step_kernel<DT, LP><<<dim3((unsigned)(groups * a.batch)), 256, 0, s>>>(a, groups);
     return hipGetLastError();
 }
 
@@ -291,27 +374,59 @@ template <int DT, int LP, int NS, int W, int TK> static hipError_t launch_tile(c
     const unsigned long long at = (unsigned long long)a.u | (unsigned long long)a.delta | (unsigned long long)a.z | (unsigned long long)a.y;
     const unsigned long long steps = a.u_batch | a.u_token | a.delta_batch | a.delta_token | a.z_batch | a.z_token | a.y_batch | a.y_token;
     const unsigned long long at_bc = (unsigned long long)a.B | (unsigned long long)a.C, steps_bc = a.b_batch | a.b_token | a.c_batch | a.c_token;
-    const bool wide = (at | steps * sizeof(T)) % (VE * sizeof(T)) == 0, wide_bc = (at_bc | steps_bc * sizeof(T)) % (VB * sizeof(T)) == 0;
+    // a sequence's rows in one buffer: aligned, not overlapping (what follows the last token stays outside), offsets within 31 bits also a tile past the end
+    auto rows = [&](long long width, std::initializer_list<long long> tokens) {
+        for (long long t : tokens)
+            if (t < width || t > INT_MAX / (long long)sizeof(T) / (a.length + 2 * W * TK)) return false;
+        return true;
+    };
+    const bool wide = (at | steps * sizeof(T)) % (VE * sizeof(T)) == 0 && a.channels % VE == 0 && rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token}));
+    const bool wide_bc = (at_bc | steps_bc * sizeof(T)) % (VB * sizeof(T)) == 0 && a.states % VB == 0 && rows(a.states, {a.b_token, a.c_token});
     tile_kernel<DT, LP, NS, W, TK><<<dim3((unsigned)(groups * a.batch)), 64 * W, 0, s>>>(a, groups, wide, wide_bc);
     return hipGetLastError();
 }
 
+static constexpr long long CUS = 256;
+
+// Workgroups of 64 / LP channels each.
+static long long groups_of(const xl_scan_args &a, int lp) { return a.batch * ((a.channels * lp + 63) / 64); }
+
+// Waves of a workgroup.  One that has a compute unit to itself (its registers leave room for two waves a SIMD) takes eight, four where two fit and two where there are
+// four and more to overlap.  16 states, 3025 tokens, us with 2, 4, 8 waves: 256 workgroups 199, 107, 80; 1024 workgroups 289, 293, 320.
+template <int DT, int LP, int NS> static hipError_t launch_waves(const xl_scan_args &a, hipStream_t s)
+{
+    const long long groups = groups_of(a, LP);
+    if (groups <= CUS && a.length > 64) return launch_tile<DT, LP, NS, 8, 16>(a, s);
+    if (groups < 4 * CUS && a.length > 32) return launch_tile<DT, LP, NS, 4, 16>(a, s);
+    return launch_tile<DT, LP, NS, 2, 16>(a, s);
+}
+
 template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream_t s)
 {
-    if (a.length > 16) {
-        if (a.states <= 4) return launch_tile<DT, 4, 1, 4, 16>(a, s);
-        if (a.states <= 8) return launch_tile<DT, 4, 2, 4, 16>(a, s);
-        if (a.states <= 16) return launch_tile<DT, 4, 4, 4, 16>(a, s);
-        if (a.states <= 32) return launch_tile<DT, 8, 4, 4, 16>(a, s);
-        if (a.states <= 64) return launch_tile<DT, 16, 4, 4, 16>(a, s);
-        return launch_tile<DT, 16, 8, 4, 16>(a, s);
+    // A token after the other costs 0.8 us each until there is enough to overlap, a tile 6 us or more.
+    if (a.length <= (groups_of(a, 4) <= 4 * CUS ? 4 : 12)) {
+        if (a.states <= 4) return launch_step<DT, 1>(a, s);
+        if (a.states <= 8) return launch_step<DT, 2>(a, s);
+        if (a.states <= 16) return launch_step<DT, 4>(a, s);
+        if (a.states <= 32) return launch_step<DT, 8>(a, s);
+        if (a.states <= 64) return launch_step<DT, 16>(a, s);
+        return launch_step<DT, 32>(a, s);
     }
-    if (a.states <= 4) return launch_step<DT, 1, 4>(a, s);
-    if (a.states <= 8) return launch_step<DT, 2, 4>(a, s);
-    if (a.states <= 16) return launch_step<DT, 4, 4>(a, s);
-    if (a.states <= 32) return launch_step<DT, 8, 4>(a, s);
-    if (a.states <= 64) return launch_step<DT, 16, 4>(a, s);
-    return launch_step<DT, 32, 4>(a, s);
+    // Four states a lane cost the fewest operations.  With fewer the channels spread over more workgroups, which pays while each still has a compute unit to itself
+    // (16 states, 3025 tokens, us with 4, 2, 1 states a lane: 1024 channels 77, 54, 45; 2048 channels 77, 61, 82; 4096 channels 80, 118, 170).
+    if (a.states <= 4) return launch_waves<DT, 4, 1>(a, s);
+    if (a.states <= 8) return launch_waves<DT, 4, 2>(a, s);
+    if (a.states <= 16) {
+        if (groups_of(a, 16) <= CUS) return launch_tile<DT, 16, 1, 16, 16>(a, s);
+        if (groups_of(a, 8) <= CUS) return launch_tile<DT, 8, 2, 8, 16>(a, s);
+        return launch_waves<DT, 4, 4>(a, s);
+    }
+    if (a.states <= 32) {
+        if (groups_of(a, 16) <= CUS) return launch_tile<DT, 16, 2, 8, 16>(a, s);
+        return launch_waves<DT, 8, 4>(a, s);
+    }
+    if (a.states <= 64) return launch_waves<DT, 16, 4>(a, s);
+    return launch_tile<DT, 16, 8, 4, 16>(a, s);
 }
 
 hipError_t launch_selective_scan(const xl_scan_args &a, hipStream_t s)
