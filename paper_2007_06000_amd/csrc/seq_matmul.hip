@@ -5,6 +5,8 @@
 // A block's sum is one matrix operation 16 x 16 x 128 (or four of 16 x 16 x 32, below); it starts at zero, and its result is scaled into the fp32 sums by one
 // multiply-add for each of a lane's four.  The rows of b are the operation's rows and those of a its columns: a lane's four results are then neighbours in a row of
 // y, and share one scale of a (the lane's column) and one of b (its 16 rows lie in one block of 128).
+#include <type_traits>
+
 #include "seq_internal.h"
 
 namespace xls {
@@ -127,12 +129,12 @@ __global__ __launch_bounds__(WAVES * 64) void thin_kernel(const xl_block_matmul_
     }
 }
 
-// BM rows of a by BN rows of b, WM x WN waves, each with BM / WM by BN / WN of them: TM x TN matrix operations a block.  Both operands' blocks go straight to LDS, two
-// stages in turn: the next block comes while this one is multiplied.  A row's block is 128 bytes, 8 chunks of 16; chunk c of row r lies at chunk c ^ (r & 7),
-// so that the 16 rows that an operation reads at once, 128 bytes apart, fall on different banks.
-template <int BM, int BN> struct Stage {
-    char a[BM * 128], b[BN * 128];
-    float scale[BM];
+// BM rows of a by BN rows of b, WM x WN waves, each with BM / WM by BN / WN of them: TM x TN matrix operations a block.  Both operands' blocks go straight to LDS, S
+// stages of KS blocks in turn: S - 1 stages are on their way while one is multiplied.  A row's block is 128 bytes, 8 chunks of 16; chunk c of row r lies
+// at chunk c ^ (r & 7), so that the 16 rows that an operation reads at once, 128 bytes apart, fall on different banks.
+template <int BM, int BN, int KS> struct Stage {
+    char a[KS][BM * 128], b[KS][BN * 128];
+    float scale[KS][BM];
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p, long long begin, long long size)
@@ -152,13 +154,16 @@ __device__ __forceinline__ void to_lds4(__amdgpu_buffer_rsrc_t from, void *to, u
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 4, at, begin, 0, 0);
 }
 
-template <int DT, int BM, int BN, int WM, int WN>
+template <int DT, int BM, int BN, int WM, int WN, int KS, int S>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmul_args p, int tiles_m, int tiles_n, bool wide)
 {
-    constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;
+    typedef typename Elem<DT>::T T;
+    constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB + 1;
+    typedef Stage<BM, BN, KS> St;
     static_assert(LA >= 1 && LB >= 1 && TN * 16 <= XL_SCALE_BLOCK && BM % 64 == 0 && BM / 64 <= WAVES, "the waves share the loads");
+    static_assert((size_t)BM * BN * sizeof(T) <= S * sizeof(St), "the results pass through LDS");
     typedef BlockProduct<DT == XL_F32> P;
-    __shared__ Stage<BM, BN> even, odd;
+    __shared__ St stages[S];
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16;
     // Workgroups go to the 8 XCDs in turn; each XCD gets a contiguous part of an order in which 8 x 4 neighbours share rows of a and of b in its L2.
@@ -184,20 +189,25 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
     for (int i = 0; i < LB; ++i) b_at[i] = (unsigned)min((wave + i * WAVES) * 8 + lane / 8, rows_b - 1) * (unsigned)p.b_row;
     const unsigned s_at = (unsigned)min(wave % (BM / 64) * 64 + lane, rows_a - 1) * (unsigned)p.a_scale_row * 4;
     const int wm = wave % WM, wn = wave / WM;
+    // the wave's rows of b share a scale for each block; a lane keeps one of 64 blocks'
     const float *sb = p.b_scales + ((n0 + min(wn * TN * 16, rows_b - 1)) / XL_SCALE_BLOCK) * p.b_scale_row;
-
-    auto fetch = [&](Stage<BM, BN> &st, int kb) __attribute__((always_inline)) {
-        const unsigned c = kb == blocks - 1 ? last_chunk : chunk * 16;
-#pragma unroll
-        for (int i = 0; i < LA; ++i) to_lds16(ra, st.a + (wave + i * WAVES) * 1024, a_at[i] + c, kb * XL_SCALE_BLOCK);
-#pragma unroll
-        for (int i = 0; i < LB; ++i) to_lds16(rb, st.b + (wave + i * WAVES) * 1024, b_at[i] + c, kb * XL_SCALE_BLOCK);
-        to_lds4(rs, st.scale + wave % (BM / 64) * 64, s_at, kb * (unsigned)p.a_scale_block * 4);
+    auto scales_b = [&](int kb) __attribute__((always_inline)) {
+        float v = sb[min(kb + lane, blocks - 1) * p.b_scale_block];
+        asm volatile("" : "+v"(v));         // waited for here, and not in every step
+        return v;
     };
-    auto clear = [&](Stage<BM, BN> &st) __attribute__((always_inline)) {       // numbers from K on become zeros
+
+    // one of a wave's LOADS loads of block kb, into block k of a stage
+    auto fetch = [&](St &st, int k, int kb, int load) __attribute__((always_inline)) {
+        const unsigned c = kb == blocks - 1 ? last_chunk : chunk * 16;
+        if (load < LA) to_lds16(ra, st.a[k] + (wave + load * WAVES) * 1024, a_at[load < LA ? load : 0] + c, kb * XL_SCALE_BLOCK);
+        else if (load < LA + LB) to_lds16(rb, st.b[k] + (wave + (load - LA) * WAVES) * 1024, b_at[load < LA ? 0 : load < LA + LB ? load - LA : 0] + c, kb * XL_SCALE_BLOCK);
+        else to_lds4(rs, st.scale[k] + wave % (BM / 64) * 64, s_at, kb * (unsigned)p.a_scale_block * 4);
+    };
+    auto clear = [&](char *rows128, int rows) __attribute__((always_inline)) {       // numbers from K on become zeros
         const int live = K % XL_SCALE_BLOCK;
-        for (int i = threadIdx.x; i < (BM + BN) * 8; i += 64 * WAVES) {
-            char *at = st.a + i * 16;           // b follows a
+        for (int i = threadIdx.x; i < rows * 8; i += 64 * WAVES) {
+            char *at = rows128 + i * 16;
             const int c = (i % 8) ^ (i / 8 % 8), bytes = live - c * 16;
             if (bytes >= 16) continue;
             u32x4 v = *reinterpret_cast<u32x4 *>(at);
@@ -217,98 +227,162 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
     };
 
     f32x4 acc[TM][TN] = {};
-    // The operations of one row of tiles run while the results of the row before are scaled in.
-    auto multiply = [&](const Stage<BM, BN> &st, float s_b) __attribute__((always_inline)) {
+    // While the operations of one row of tiles run, the results of the row before are scaled in, the operand of the row behind is read, and two loads of a later
+    // block are sent off (all of them at once would hold the wave up until the last has left).
+    auto multiply = [&](const St &st, int kk, float s_b, auto fetching, St &to, int kb) __attribute__((always_inline)) {
         typename P::Operand b[TN];
+        Part a[2];
+        float s[3];
+        a[0] = part(st.a[kk] + wm * TM * 2048, quad);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = P::operand(part(st.b + (wn * TN + j) * 2048, quad));
+        for (int j = 0; j < TN; ++j) b[j] = P::operand(part(st.b[kk] + (wn * TN + j) * 2048, quad));
+        s[0] = st.scale[kk][wm * TM * 16 + col];
         f32x4 v[2][TN];
-        float s = 0.f;
 #pragma unroll
         for (int i = 0; i <= TM; ++i) {
-            if (i < TM) {
-                const typename P::Operand a = P::operand(part(st.a + (wm * TM + i) * 2048, quad));
+            if constexpr (fetching) {
+                constexpr int EACH = (LOADS + TM - 1) / TM > 2 ? (LOADS + TM - 1) / TM : 2;
 #pragma unroll
-                for (int j = 0; j < TN; ++j) v[i % 2][j] = P::run(b[j], a);
+                for (int l = i * EACH; l < (i + 1) * EACH && l < LOADS; ++l) fetch(to, kk, kb, l);
+            }
+            if (i + 1 < TM) {
+                a[(i + 1) % 2] = part(st.a[kk] + (wm * TM + i + 1) * 2048, quad);
+                s[(i + 1) % 3] = st.scale[kk][(wm * TM + i + 1) * 16 + col];
+            }
+            if (i < TM) {
+                const typename P::Operand ai = P::operand(a[i % 2]);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) v[i % 2][j] = P::run(b[j], ai);
             }
             if (i > 0) {
+                const float f = s[(i - 1) % 3] * s_b;
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i - 1][j][k] = __builtin_fmaf(s, v[(i - 1) % 2][j][k], acc[i - 1][j][k]);
+                    for (int k = 0; k < 4; ++k) acc[i - 1][j][k] = __builtin_fmaf(f, v[(i - 1) % 2][j][k], acc[i - 1][j][k]);
                     asm volatile("" : "+v"(acc[i - 1][j]));     // here, and not put off until all of a block's results wait in registers
                 }
             }
-            if (i < TM) s = st.scale[(wm * TM + i) * 16 + col] * s_b;
+            if (DT != XL_F32 && i > 0 && i < TM) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto arrived = [&]() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    auto last_arrived = [&](Stage<BM, BN> &st) __attribute__((always_inline)) {
-        arrived();
-        if (K % XL_SCALE_BLOCK) {
-            clear(st);
-            __syncthreads();
+    // (Without the promise that the two stages are apart the compiler waits for the one that is loaded before it reads the other.)
+    auto step = [&](St *__restrict__ to, const St *__restrict__ from, int kb, float s_b, auto fetching) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            if (KS > 1 && kb + k >= blocks) break;
+            const float s = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s_b), (kb + k) % 64));
+            multiply(*from, k, s, fetching, *to, min(kb + k + (S - 1) * KS, blocks - 1));
         }
     };
-    // The next block is on its way to `to` while the one in `from` is multiplied.  (Without the promise that the two are apart the compiler waits for the one before it
-    // reads the other.)
-    auto step = [&](Stage<BM, BN> *__restrict__ to, const Stage<BM, BN> *__restrict__ from, int kb, float s_b) __attribute__((always_inline)) {
-        fetch(*to, kb);
-        multiply(*from, s_b);
-    };
-    auto scale_b = [&](int kb) __attribute__((always_inline)) { return sb[min(kb, blocks - 1) * p.b_scale_block]; };
 
-    if (blocks > 0) {
-        float se = scale_b(0), so = scale_b(1);
-        fetch(even, 0);
-        int kb = 0;
-        for (; kb + 2 < blocks; kb += 2) {
-            arrived();
-            step(&odd, &even, kb + 1, se);
-            se = scale_b(kb + 2);
-            arrived();
-            step(&even, &odd, kb + 2, so);
-            so = scale_b(kb + 3);
-        }
-        if (kb + 1 < blocks) {
-            arrived();
-            step(&odd, &even, kb + 1, se);
-            last_arrived(odd);
-            multiply(odd, so);
-        } else {
-            last_arrived(even);
-            multiply(even, se);
+    float s_b = blocks > 0 ? scales_b(0) : 0.f;
+#pragma unroll
+    for (int i = 0; i < (S - 1) * KS; ++i) {
+        if (i / KS * KS < blocks) {             // whole stages: past the last block it comes once more
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) fetch(stages[i / KS], i % KS, min(i, blocks - 1), l);
         }
     }
+    int from = 0, to = S - 1, kb = 0;
+    auto next = [&](auto fetching) __attribute__((always_inline)) {
+        if (kb && kb % 64 == 0) s_b = scales_b(kb);
+        step(&stages[to], &stages[from], kb, s_b, fetching);
+        from = from + 1 == S ? 0 : from + 1;
+        to = to + 1 == S ? 0 : to + 1;
+        kb += KS;
+    };
+    // Before each: this wave's part of the stage has arrived, those of the stages behind it may be on their way; then everybody's has, and everybody is done with the
+    // stage that is loaded next.  (A barrier of the language would wait for all loads into LDS.)
+    while (kb + (S - 1) * KS < blocks) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * KS * LOADS) : "memory");
+        next(std::true_type());
+    }
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int behind = S - 2; behind >= 0; --behind) {       // the last S - 1 stages, or as many as there are
+        if (kb + behind * KS >= blocks) continue;
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(behind * KS * LOADS) : "memory");
+        if (behind == 0 && K % XL_SCALE_BLOCK) {
+            clear(stages[from].a[(blocks - 1) % KS], BM);
+            clear(stages[from].b[(blocks - 1) % KS], BN);
+            __syncthreads();
+        }
+        next(std::false_type());
+    }
+
+    // The results go through LDS, where a wave turns its part into whole rows: stores of 16 bytes a lane, 128 and more in a row.  Chunks of 16 bytes are
+    // placed as above.
+    __syncthreads();
+    constexpr int ROW = TN * 16 * sizeof(T), CHUNKS = ROW / 16, PER = 16 / sizeof(T);
+    char *mine = reinterpret_cast<char *>(stages) + wave * (TM * 16 * ROW);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) store4<DT>(p, m0 + (wm * TM + i) * 16 + col, n0 + (wn * TN + j) * 16 + quad * 4, acc[i][j], wide);
+    for (int j = 0; j < TN; ++j) {
+        const int n = n0 + (wn * TN + j) * 16 + quad * 4;
+        float bias[4] = {};
+        if (p.bias) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) bias[k] = n + k < p.n ? p.bias[n + k] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            typedef T Four __attribute__((ext_vector_type(4)));
+            Four v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = (T)(acc[i][j][k] + bias[k]);
+            const int at = (j * 16 + quad * 4) * sizeof(T);
+            *reinterpret_cast<Four *>(mine + (i * 16 + col) * ROW + ((at / 16) ^ (col & (CHUNKS - 1))) * 16 + at % 16) = v;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int n = n0 + wn * TN * 16 + lane % CHUNKS * PER, live = (int)min((long long)PER, p.n - n);
+    T *y = static_cast<T *>(p.y) + (m0 + wm * TM * 16 + lane / CHUNKS) * p.y_row + n;
+#pragma unroll
+    for (int i = 0; i < TM * 16 / (64 / CHUNKS); ++i, y += 64 / CHUNKS * p.y_row) {
+        const int r = i * (64 / CHUNKS) + lane / CHUNKS;
+        typedef T Chunk __attribute__((ext_vector_type(PER)));
+        const Chunk v = *reinterpret_cast<const Chunk *>(mine + r * ROW + ((lane % CHUNKS) ^ (r & (CHUNKS - 1))) * 16);
+        if (m0 + wm * TM * 16 + r >= p.m) continue;
+        if (wide && live == PER) {
+            *reinterpret_cast<Chunk *>(y) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (k < live) y[k] = v[k];
+        }
+    }
 }
 
-template <int DT, int BM, int BN, int WM, int WN> static hipError_t launch_tile(const xl_block_matmul_args &a, bool wide, hipStream_t s)
+template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError_t launch_tile(const xl_block_matmul_args &a, bool wide, hipStream_t s)
 {
     const long long tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
-    tile_kernel<DT, BM, BN, WM, WN><<<dim3((unsigned)(tm * tn)), 64 * WM * WN, 0, s>>>(a, (int)tm, (int)tn, wide);
+    tile_kernel<DT, BM, BN, WM, WN, KS, S><<<dim3((unsigned)(tm * tn)), 64 * WM * WN, 0, s>>>(a, (int)tm, (int)tn, wide);
     return hipGetLastError();
 }
 
 template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)
 {
     typedef typename Elem<DT>::T T;
-    const bool wide = ((unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T)) % (4 * sizeof(T)) == 0;
+    const unsigned long long at = (unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T);
     // a tile of the tile kernel lies within 31 bits, and so do its scales
     const long long limit = 1ll << 22, blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
     if (a.m > 32 && a.a_row < limit && a.b_row < limit && a.a_scale_row < limit / 16 && a.a_scale_block < (1ll << 28) / (blocks + 1)) {
-        if (DT != XL_F32 && a.m * a.n >= 256ll * 256 * 128) return launch_tile<DT, 256, 256, 2, 4>(a, wide, s);
-        return launch_tile<DT, 128, 128, 2, 2>(a, wide, s);
+        if constexpr (DT != XL_F32)
+            if (a.m * a.n >= 256ll * 256 * 128) return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, at % 16 == 0, s);
+        if (a.m * a.n >= 128ll * 128 * 128) return launch_tile<DT, 128, 128, 2, 4, 1, 4>(a, at % 16 == 0, s);
+        return launch_tile<DT, 64, 64, 4, 2, 2, 3>(a, at % 16 == 0, s);
     }
     const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 15) / 16);
-    thin_kernel<DT, 4><<<dim3((unsigned)tiles), 256, 0, s>>>(a, (int)tiles_n, wide);
+    thin_kernel<DT, 4><<<dim3((unsigned)tiles), 256, 0, s>>>(a, (int)tiles_n, at % (4 * sizeof(T)) == 0);
     return hipGetLastError();
 }
 
