@@ -10,8 +10,8 @@
  *   xl_quantize_blocks   numbers -> 8-bit floating point (e4m3) with one scale for each block of 128
  *   xl_block_matmul      product of two such operands
  *
- * Every call takes one struct of 64-bit numbers and DEVICE pointers, enqueues one kernel on `stream` and returns
- * without synchronising: it may be recorded into a HIP graph.  The library allocates nothing, needs no workspace and
+ * Every call takes one struct of 64-bit numbers and DEVICE pointers, enqueues one kernel (a large
+ * product two) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates nothing, needs no workspace and
  * keeps nothing between calls.  Calls never throw or abort.  The current HIP device must be a gfx950 (XL_E_DEVICE) that can reach the
  * pointers.  Inference only: there are no gradients.
  *

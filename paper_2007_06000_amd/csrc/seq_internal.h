@@ -78,6 +78,14 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, int length)
     return lengths ? min(max(lengths[b], 0), length) : length;
 }
 
+// What lanes of this wave have put into LDS can be read by the others.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 hipError_t launch_causal_conv(const xl_causal_conv_args &a, hipStream_t s);
 hipError_t launch_selective_scan(const xl_scan_args &a, hipStream_t s);
 hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t s);

@@ -94,38 +94,68 @@ template <int DT> __device__ __forceinline__ void store4(const xl_block_matmul_a
     }
 }
 
-// 16 rows of b by 16 rows of a; the waves of the workgroup divide the reduction.
-template <int DT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void thin_kernel(const xl_block_matmul_args a, int tiles_n, bool wide)
+// Few rows of a: what costs is reading b once.  16 rows of b and MT x 16 of a a workgroup, whose eight waves take the blocks in turn; their sums meet in LDS, in the
+// same order every time.  (16 x 4096 x 2048: 3.9 us, of which an empty launch is 2.6; 16 x 8192 x 8192: 17.0 us, 4.0 TB/s.  Four or sixteen waves, or the
+// operands of two or four blocks on their way at once, measured the same within 5 %.)
+template <int DT, int MT>
+__global__ __launch_bounds__(512) void thin_kernel(const xl_block_matmul_args a, int tiles_n, bool wide)
 {
-    __shared__ f32x4 part[WAVES][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, quad = lane / 16, K = (int)a.k;
+    constexpr int WAVES = 8;
+    typedef BlockProduct<DT == XL_F32> P;
+    __shared__ f32x4 part[WAVES][MT][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, K = (int)a.k;
     const int n0 = (blockIdx.x % tiles_n) * 16, blocks = (K + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
-    const long long m0 = (long long)(blockIdx.x / tiles_n) * 16;
+    const long long m0 = (long long)(blockIdx.x / tiles_n) * (16 * MT);
     const char *brow = static_cast<const char *>(a.b) + min((long long)n0 + col, a.n - 1) * a.b_row;
-    const long long ai = min(m0 + col, a.m - 1);
-    const char *arow = static_cast<const char *>(a.a) + ai * a.a_row;
-    const float *sa = a.a_scales + ai * a.a_scale_row, *sb = a.b_scales + (n0 / XL_SCALE_BLOCK) * a.b_scale_row;
-    f32x4 acc = {};
+    const float *sb = a.b_scales + (n0 / XL_SCALE_BLOCK) * a.b_scale_row;
+    const char *arow[MT];
+    const float *sa[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const long long r = min(m0 + i * 16 + col, a.m - 1);
+        arow[i] = static_cast<const char *>(a.a) + r * a.a_row;
+        sa[i] = a.a_scales + r * a.a_scale_row;
+    }
+    f32x4 acc[MT] = {};
     for (int kb = wave; kb < blocks; kb += WAVES) {
         const int k = kb * XL_SCALE_BLOCK + quad * 32;
-        Part r, c;
-        r.q[0] = load16(brow, k, K);
-        r.q[1] = load16(brow, k + 16, K);
-        c.q[0] = load16(arow, k, K);
-        c.q[1] = load16(arow, k + 16, K);
-        typedef BlockProduct<DT == XL_F32> P;
-        const f32x4 p = P::run(P::operand(r), P::operand(c));
-        const float s = sa[kb * a.a_scale_block] * sb[kb * a.b_scale_block];
+        Part r, c[MT];
+        float s[MT];
+        const float t = sb[kb * a.b_scale_block];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(s, p[i], acc[i]);
+        for (int i = 0; i < MT; ++i) s[i] = sa[i][kb * a.a_scale_block];
+        if ((kb + 1) * XL_SCALE_BLOCK <= K) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                r.q[h] = *reinterpret_cast<const u32x4 *>(brow + k + h * 16);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) c[i].q[h] = *reinterpret_cast<const u32x4 *>(arow[i] + k + h * 16);
+            }
+        } else {            // K ends inside this block
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                r.q[h] = load16(brow, k + h * 16, K);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) c[i].q[h] = load16(arow[i], k + h * 16, K);
+            }
+        }
+        const typename P::Operand rows = P::operand(r);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const f32x4 p = P::run(rows, P::operand(c[i]));
+            const float f = s[i] * t;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_fmaf(f, p[j], acc[i][j]);
+        }
     }
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
-        store4<DT>(a, m0 + col, n0 + quad * 4, acc, wide);
+    for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < MT; i += WAVES) {
+        f32x4 sum = part[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += part[w][i][lane];
+        store4<DT>(a, m0 + i * 16 + col, n0 + quad * 4, sum, wide);
     }
 }
 
@@ -341,9 +371,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
             *reinterpret_cast<Four *>(mine + (i * 16 + col) * ROW + ((at / 16) ^ (col & (CHUNKS - 1))) * 16 + at % 16) = v;
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_sync();
     const int n = n0 + wn * TN * 16 + lane % CHUNKS * PER, live = (int)min((long long)PER, p.n - n);
     T *y = static_cast<T *>(p.y) + (m0 + wm * TM * 16 + lane / CHUNKS) * p.y_row + n;
 #pragma unroll
@@ -369,21 +397,53 @@ template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError
     return hipGetLastError();
 }
 
-template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)
+static constexpr long long CUS = 256;
+
+template <int DT, int MT> static hipError_t launch_thin(const xl_block_matmul_args &a, hipStream_t s)
 {
     typedef typename Elem<DT>::T T;
     const unsigned long long at = (unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T);
-    // a tile of the tile kernel lies within 31 bits, and so do its scales
-    const long long limit = 1ll << 22, blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
-    if (a.m > 32 && a.a_row < limit && a.b_row < limit && a.a_scale_row < limit / 16 && a.a_scale_block < (1ll << 28) / (blocks + 1)) {
-        if constexpr (DT != XL_F32)
-            if (a.m * a.n >= 256ll * 256 * 128) return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, at % 16 == 0, s);
-        if (a.m * a.n >= 128ll * 128 * 128) return launch_tile<DT, 128, 128, 2, 4, 1, 4>(a, at % 16 == 0, s);
-        return launch_tile<DT, 64, 64, 4, 2, 2, 3>(a, at % 16 == 0, s);
-    }
-    const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 15) / 16);
-    thin_kernel<DT, 4><<<dim3((unsigned)tiles), 256, 0, s>>>(a, (int)tiles_n, at % (4 * sizeof(T)) == 0);
+    const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 16 * MT - 1) / (16 * MT));
+    thin_kernel<DT, MT><<<dim3((unsigned)tiles), 512, 0, s>>>(a, (int)tiles_n, at % (4 * sizeof(T)) == 0);
     return hipGetLastError();
+}
+
+template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)
+{
+    typedef typename Elem<DT>::T T;
+    const bool wide = ((unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T)) % 16 == 0;
+    const long long blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
+    // a tile of the tile kernel lies within 31 bits, and so do its scales
+    const long long limit = 1ll << 22;
+    const bool near = a.a_row < limit && a.b_row < limit && a.a_scale_row < limit / 16 && a.a_scale_block < (1ll << 28) / (blocks + 1);
+    if (a.m <= 16) return launch_thin<DT, 1>(a, s);
+    if (a.m <= 32 || !near) return launch_thin<DT, 2>(a, s);
+    // The smallest tiles that still have a compute unit each, or share one by twos, then larger ones (us, bf16, k 2048, tiles of 64 alone / by twos, 128 alone / by twos, 256: 1024 x 1024 7.2, 8.5,
+    // 11.9, 13.9, 25; 1024 x 2048 12.9, 10.5, 12.2, 14.2, 26; 1024 x 4096 24, 18.5, 13.0, 15.1, 26; 2048 x 4096 46, 34, 24, 21, 28; 4096 x 4096 90, 66, 46, 41, 33).
+    auto tiles = [](long long m, long long n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+    if (tiles(a.m, a.n, 64) <= CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 3>(a, wide, s);
+    if (tiles(a.m, a.n, 64) <= 2 * CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 2>(a, wide, s);
+    if (tiles(a.m, a.n, 128) <= CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 4>(a, wide, s);
+    if constexpr (DT == XL_F32) {
+        return launch_tile<DT, 128, 128, 2, 2, 1, 2>(a, wide, s);       // (four waves: 68 us, eight: 69, at 4096 x 4096 x 2048)
+    } else {
+        if (tiles(a.m, a.n, 128) <= 2 * CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 2>(a, wide, s);
+        // Tiles of 256 go through the chip in rounds of one a compute unit, and the last round may have few.  Where smaller tiles can do with what is left in less than half a
+        // round, they do, in a second launch (24642 x 4096 x 4096: 386 us in seven rounds, 350 so).
+        const long long tn = (a.n + 255) / 256, rows = tiles(a.m, a.n, 256) / CUS * CUS / tn * 256;
+        if (rows > 0 && rows < a.m && blocks >= 8 && tiles(a.m - rows, a.n, 128) <= CUS) {
+            xl_block_matmul_args part = a;
+            part.m = rows;
+            const hipError_t e = launch_tile<DT, 256, 256, 2, 4, 1, 2>(part, wide, s);
+            if (e != hipSuccess) return e;
+            part.m = a.m - rows;
+            part.a = static_cast<const char *>(a.a) + rows * a.a_row;
+            part.a_scales = a.a_scales + rows * a.a_scale_row;
+            part.y = static_cast<T *>(a.y) + rows * a.y_row;
+            return launch_type<DT>(part, s);
+        }
+        return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, wide, s);
+    }
 }
 
 hipError_t launch_block_matmul(const xl_block_matmul_args &a, hipStream_t s)

@@ -136,12 +136,6 @@ template <int LP> __device__ __forceinline__ float sum_over_lanes(float *p, int 
 // folds those of the waves before it into the state that it begins with, and runs its tokens again, the factors and inputs
 // still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
 // tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 template <int DT, int LP, int NS, int W, int TK>
 __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups, bool wide, bool wide_bc)
 {

@@ -1,7 +1,7 @@
 """Sequence operators on torch tensors: causal convolution, selective scan, block quantisation, block-scaled product.
 
 The names and the meaning of every argument mirror include/xl_seq.h; the arithmetic runs in the HIP kernels of libxl_seq.so, and there is no
-CPU fallback.  Each call enqueues one kernel on the current stream of its tensors' device and returns without waiting;
+CPU fallback.  Each call enqueues one kernel (a large product two) on the current stream of its tensors' device and returns without waiting;
 what does not fit raises `XlError` before anything is launched.  Inference only: tensors that ask for gradients are refused.
 """
 from __future__ import annotations

@@ -160,3 +160,31 @@ def test_refusals():
                  lambda: seq.quantize_weight(torch.zeros(4, 40, device="cuda", requires_grad=True))):
         with pytest.raises(XlError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("m,n,k", [(4096, 2048, 128), (2100, 4000, 130), (3000, 3000, 1040), (5000, 1800, 384), (1030, 9000, 256), (16000, 600, 520)])
+def test_large_products_against_a_smaller_part_of_them(m, n, k, dtype):
+    """Every row and column of the large tiles' kernel, rows and columns in samples against the definition."""
+    a, sa, b, sb, bias = operands(m, n, k)
+    y = seq.block_matmul(a, sa, b, sb, bias=bias, dtype=dtype)
+    rows = torch.cat([torch.arange(0, m, 97), torch.arange(m - 40, m)]).cuda()
+    check(a.view(torch.uint8)[rows].view(F8), sa[rows], b, sb, bias, y[rows], "rows")
+    cols = (n + 127) // 128
+    for j in (0, cols // 2, cols - 1):          # whole columns of 128
+        at = slice(128 * j, min(n, 128 * (j + 1)))
+        check(a, sa, b[at], sb[j:j + 1], bias[at], y[:, at], f"columns of block {j}")
+
+
+def test_large_product_with_numbers_behind_the_rows_and_a_wider_result():
+    m, n, k = 2300, 3900, 200
+    a, sa, b, sb, bias = operands(m, n, k)
+    wa, wb = (torch.full((t.shape[0], 256), float("nan"), device="cuda").to(F8) for t in (a, b))
+    wa[:, :k], wb[:, :k] = a, b
+    want = seq.block_matmul(a, sa, b, sb, bias=bias)
+    assert torch.equal(seq.block_matmul(wa[:, :k], sa, wb[:, :k], sb, bias=bias), want)
+    for off in (0, 8, 3):
+        out = torch.full((m, n + 20), 7.0, dtype=torch.bfloat16, device="cuda")
+        assert torch.equal(seq.block_matmul(a, sa.contiguous(), b, sb, bias=bias, out=out[:, off:off + n]), want)
+        out[:, off:off + n] = 7
+        assert (out == 7).all()
