@@ -24,23 +24,39 @@ template <> struct Elem<XL_BF16> {
     typedef __bf16 T;
 };
 
-// V elements at p as fp32; VEC: p is aligned to their size together, and one load brings them.
-template <int DT, int V> __device__ __forceinline__ void load_vec(const void *p, long long at, float *out)
+template <typename T, int V> using Vec = T __attribute__((ext_vector_type(V)));
+
+// V elements at p, of any alignment, as one access.
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
 {
-    typedef typename Elem<DT>::T T;
-    typedef T Vec __attribute__((ext_vector_type(V)));
-    const Vec v = *reinterpret_cast<const Vec *>(static_cast<const T *>(p) + at);
-#pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = (float)v[i];
+    Vec<T, V> v;
+    __builtin_memcpy(&v, p, V * sizeof(T));
+    return v;
 }
-template <int DT, int V> __device__ __forceinline__ void store_vec(void *p, long long at, const float *in)
+template <typename T, int V> __device__ __forceinline__ void store_vec(T *p, Vec<T, V> v) { __builtin_memcpy(p, &v, V * sizeof(T)); }
+
+// V elements at p, of any alignment, of which the first n exist; the others come out as zeros.
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_some(const T *p, int n)
 {
-    typedef typename Elem<DT>::T T;
-    typedef T Vec __attribute__((ext_vector_type(V)));
-    Vec v;
+    Vec<T, V> v = {};
+    if (n >= V) {
+        v = load_vec<T, V>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = (T)in[i];
-    *reinterpret_cast<Vec *>(static_cast<T *>(p) + at) = v;
+        for (int i = 0; i < V; ++i)
+            if (i < n) v[i] = p[i];
+    }
+    return v;
+}
+template <typename T, int V> __device__ __forceinline__ void store_some(T *p, int n, Vec<T, V> v)
+{
+    if (n >= V) {
+        store_vec<T, V>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = v[i];
+    }
 }
 
 // One hardware exponential (about one unit in the last place; results below the normal range are zero).

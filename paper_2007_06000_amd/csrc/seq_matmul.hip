@@ -77,28 +77,21 @@ __device__ __forceinline__ u32x4 load16(const char *row, int k, int K)
     return v;
 }
 
-template <int DT> __device__ __forceinline__ void store4(const xl_block_matmul_args &a, long long i, int j, f32x4 v, bool wide)
+template <int DT> __device__ __forceinline__ void store4(const xl_block_matmul_args &a, long long i, int j, f32x4 v)
 {
     typedef typename Elem<DT>::T T;
     if (i >= a.m || j >= a.n) return;
-    float out[4];
+    Vec<T, 4> out;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = v[k] + (a.bias && j + k < a.n ? a.bias[j + k] : 0.f);
-    T *y = static_cast<T *>(a.y) + i * a.y_row;
-    if (wide && j + 4 <= a.n) {
-        store_vec<DT, 4>(y, j, out);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (j + k < a.n) y[j + k] = (T)out[k];
-    }
+    for (int k = 0; k < 4; ++k) out[k] = (T)(v[k] + (a.bias && j + k < a.n ? a.bias[j + k] : 0.f));
+    store_some<T, 4>(static_cast<T *>(a.y) + i * a.y_row + j, (int)(a.n - j), out);
 }
 
 // Few rows of a: what costs is reading b once.  16 rows of b and MT x 16 of a a workgroup, whose eight waves take the blocks in turn; their sums meet in LDS, in the
 // same order every time.  (16 x 4096 x 2048: 3.9 us, of which an empty launch is 2.6; 16 x 8192 x 8192: 17.0 us, 4.0 TB/s.  Four or sixteen waves, or the
 // operands of two or four blocks on their way at once, measured the same within 5 %.)
 template <int DT, int MT>
-__global__ __launch_bounds__(512) void thin_kernel(const xl_block_matmul_args a, int tiles_n, bool wide)
+__global__ __launch_bounds__(512) void thin_kernel(const xl_block_matmul_args a, int tiles_n)
 {
     constexpr int WAVES = 8;
     typedef BlockProduct<DT == XL_F32> P;
@@ -155,7 +148,7 @@ __global__ __launch_bounds__(512) void thin_kernel(const xl_block_matmul_args a,
         f32x4 sum = part[0][i][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) sum += part[w][i][lane];
-        store4<DT>(a, m0 + i * 16 + col, n0 + quad * 4, sum, wide);
+        store4<DT>(a, m0 + i * 16 + col, n0 + quad * 4, sum);
     }
 }
 
@@ -185,7 +178,7 @@ __device__ __forceinline__ void to_lds4(__amdgpu_buffer_rsrc_t from, void *to, u
 }
 
 template <int DT, int BM, int BN, int WM, int WN, int KS, int S>
-__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmul_args p, int tiles_m, int tiles_n, bool wide)
+__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmul_args p, int tiles_m, int tiles_n)
 {
     typedef typename Elem<DT>::T T;
     constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB + 1;
@@ -363,12 +356,11 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            typedef T Four __attribute__((ext_vector_type(4)));
-            Four v;
+            Vec<T, 4> v;
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = (T)(acc[i][j][k] + bias[k]);
             const int at = (j * 16 + quad * 4) * sizeof(T);
-            *reinterpret_cast<Four *>(mine + (i * 16 + col) * ROW + ((at / 16) ^ (col & (CHUNKS - 1))) * 16 + at % 16) = v;
+            *reinterpret_cast<Vec<T, 4> *>(mine + (i * 16 + col) * ROW + ((at / 16) ^ (col & (CHUNKS - 1))) * 16 + at % 16) = v;
         }
     }
     wave_sync();
@@ -377,23 +369,16 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
 #pragma unroll
     for (int i = 0; i < TM * 16 / (64 / CHUNKS); ++i, y += 64 / CHUNKS * p.y_row) {
         const int r = i * (64 / CHUNKS) + lane / CHUNKS;
-        typedef T Chunk __attribute__((ext_vector_type(PER)));
-        const Chunk v = *reinterpret_cast<const Chunk *>(mine + r * ROW + ((lane % CHUNKS) ^ (r & (CHUNKS - 1))) * 16);
+        const Vec<T, PER> v = *reinterpret_cast<const Vec<T, PER> *>(mine + r * ROW + ((lane % CHUNKS) ^ (r & (CHUNKS - 1))) * 16);
         if (m0 + wm * TM * 16 + r >= p.m) continue;
-        if (wide && live == PER) {
-            *reinterpret_cast<Chunk *>(y) = v;
-        } else {
-#pragma unroll
-            for (int k = 0; k < PER; ++k)
-                if (k < live) y[k] = v[k];
-        }
+        store_some<T, PER>(y, live, v);
     }
 }
 
-template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError_t launch_tile(const xl_block_matmul_args &a, bool wide, hipStream_t s)
+template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError_t launch_tile(const xl_block_matmul_args &a, hipStream_t s)
 {
     const long long tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
-    tile_kernel<DT, BM, BN, WM, WN, KS, S><<<dim3((unsigned)(tm * tn)), 64 * WM * WN, 0, s>>>(a, (int)tm, (int)tn, wide);
+    tile_kernel<DT, BM, BN, WM, WN, KS, S><<<dim3((unsigned)(tm * tn)), 64 * WM * WN, 0, s>>>(a, (int)tm, (int)tn);
     return hipGetLastError();
 }
 
@@ -401,17 +386,14 @@ static constexpr long long CUS = 256;
 
 template <int DT, int MT> static hipError_t launch_thin(const xl_block_matmul_args &a, hipStream_t s)
 {
-    typedef typename Elem<DT>::T T;
-    const unsigned long long at = (unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T);
     const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 16 * MT - 1) / (16 * MT));
-    thin_kernel<DT, MT><<<dim3((unsigned)tiles), 512, 0, s>>>(a, (int)tiles_n, at % (4 * sizeof(T)) == 0);
+    thin_kernel<DT, MT><<<dim3((unsigned)tiles), 512, 0, s>>>(a, (int)tiles_n);
     return hipGetLastError();
 }
 
 template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)
 {
     typedef typename Elem<DT>::T T;
-    const bool wide = ((unsigned long long)a.y | (unsigned long long)a.y_row * sizeof(T)) % 16 == 0;
     const long long blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
     // a tile of the tile kernel lies within 31 bits, and so do its scales
     const long long limit = 1ll << 22;
@@ -421,20 +403,20 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
     // The smallest tiles that still have a compute unit each, or share one by twos, then larger ones (us, bf16, k 2048, tiles of 64 alone / by twos, 128 alone / by twos, 256: 1024 x 1024 7.2, 8.5,
     // 11.9, 13.9, 25; 1024 x 2048 12.9, 10.5, 12.2, 14.2, 26; 1024 x 4096 24, 18.5, 13.0, 15.1, 26; 2048 x 4096 46, 34, 24, 21, 28; 4096 x 4096 90, 66, 46, 41, 33).
     auto tiles = [](long long m, long long n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-    if (tiles(a.m, a.n, 64) <= CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 3>(a, wide, s);
-    if (tiles(a.m, a.n, 64) <= 2 * CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 2>(a, wide, s);
-    if (tiles(a.m, a.n, 128) <= CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 4>(a, wide, s);
+    if (tiles(a.m, a.n, 64) <= CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 3>(a, s);
+    if (tiles(a.m, a.n, 64) <= 2 * CUS) return launch_tile<DT, 64, 64, 4, 2, 2, 2>(a, s);
+    if (tiles(a.m, a.n, 128) <= CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 4>(a, s);
     if constexpr (DT == XL_F32) {
-        return launch_tile<DT, 128, 128, 2, 2, 1, 2>(a, wide, s);       // (four waves: 68 us, eight: 69, at 4096 x 4096 x 2048)
+        return launch_tile<DT, 128, 128, 2, 2, 1, 2>(a, s);       // (four waves: 68 us, eight: 69, at 4096 x 4096 x 2048)
     } else {
-        if (tiles(a.m, a.n, 128) <= 2 * CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 2>(a, wide, s);
+        if (tiles(a.m, a.n, 128) <= 2 * CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 2>(a, s);
         // Tiles of 256 go through the chip in rounds of one a compute unit, and the last round may have few.  Where smaller tiles can do with what is left in less than half a
         // round, they do, in a second launch (24642 x 4096 x 4096: 386 us in seven rounds, 350 so).
         const long long tn = (a.n + 255) / 256, rows = tiles(a.m, a.n, 256) / CUS * CUS / tn * 256;
         if (rows > 0 && rows < a.m && blocks >= 8 && tiles(a.m - rows, a.n, 128) <= CUS) {
             xl_block_matmul_args part = a;
             part.m = rows;
-            const hipError_t e = launch_tile<DT, 256, 256, 2, 4, 1, 2>(part, wide, s);
+            const hipError_t e = launch_tile<DT, 256, 256, 2, 4, 1, 2>(part, s);
             if (e != hipSuccess) return e;
             part.m = a.m - rows;
             part.a = static_cast<const char *>(a.a) + rows * a.a_row;
@@ -442,7 +424,7 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
             part.y = static_cast<T *>(a.y) + rows * a.y_row;
             return launch_type<DT>(part, s);
         }
-        return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, wide, s);
+        return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, s);
     }
 }
 

@@ -25,15 +25,12 @@ __device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)
 }
 
 // Eight numbers of a row from column k on; those past its end are zeros.
-template <int DT, bool WIDE> __device__ __forceinline__ void load8(const typename Elem<DT>::T *x, long long at, int k, int K, float *v)
+template <int DT> __device__ __forceinline__ void load8(const typename Elem<DT>::T *x, long long at, int k, int K, float *v)
 {
-    if (WIDE && k + 8 <= K) {
-        if (DT == XL_F32) {
-            load_vec<DT, 4>(x, at + k, v);
-            load_vec<DT, 4>(x, at + k + 4, v + 4);
-        } else {
-            load_vec<DT, 8>(x, at + k, v);
-        }
+    if (k + 8 <= K) {
+        const Vec<typename Elem<DT>::T, 8> w = load_vec<typename Elem<DT>::T, 8>(x + at + k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
         return;
     }
 #pragma unroll
@@ -42,7 +39,7 @@ template <int DT, bool WIDE> __device__ __forceinline__ void load8(const typenam
 
 // One row's blocks: 16 lanes a block, 8 numbers a lane.  The 16 blocks of a workgroup lie under each other, in 16 rows: their
 // scales are neighbours where a column of scales is contiguous, as the product wants them.
-template <int DT, bool WIDE>
+template <int DT>
 __global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
 {
     typedef typename Elem<DT>::T T;
@@ -50,7 +47,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
     const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
     if (row >= a.rows) return;
     float v[8];
-    load8<DT, WIDE>(static_cast<const T *>(a.x), row * a.x_row, k, K, v);
+    load8<DT>(static_cast<const T *>(a.x), row * a.x_row, k, K, v);
     unsigned most = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
@@ -65,7 +62,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
 }
 
 // A block of 128 rows by 128 columns a workgroup; a thread has 8 columns of every sixteenth row.  Weights are quantised once.
-template <int DT, bool WIDE>
+template <int DT>
 __global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
 {
     typedef typename Elem<DT>::T T;
@@ -78,7 +75,7 @@ __global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
     for (int r = 0; r < 8; ++r) {
         const long long row = row0 + r * 16;
         if (row < a.rows) {
-            load8<DT, WIDE>(static_cast<const T *>(a.x), row * a.x_row, k, K, v[r]);
+            load8<DT>(static_cast<const T *>(a.x), row * a.x_row, k, K, v[r]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[r][i]));
         }
@@ -104,16 +101,13 @@ __global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
 
 template <int DT> static hipError_t launch_type(const xl_quantize_args &a, hipStream_t s)
 {
-    const bool wide = ((unsigned long long)a.x | (unsigned long long)a.x_row * sizeof(typename Elem<DT>::T)) % 16 == 0;
     const unsigned kb = (unsigned)((a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK);
     if (a.block_rows == 1) {
         const dim3 grid((unsigned)((a.rows + 15) / 16), kb);
-        if (wide) rows_kernel<DT, true><<<grid, 256, 0, s>>>(a);
-        else rows_kernel<DT, false><<<grid, 256, 0, s>>>(a);
+        rows_kernel<DT><<<grid, 256, 0, s>>>(a);
     } else {
         const dim3 grid((unsigned)((a.rows + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK), kb);
-        if (wide) blocks_kernel<DT, true><<<grid, 256, 0, s>>>(a);
-        else blocks_kernel<DT, false><<<grid, 256, 0, s>>>(a);
+        blocks_kernel<DT><<<grid, 256, 0, s>>>(a);
     }
     return hipGetLastError();
 }

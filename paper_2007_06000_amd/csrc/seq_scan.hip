@@ -10,7 +10,6 @@ namespace xls {
 
 // A sequence's rows of one tensor: element [t][i] lies t * step + i elements behind `base`.  Where rows are aligned, of whole vectors and in 2 GB (`wide`) a buffer covers exactly the
 // tokens that the sequence has, so that one past its end reads as zeros and its store goes nowhere, without a comparison.
-template <typename T, int V> using Vec = T __attribute__((ext_vector_type(V)));
 struct Rows {
     __amdgpu_buffer_rsrc_t rsrc;
     __device__ __forceinline__ Rows(const void *base, long long step, int rows, int width, int size)
@@ -37,30 +36,6 @@ struct Rows {
     }
 };
 static constexpr unsigned NOWHERE = 0x80000000u;       // past the end of every such buffer
-
-// The general case, for rows of any alignment: the first n of V elements exist, the others come out as zeros.
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_some(const T *p, int n)
-{
-    Vec<T, V> v = {};
-    if (n >= V) {
-        __builtin_memcpy(&v, p, sizeof v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) v[i] = p[i];
-    }
-    return v;
-}
-template <typename T, int V> __device__ __forceinline__ void store_some(T *p, int n, Vec<T, V> v)
-{
-    if (n >= V) {
-        __builtin_memcpy(p, &v, sizeof v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = v[i];
-    }
-}
 
 // A token after the other: LP lanes a channel, four states (a 16-byte load) a lane, 256 / LP channels a workgroup.
 template <int DT, int LP>
