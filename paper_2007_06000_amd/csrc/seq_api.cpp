@@ -138,7 +138,7 @@ xl_status xl_quantize_blocks(const xl_quantize_args *args, void *stream)
     const int size = size_of(a.dtype);
     if (!size) return fail(XL_E_UNSUPPORTED, "%s: unknown element type %lld", w, a.dtype);
     if (a.block_rows != 1 && a.block_rows != XL_SCALE_BLOCK) return fail(XL_E_UNSUPPORTED, "%s: blocks of %lld rows (1 or %d)", w, a.block_rows, XL_SCALE_BLOCK);
-    if (!is_size(a.rows) || !is_size(a.k) || a.k > 65535ll * XL_SCALE_BLOCK) return fail(XL_E_SHAPE, "%s: %lld rows of %lld out of range", w, a.rows, a.k);
+    if (!is_size(a.rows) || !is_size(a.k)) return fail(XL_E_SHAPE, "%s: %lld rows of %lld out of range", w, a.rows, a.k);
     if (a.rows == 0 || a.k == 0) return XL_OK;
     if (!a.x || !a.q || !a.scales) return fail(XL_E_NULL, "%s: x, q or scales is NULL", w);
     if (!aligned(a.x, size) || !aligned(a.scales, 4)) return fail(XL_E_ALIGN, "%s: x or scales is not aligned to its elements", w);
