@@ -55,8 +55,7 @@ def _fail(status: int, message: str):
     raise XlError(status, message)
 
 
-def _call(name: str, packed: bytes, device: int):
-    f = getattr(_lib or lib(), name)
+def _call(f, packed: bytes, device: int):
     if torch._C._cuda_getDevice() == device:
         st = f(packed, torch._C._cuda_getCurrentRawStream(device))
     else:
@@ -66,48 +65,61 @@ def _call(name: str, packed: bytes, device: int):
         raise XlError(st, lib().xl_seq_last_error().decode())
 
 
-def _check(what: str, device: torch.device, tensors):
-    """(name, tensor or None, type or None, shape or None) each: on the device, of the type and shape, no gradient asked for."""
-    if device.type != "cuda":
+# A call of one token takes the GPU 2 to 6 us, less than the host needs to check a dozen tensors by their names: what fits is let through by one
+# test of a tensor's attributes, and only what does not is looked at again to say why.
+
+def _device(what: str, t: torch.Tensor) -> int:
+    if not t.is_cuda:
         _fail(XL_E_DEVICE, f"{what}: tensors must be on a GPU (there is no CPU path)")
-    grad = torch.is_grad_enabled()
-    for name, t, dtype, shape in tensors:
-        if t is None:
-            continue
-        if t.device != device:
-            _fail(XL_E_DEVICE, f"{what}: {name} is on {t.device}, not on {device}")
-        if dtype is not None and t.dtype != dtype:
-            _fail(XL_E_UNSUPPORTED, f"{what}: {name} is {t.dtype}, not {dtype}")
-        if shape is not None and t.shape != shape:
-            _fail(XL_E_SHAPE, f"{what}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-        if grad and t.requires_grad:
-            _fail(XL_E_UNSUPPORTED, f"{what}: {name} asks for a gradient: inference only")
+    return t.get_device()
 
 
-def _rows(what: str, name: str, t: torch.Tensor) -> Tuple[int, int]:
+def _refuse(what: str, name: str, t: torch.Tensor, dtype, shape, device: int, dense: bool):
+    if t.get_device() != device:
+        _fail(XL_E_DEVICE, f"{what}: {name} is on {t.device}, not on cuda:{device}")
+    if t.dtype != dtype:
+        _fail(XL_E_UNSUPPORTED, f"{what}: {name} is {t.dtype}, not {dtype}")
+    if t.shape != shape:
+        _fail(XL_E_SHAPE, f"{what}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _fail(XL_E_UNSUPPORTED, f"{what}: {name} asks for a gradient: inference only")
+    if dense and not t.is_contiguous():
+        _fail(XL_E_SHAPE, f"{what}: {name} must be contiguous")
+
+
+def _check(what: str, name: str, t: torch.Tensor, dtype, shape, device: int):
+    """A tensor with strides of its own: on the device, of the type and shape, no gradient asked for."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or t.requires_grad:
+        _refuse(what, name, t, dtype, shape, device, False)
+
+
+def _rows(what: str, name: str, t: torch.Tensor, dtype, shape, device: int) -> Tuple[int, int]:
     """Steps between sequences and tokens of [batch, length, width] with a contiguous last dimension."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or t.requires_grad:
+        _refuse(what, name, t, dtype, shape, device, False)
     b, n, c = t.stride()
-    if c != 1 and t.shape[2] > 1:
+    if c != 1 and shape[2] > 1:
         _fail(XL_E_SHAPE, f"{what}: the last dimension of {name} must be contiguous")
     return b, n
 
 
-def _dense(what: str, name: str, t: Optional[torch.Tensor]) -> int:
+def _dense(what: str, name: str, t: Optional[torch.Tensor], dtype, shape, device: int) -> int:
+    """The address of a contiguous tensor, or 0."""
     if t is None:
         return 0
-    if not t.is_contiguous():
-        _fail(XL_E_SHAPE, f"{what}: {name} must be contiguous")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or t.requires_grad or not t.is_contiguous():
+        _refuse(what, name, t, dtype, shape, device, True)
     return t.data_ptr()
 
 
-def _states(what: str, batch: int, tail: Tuple[int, ...], dtype, device, state, new_state, slots):
-    """The state that goes in, the one that comes out and their number of rows."""
-    if slots is not None and state is None:
+def _states(what: str, batch: int, tail: Tuple[int, ...], like: torch.Tensor, state, new_state, slots):
+    """The state's shape and the one that comes out, which is made like `like` if there is none yet."""
+    if slots is None:
+        shape = (batch, *tail)
+        return shape, like.new_empty(shape) if new_state is None else new_state
+    if state is None:
         _fail(XL_E_SHAPE, f"{what}: slots name rows of a state, and none is given")
-    rows = state.shape[0] if slots is not None and state.dim() else batch
-    if new_state is None:
-        new_state = state if slots is not None else torch.empty((batch, *tail), dtype=dtype, device=device)
-    return rows, (rows, *tail), new_state
+    return (state.shape[0] if state.dim() else batch, *tail), state if new_state is None else new_state
 
 
 def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *, silu: bool = True,
@@ -122,21 +134,20 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
     what = "causal_conv"
     if x.dim() != 3 or weight.dim() != 2:
         _fail(XL_E_SHAPE, f"{what}: x is [batch, length, channels] and weight [channels, taps]")
-    dtype, device = x.dtype, x.device
-    batch, length, channels = x.shape
-    taps = weight.shape[1]
-    rows, shape, new_state = _states(what, batch, (max(taps - 1, 0), channels), dtype, device, state, new_state, slots)
-    if out is None:
-        out = torch.empty((batch, length, channels), dtype=dtype, device=device)
+    device, dtype, size = _device(what, x), x.dtype, x.shape
     if dtype not in DTYPES:
         _fail(XL_E_UNSUPPORTED, f"{what}: x is {dtype}")
-    _check(what, device, (("x", x, None, None), ("weight", weight, torch.float32, (channels, taps)), ("bias", bias, torch.float32, (channels,)),
-                          ("state", state, dtype, shape), ("new_state", new_state, dtype, shape), ("lengths", lengths, torch.int32, (batch,)),
-                          ("slots", slots, torch.int32, (batch,)), ("out", out, dtype, x.shape)))
-    _call("xl_causal_conv", _CONV.pack(
-        batch, length, channels, taps, DTYPES[dtype], silu, *_rows(what, "x", x), *_rows(what, "out", out), rows, x.data_ptr(), _dense(what, "weight", weight),
-        _dense(what, "bias", bias), _dense(what, "state", state), _dense(what, "new_state", new_state), _dense(what, "lengths", lengths),
-        _dense(what, "slots", slots), out.data_ptr()), device.index)
+    batch, length, channels = size
+    taps = weight.shape[1]
+    shape, new_state = _states(what, batch, (max(taps - 1, 0), channels), x, state, new_state, slots)
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    f32, i32 = torch.float32, torch.int32
+    _call((_lib or lib()).xl_causal_conv, _CONV.pack(
+        batch, length, channels, taps, DTYPES[dtype], silu, *_rows(what, "x", x, dtype, size, device), *_rows(what, "out", out, dtype, size, device), shape[0],
+        x.data_ptr(), _dense(what, "weight", weight, f32, (channels, taps), device), _dense(what, "bias", bias, f32, (channels,), device),
+        _dense(what, "state", state, dtype, shape, device), _dense(what, "new_state", new_state, dtype, shape, device),
+        _dense(what, "lengths", lengths, i32, (batch,), device), _dense(what, "slots", slots, i32, (batch,), device), out.data_ptr()), device)
     return out, new_state
 
 
@@ -153,58 +164,63 @@ def selective_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: tor
     what = "selective_scan"
     if u.dim() != 3 or A.dim() != 2:
         _fail(XL_E_SHAPE, f"{what}: u is [batch, length, channels] and A [channels, states]")
-    dtype, device = u.dtype, u.device
-    batch, length, channels = u.shape
-    n = A.shape[1]
-    rows, shape, new_state = _states(what, batch, (channels, n), torch.float32, device, state, new_state, slots)
-    if out is None:
-        out = torch.empty((batch, length, channels), dtype=dtype, device=device)
+    device, dtype, size = _device(what, u), u.dtype, u.shape
     if dtype not in DTYPES:
         _fail(XL_E_UNSUPPORTED, f"{what}: u is {dtype}")
-    wide, f32 = (batch, length, n), torch.float32
-    _check(what, device, (("u", u, None, None), ("delta", delta, dtype, u.shape), ("A", A, f32, (channels, n)), ("B", B, dtype, wide), ("C", C, dtype, wide),
-                          ("D", D, f32, (channels,)), ("z", z, dtype, u.shape), ("delta_bias", delta_bias, f32, (channels,)), ("state", state, f32, shape),
-                          ("new_state", new_state, f32, shape), ("lengths", lengths, torch.int32, (batch,)), ("slots", slots, torch.int32, (batch,)),
-                          ("out", out, dtype, u.shape)))
-    _call("xl_selective_scan", _SCAN.pack(
-        batch, length, channels, n, DTYPES[dtype], softplus, *_rows(what, "u", u), *_rows(what, "delta", delta),
-        *(_rows(what, "z", z) if z is not None else (0, 0)), *_rows(what, "out", out), *_rows(what, "B", B), *_rows(what, "C", C), rows, u.data_ptr(), delta.data_ptr(),
-        _dense(what, "A", A), B.data_ptr(), C.data_ptr(), _dense(what, "D", D), _dense(what, "delta_bias", delta_bias), z.data_ptr() if z is not None else 0,
-        _dense(what, "state", state), _dense(what, "new_state", new_state), _dense(what, "lengths", lengths), _dense(what, "slots", slots),
-        out.data_ptr()), device.index)
+    batch, length, channels = size
+    n = A.shape[1]
+    f32, i32, one, wide = torch.float32, torch.int32, (channels,), (batch, length, n)
+    a = _dense(what, "A", A, f32, (channels, n), device)
+    shape, new_state = _states(what, batch, (channels, n), A, state, new_state, slots)
+    if out is None:
+        out = torch.empty_like(u, memory_format=torch.contiguous_format)
+    gate, z_batch, z_token = 0, 0, 0
+    if z is not None:
+        gate = z.data_ptr()
+        z_batch, z_token = _rows(what, "z", z, dtype, size, device)
+    _call((_lib or lib()).xl_selective_scan, _SCAN.pack(
+        batch, length, channels, n, DTYPES[dtype], softplus, *_rows(what, "u", u, dtype, size, device), *_rows(what, "delta", delta, dtype, size, device),
+        z_batch, z_token, *_rows(what, "out", out, dtype, size, device), *_rows(what, "B", B, dtype, wide, device), *_rows(what, "C", C, dtype, wide, device),
+        shape[0], u.data_ptr(), delta.data_ptr(), a, B.data_ptr(), C.data_ptr(), _dense(what, "D", D, f32, one, device),
+        _dense(what, "delta_bias", delta_bias, f32, one, device), gate, _dense(what, "state", state, f32, shape, device),
+        _dense(what, "new_state", new_state, f32, shape, device), _dense(what, "lengths", lengths, i32, (batch,), device),
+        _dense(what, "slots", slots, i32, (batch,), device), out.data_ptr()), device)
     return out, new_state
 
 
 def _quantize(what: str, x: torch.Tensor, block_rows: int, out, scales):
     if x.dim() != 2:
         _fail(XL_E_SHAPE, f"{what}: x is [rows, k]")
-    rows, k = x.shape
-    device = x.device
-    blocks = (k + SCALE_BLOCK - 1) // SCALE_BLOCK
+    device, dtype, size = _device(what, x), x.dtype, x.shape
+    if dtype not in DTYPES:
+        _fail(XL_E_UNSUPPORTED, f"{what}: x is {dtype}")
+    rows, k = size
+    shape = ((rows + block_rows - 1) // block_rows, (k + SCALE_BLOCK - 1) // SCALE_BLOCK)
+    f8, f32 = torch.float8_e4m3fn, torch.float32
     if out is None:
         wide = (k + 15) // 16 * 16
-        out = torch.empty((rows, wide), dtype=torch.float8_e4m3fn, device=device)
+        out = torch.empty((rows, wide), dtype=f8, device=x.device)
         if wide != k:
             out = out[:, :k]
     if scales is None:      # a column for each block: the product reads the scales of neighbouring rows together
-        scales = torch.empty((blocks, rows), dtype=torch.float32, device=device).t() if block_rows == 1 else \
-            torch.empty(((rows + block_rows - 1) // block_rows, blocks), dtype=torch.float32, device=device)
-    if x.dtype not in DTYPES:
-        _fail(XL_E_UNSUPPORTED, f"{what}: x is {x.dtype}")
-    _check(what, device, (("x", x, None, None), ("out", out, torch.float8_e4m3fn, x.shape),
-                          ("scales", scales, torch.float32, ((rows + block_rows - 1) // block_rows, blocks))))
-    if k > 1 and (x.stride(1) != 1 or out.stride(1) != 1):
+        scales = torch.empty_strided(shape, (1, rows) if block_rows == 1 else (shape[1], 1), dtype=f32, device=x.device)
+    _check(what, "x", x, dtype, size, device)
+    _check(what, "out", out, f8, size, device)
+    _check(what, "scales", scales, f32, shape, device)
+    (x_row, x_step), (q_row, q_step) = x.stride(), out.stride()
+    if k > 1 and (x_step != 1 or q_step != 1):
         _fail(XL_E_SHAPE, f"{what}: rows of x and out must be contiguous")
-    _readable(what, "out", out)
-    _call("xl_quantize_blocks", _QUANTIZE.pack(rows, k, block_rows, DTYPES[x.dtype], x.stride(0), out.stride(0), scales.stride(0), scales.stride(1),
-                                               x.data_ptr(), out.data_ptr(), scales.data_ptr()), device.index)
+    if k % 16:
+        _readable(what, "out", out)
+    _call((_lib or lib()).xl_quantize_blocks, _QUANTIZE.pack(rows, k, block_rows, DTYPES[dtype], x_row, q_row, *scales.stride(), x.data_ptr(), out.data_ptr(),
+                                                             scales.data_ptr()), device)
     return out, scales
 
 
 def _readable(what: str, name: str, t: torch.Tensor):
     """The memory of the last row of 8-bit numbers goes on to the next multiple of 16 bytes."""
     rows, k = t.shape
-    if k % 16 and rows and t.storage_offset() + (rows - 1) * t.stride(0) + (k + 15) // 16 * 16 > t.untyped_storage().nbytes():
+    if rows and t.storage_offset() + (rows - 1) * t.stride(0) + (k + 15) // 16 * 16 > t.untyped_storage().nbytes():
         _fail(XL_E_SHAPE, f"{what}: the last row of {name} must have memory up to the next multiple of 16 bytes")
 
 
@@ -224,24 +240,27 @@ def block_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sca
     what = "block_matmul"
     if a.dim() != 2 or b.dim() != 2:
         _fail(XL_E_SHAPE, f"{what}: a is [m, k] and b [n, k]")
-    m, k = a.shape
+    device, (m, k) = _device(what, a), a.shape
     n = b.shape[0]
-    device = a.device
+    shape, blocks, f8, f32 = (m, n), (k + SCALE_BLOCK - 1) // SCALE_BLOCK, torch.float8_e4m3fn, torch.float32
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=device)
+        out = torch.empty(shape, dtype=dtype, device=a.device)
     else:
         dtype = out.dtype
+        _check(what, "out", out, dtype, shape, device)
     if dtype not in DTYPES:
         _fail(XL_E_UNSUPPORTED, f"{what}: the result is {dtype}")
-    blocks = (k + SCALE_BLOCK - 1) // SCALE_BLOCK
-    f8, f32 = torch.float8_e4m3fn, torch.float32
-    _check(what, device, (("a", a, f8, None), ("b", b, f8, (n, k)), ("a_scales", a_scales, f32, (m, blocks)),
-                          ("b_scales", b_scales, f32, ((n + SCALE_BLOCK - 1) // SCALE_BLOCK, blocks)), ("bias", bias, f32, (n,)), ("out", out, None, (m, n))))
-    if (k > 1 and (a.stride(1) != 1 or b.stride(1) != 1)) or (n > 1 and out.stride(1) != 1):
+    _check(what, "a", a, f8, (m, k), device)
+    _check(what, "b", b, f8, (n, k), device)
+    _check(what, "a_scales", a_scales, f32, (m, blocks), device)
+    _check(what, "b_scales", b_scales, f32, ((n + SCALE_BLOCK - 1) // SCALE_BLOCK, blocks), device)
+    (a_row, a_step), (b_row, b_step), (y_row, y_step) = a.stride(), b.stride(), out.stride()
+    if (k > 1 and (a_step != 1 or b_step != 1)) or (n > 1 and y_step != 1):
         _fail(XL_E_SHAPE, f"{what}: rows of a, b and out must be contiguous")
-    _readable(what, "a", a)
-    _readable(what, "b", b)
-    _call("xl_block_matmul", _MATMUL.pack(m, n, k, DTYPES[dtype], a.stride(0), b.stride(0), *a_scales.stride(), *b_scales.stride(),
-                                          out.stride(0), a.data_ptr(), b.data_ptr(), a_scales.data_ptr(), b_scales.data_ptr(), _dense(what, "bias", bias),
-                                          out.data_ptr()), device.index)
+    if k % 16:
+        _readable(what, "a", a)
+        _readable(what, "b", b)
+    _call((_lib or lib()).xl_block_matmul, _MATMUL.pack(
+        m, n, k, DTYPES[dtype], a_row, b_row, *a_scales.stride(), *b_scales.stride(), y_row, a.data_ptr(), b.data_ptr(), a_scales.data_ptr(), b_scales.data_ptr(),
+        _dense(what, "bias", bias, f32, (n,), device), out.data_ptr()), device)
     return out
