@@ -27,8 +27,9 @@ def fields(name):
     return out
 
 
-STRUCTS = {"xl_causal_conv": ("xl_causal_conv_args", seq._CONV), "xl_selective_scan": ("xl_scan_args", seq._SCAN),
-           "xl_quantize_blocks": ("xl_quantize_args", seq._QUANTIZE), "xl_block_matmul": ("xl_block_matmul_args", seq._MATMUL)}
+# the argument structs: 64-bit numbers, then pointers
+STRUCTS = {"xl_causal_conv": ("xl_causal_conv_args", struct.Struct("=11q8Q")), "xl_selective_scan": ("xl_scan_args", struct.Struct("=19q13Q")),
+           "xl_quantize_blocks": ("xl_quantize_args", struct.Struct("=8q3Q")), "xl_block_matmul": ("xl_block_matmul_args", struct.Struct("=11q6Q"))}
 
 
 def call(name, **values):
