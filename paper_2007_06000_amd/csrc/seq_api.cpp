@@ -6,7 +6,7 @@
 #include <cstdio>
 #include <cstring>
 
-#include "seq_internal.h"
+#include "seq_launch.h"
 
 static thread_local char g_error[256] = "";
 

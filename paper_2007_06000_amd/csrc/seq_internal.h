@@ -1,8 +1,8 @@
-// What the kernels of the sequence operators share: element types, division of work, launchers.
+// What the kernels of the sequence operators share: element types, accesses, elementary functions.
 #pragma once
 #include <hip/hip_runtime.h>
 
-#include "xl_seq.h"
+#include "seq_launch.h"
 
 namespace xls {
 
@@ -101,10 +101,5 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-
-hipError_t launch_causal_conv(const xl_causal_conv_args &a, hipStream_t s);
-hipError_t launch_selective_scan(const xl_scan_args &a, hipStream_t s);
-hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t s);
-hipError_t launch_block_matmul(const xl_block_matmul_args &a, hipStream_t s);
 
 }  // namespace xls
