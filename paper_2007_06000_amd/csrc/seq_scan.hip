@@ -8,7 +8,7 @@
 
 namespace xls {
 
-// A sequence's rows of one tensor: element [t][i] lies t * step + i elements behind `base`.  Where rows are aligned, of whole vectors and in 2 GB (`wide`) a buffer covers exactly the
+// A sequence's rows of one tensor: element [t][i] lies t * step + i elements behind `base`.  Where rows do not overlap and a sequence lies within 2 GB a buffer covers exactly the
 // tokens that the sequence has, so that one past its end reads as zeros and its store goes nowhere, without a comparison.
 struct Rows {
     __amdgpu_buffer_rsrc_t rsrc;
@@ -36,6 +36,10 @@ struct Rows {
     }
 };
 static constexpr unsigned NOWHERE = 0x80000000u;       // past the end of every such buffer
+
+// How a lane reads its part of a tile: up to four numbers of a token at once, where rows are aligned and of whole vectors; one number of as many tokens; and
+// the same with comparisons and 64-bit addresses, where there are no such buffers.
+enum Access { VECTORS, SINGLES, SCATTERED };
 
 // A token after the other: LP lanes a channel, four states (a 16-byte load) a lane, 256 / LP channels a workgroup.
 template <int DT, int LP>
@@ -111,13 +115,13 @@ template <int LP> __device__ __forceinline__ float sum_over_lanes(float *p, int 
 // folds those of the waves before it into the state that it begins with, and runs its tokens again, the factors and inputs
 // still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
 // tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
-template <int DT, int LP, int NS, int W, int TK>
-__global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups, bool wide, bool wide_bc)
+template <int DT, int LP, int NS, int W, int TK, Access ACCESS>
+__global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups)
 {
     typedef typename Elem<DT>::T T;
     constexpr int CH = 64 / LP, NP = LP * NS, TT = W * TK, PT = TK + 4;
-    constexpr int PER = CH * TK / 64, VE = PER < 4 ? PER : 4, IT = PER / VE;            // a thread's part of a tile's u, delta, z and y
-    constexpr int PERB = NP * TK / 64, VB = PERB < 4 ? PERB : 4, IB = PERB / VB;        // and of its B and C
+    constexpr int PER = CH * TK / 64, VE = ACCESS != VECTORS ? 1 : PER < 4 ? PER : 4, IT = PER / VE;    // a thread's part of a tile's u, delta, z and y
+    constexpr int PERB = NP * TK / 64, VB = ACCESS != VECTORS ? 1 : PERB < 4 ? PERB : 4, IB = PERB / VB; // and of its B and C
     static_assert(PER >= 1 && PERB >= 1 && TK % LP == 0, "a wave's tokens divide among its lanes");
     __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT];    // steps, and step x input (later the outputs): [channel][token]
     __shared__ float Bs_all[W][TK * NP], Cs_all[W][TK * NP];    // [token][state]
@@ -156,22 +160,27 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     const unsigned u_at = nc > 0 ? ((tw + et) * (unsigned)a.u_token + ec) * S : NOWHERE, d_at = nc > 0 ? ((tw + et) * (unsigned)a.delta_token + ec) * S : NOWHERE, z_at = nc > 0 ? ((tw + et) * (unsigned)a.z_token + ec) * S : NOWHERE;
     const unsigned y_at = nc > 0 ? ((tw + et) * (unsigned)a.y_token + ec) * S : NOWHERE, b_at = nb > 0 ? ((tw + bt) * (unsigned)a.b_token + bn) * S : NOWHERE, c_at = nb > 0 ? ((tw + bt) * (unsigned)a.c_token + bn) * S : NOWHERE;
 
-    const int tokens = wide ? len : 0, tokens_bc = wide_bc ? len : 0;
+    const int tokens = ACCESS != SCATTERED ? len : 0;
     const int width = min(CH, D - c0);
     const Rows urows(up, a.u_token, tokens, width, S), drows(dp, a.delta_token, tokens, width, S), zrows(zp, a.z_token, a.z ? tokens : 0, width, S);
-    const Rows yrows(yp, a.y_token, tokens, width, S), Brows(Bp, a.b_token, tokens_bc, N, S), Crows(Cp, a.c_token, tokens_bc, N, S);
+    const Rows yrows(yp, a.y_token, tokens, width, S), Brows(Bp, a.b_token, tokens, N, S), Crows(Cp, a.c_token, tokens, N, S);
     const unsigned u_row = (unsigned)a.u_token * S, d_row = (unsigned)a.delta_token * S, z_row = a.z ? (unsigned)a.z_token * S : 0, y_row = (unsigned)a.y_token * S;
     const unsigned b_row = (unsigned)a.b_token * S, c_row = (unsigned)a.c_token * S;
 
     Vec<T, VE> ur[IT], dr[IT], zr[IT];
     Vec<T, VB> Br[IB], Cr[IB];
     auto fetch = [&](int t0) {
-        if (wide) {
+        if constexpr (ACCESS != SCATTERED) {
 #pragma unroll
             for (int k = 0; k < IT; ++k) {
                 ur[k] = urows.template load<Vec<T, VE>>(u_at + k * ET * u_row, t0 * u_row);
                 dr[k] = drows.template load<Vec<T, VE>>(d_at + k * ET * d_row, t0 * d_row);
                 zr[k] = zrows.template load<Vec<T, VE>>(z_at + k * ET * z_row, t0 * z_row);
+            }
+#pragma unroll
+            for (int k = 0; k < IB; ++k) {
+                Br[k] = Brows.template load<Vec<T, VB>>(b_at + k * BT * b_row, t0 * b_row);
+                Cr[k] = Crows.template load<Vec<T, VB>>(c_at + k * BT * c_row, t0 * c_row);
             }
         } else {
 #pragma unroll
@@ -182,14 +191,6 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
                 dr[k] = load_some<T, VE>(dp + t * a.delta_token + ec, n);
                 zr[k] = load_some<T, VE>(zp + t * a.z_token + ec, a.z ? n : 0);
             }
-        }
-        if (wide_bc) {
-#pragma unroll
-            for (int k = 0; k < IB; ++k) {
-                Br[k] = Brows.template load<Vec<T, VB>>(b_at + k * BT * b_row, t0 * b_row);
-                Cr[k] = Crows.template load<Vec<T, VB>>(c_at + k * BT * c_row, t0 * c_row);
-            }
-        } else {
 #pragma unroll
             for (int k = 0; k < IB; ++k) {
                 const long long t = t0 + tw + bt + k * BT;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             Vec<T, VE> v;
 #pragma unroll
             for (int i = 0; i < VE; ++i) v[i] = (T)out[i];
-            if (wide) yrows.store(y_at + k * ET * y_row, t0 * y_row, v);
+            if constexpr (ACCESS != SCATTERED) yrows.store(y_at + k * ET * y_row, t0 * y_row, v);
             else if (t0 + tw + t < len) store_some<T, VE>(yp + (t0 + tw + t) * a.y_token + ec, nc, v);
         }
     }
@@ -340,18 +341,22 @@ template <int DT, int LP, int NS, int W, int TK> static hipError_t launch_tile(c
     typedef typename Elem<DT>::T T;
     constexpr int CH = 64 / LP, PER = CH * TK / 64, VE = PER < 4 ? PER : 4, PERB = LP * NS * TK / 64, VB = PERB < 4 ? PERB : 4;
     const int groups = (int)((a.channels + CH - 1) / CH);
+    const dim3 grid((unsigned)(groups * a.batch));
     const unsigned long long at = (unsigned long long)a.u | (unsigned long long)a.delta | (unsigned long long)a.z | (unsigned long long)a.y;
     const unsigned long long steps = a.u_batch | a.u_token | a.delta_batch | a.delta_token | a.z_batch | a.z_token | a.y_batch | a.y_token;
     const unsigned long long at_bc = (unsigned long long)a.B | (unsigned long long)a.C, steps_bc = a.b_batch | a.b_token | a.c_batch | a.c_token;
-    // a sequence's rows in one buffer: aligned, not overlapping (what follows the last token stays outside), offsets within 31 bits also a tile past the end
+    const bool vectors = (at | steps * sizeof(T)) % (VE * sizeof(T)) == 0 && a.channels % VE == 0 && (at_bc | steps_bc * sizeof(T)) % (VB * sizeof(T)) == 0 && a.states % VB == 0;
+    // a sequence's rows in one buffer: not overlapping (what follows the last token stays outside), offsets within 31 bits also a tile past the end
     auto rows = [&](long long width, std::initializer_list<long long> tokens) {
         for (long long t : tokens)
             if (t < width || t > INT_MAX / (long long)sizeof(T) / (a.length + 2 * W * TK)) return false;
         return true;
     };
-    const bool wide = (at | steps * sizeof(T)) % (VE * sizeof(T)) == 0 && a.channels % VE == 0 && rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token}));
-    const bool wide_bc = (at_bc | steps_bc * sizeof(T)) % (VB * sizeof(T)) == 0 && a.states % VB == 0 && rows(a.states, {a.b_token, a.c_token});
-    tile_kernel<DT, LP, NS, W, TK><<<dim3((unsigned)(groups * a.batch)), 64 * W, 0, s>>>(a, groups, wide, wide_bc);
+    const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
+    // 2 x 12321 x 2048 with 16 states in bf16: 283 us as vectors, 322 one by one, 561 scattered (these with four waves in every case)
+    if (!buffers) tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<grid, 64 * 4, 0, s>>>(a, groups);
+    else if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups);
+    else tile_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups);
     return hipGetLastError();
 }
 
