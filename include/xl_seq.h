@@ -80,6 +80,7 @@ typedef struct xl_scan_args {
     long long u_batch, u_token, delta_batch, delta_token, z_batch, z_token, y_batch, y_token;
     long long b_batch, b_token, c_batch, c_token;
     long long nslots;
+    long long workspace_bytes;
     const void *u, *delta;
     const float *A;                         /* [channels, states]                       */
     const void *B, *C;                      /* [batch, length, states]                  */
@@ -89,8 +90,14 @@ typedef struct xl_scan_args {
     float *new_state;
     const int *lengths, *slots;
     void *y;
+    void *workspace;
 } xl_scan_args;
 xl_status xl_selective_scan(const xl_scan_args *args, void *stream);
+
+/* Bytes of device memory (aligned to 16) with which xl_selective_scan is faster for arguments of these sizes: where there are too few channels for the
+ * chip a sequence is cut into parts that are worked on at the same time, in two kernels.  0 if there is nothing to gain.  With less, or NULL, the
+ * call does without; the results agree up to rounding.  The memory holds nothing between calls. */
+long long xl_selective_scan_workspace(const xl_scan_args *args);
 
 /*
  * x [rows, k] -> q [rows, k] in e4m3 and scales: x is about q * scale.  A scale is max(max|x| / 448, 2^-126) over its

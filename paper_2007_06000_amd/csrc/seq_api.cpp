@@ -125,9 +125,18 @@ xl_status xl_selective_scan(const xl_scan_args *args, void *stream)
     if (!a.A) return fail(XL_E_NULL, "%s: A is NULL", w);
     if (!aligned(a.A, 4) || !aligned(a.D, 4) || !aligned(a.delta_bias, 4) || !aligned(a.state, 4) || !aligned(a.new_state, 4))
         return fail(XL_E_ALIGN, "%s: A, D, delta_bias or a state is not aligned to its elements", w);
+    if (!aligned(a.workspace, 16)) return fail(XL_E_ALIGN, "%s: the workspace is not aligned to 16 bytes", w);
     if (a.length == 0 && !a.new_state) return XL_OK;
     if ((st = check_device()) != XL_OK) return st;
     return launched(xls::launch_selective_scan(a, static_cast<hipStream_t>(stream)));
+}
+
+long long xl_selective_scan_workspace(const xl_scan_args *args)
+{
+    if (!args || !is_size(args->batch) || !is_size(args->length) || !is_size(args->channels) || args->states < 1 || args->states > XL_MAX_STATES ||
+        !product_fits(args->batch, args->channels, 1, 1 << 30))
+        return 0;
+    return xls::scan_workspace(*args);
 }
 
 xl_status xl_quantize_blocks(const xl_quantize_args *args, void *stream)

@@ -1,6 +1,7 @@
 // Selective state-space scan.
 //
 //   h[n] <- exp(d A[n]) h[n] + d u B[n],   y = sum_n C[n] h[n] + D u,   y *= z sigmoid(z)
+#include <algorithm>
 #include <climits>
 #include <initializer_list>
 
@@ -110,13 +111,22 @@ template <int LP> __device__ __forceinline__ float sum_over_lanes(float *p, int 
     return (up1 ? p[1] : p[0]) + from_partner<0xb1>(up1 ? p[0] : p[1]);                                             // lane ^ 1
 }
 
+// Where there are not enough channels for the chip a sequence is worked on in `count` parts of `tokens` each.  For every part but the first there is what the one
+// before it makes of a state, E and then, behind all E, P, [batch][part][channel][state]; for the first the state that it begins with.
+struct Parts {
+    float *results;
+    int count, tokens;
+    __device__ __forceinline__ float *at(int b, int part, int c, int D, int N) const { return results + (((long long)b * count + part) * D + c) * N; }
+    __device__ __forceinline__ long long factors(long long batch, int D, int N) const { return batch * count * D * N; }
+};
+
 // Many tokens.  A workgroup owns CH = 64 / LP channels of a sequence and goes through it in tiles of W x TK tokens, TK of them a wave: the recurrence is linear, so a
 // wave runs its tokens from a state of zero (which gives E) and multiplies up their factors (P = exp(A sum d)); then the waves exchange (P, E), each
 // folds those of the waves before it into the state that it begins with, and runs its tokens again, the factors and inputs
 // still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
 // tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
 template <int DT, int LP, int NS, int W, int TK, Access ACCESS>
-__global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups)
+__global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups, const Parts parts)
 {
     typedef typename Elem<DT>::T T;
     constexpr int CH = 64 / LP, NP = LP * NS, TT = W * TK, PT = TK + 4;
@@ -132,15 +142,32 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     const int b = blockIdx.x / groups, c0 = (blockIdx.x % groups) * CH;
     const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
     const long long slot = slot_of(a.slots, a.nslots, b);
-    const int len = slot < 0 ? 0 : length_of(a.lengths, b, L);
+    const int whole = slot < 0 ? 0 : length_of(a.lengths, b, L);
     const bool in = c0 + c < D;
+    // this workgroup's tokens: from `first` to `len`, and up to `last` zeros
+    const int first = blockIdx.y * parts.tokens, last = min(L - first, parts.tokens) + first, len = min(whole, last);
 
     float A2[NS], h[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         const bool live = in && n0 + i < N;
         A2[i] = live ? a.A[(long long)(c0 + c) * N + n0 + i] * LOG2E : 0.f;
-        h[i] = live && a.state && slot >= 0 ? a.state[(slot * D + c0 + c) * N + n0 + i] : 0.f;
+        h[i] = live && a.state && slot >= 0 && parts.count == 1 ? a.state[(slot * D + c0 + c) * N + n0 + i] : 0.f;
+    }
+    if (parts.count > 1 && (first < len || first == 0)) {       // what part 0 begins with, or part 0's end and the parts behind it
+        const float *E = parts.at(b, first ? 1 : 0, c0 + c, D, N) + n0, *P = E + parts.factors(a.batch, D, N);
+        const long long step = (long long)D * N;
+        const int live = in ? N - n0 : 0;
+        Vec<float, NS> v = load_some<float, NS>(E, live);
+        for (int k = 2; k <= (int)blockIdx.y; ++k) {
+            E += step;
+            P += step;
+            const Vec<float, NS> p = load_some<float, NS>(P, live), e = load_some<float, NS>(E, live);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) v[i] = __builtin_fmaf(p[i], v[i], e[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) h[i] = v[i];
     }
     // this lane's numbers of its wave's tokens: VE channels of IT tokens
     const int ec = lane % (CH / VE) * VE, et = lane / (CH / VE), nc = min(D - c0 - ec, VE), tw = wave * TK;
@@ -201,8 +228,8 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
         }
     };
 
-    fetch(0);
-    for (int t0 = 0, set = 0; t0 < len; t0 += TT, set ^= 1) {
+    if (first < len) fetch(first);
+    for (int t0 = first, set = 0; t0 < len; t0 += TT, set ^= 1) {
         Vec<T, VE> uc[IT], zc[IT];
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
@@ -271,7 +298,6 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             if (w == wave) {
-                asm volatile("");       // a branch: every wave passes by W - 1 of these, and as selections they would cost it W * NS operations
 #pragma unroll
                 for (int i = 0; i < NS; ++i) g[i] = h[i];
             }
@@ -317,16 +343,136 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             else if (t0 + tw + t < len) store_some<T, VE>(yp + (t0 + tw + t) * a.y_token + ec, nc, v);
         }
     }
-    for (int t = len + wave * ET + et; t < L; t += W * ET) {
+    for (int t = max(len, first) + wave * ET + et; t < last; t += W * ET) {
 #pragma unroll
         for (int i = 0; i < VE; ++i)
             if (i < nc) yp[t * a.y_token + ec + i] = (T)0.f;
     }
-    if (wave == 0 && a.new_state && slot >= 0) {
+    if (wave == 0 && a.new_state && slot >= 0 && (first < len || first == 0) && len == whole) {     // the sequence ends here
 #pragma unroll
         for (int i = 0; i < NS; ++i)
             if (in && n0 + i < N) a.new_state[(slot * D + c0 + c) * N + n0 + i] = h[i];
     }
+}
+
+// The first of two kernels where a sequence is worked on in parts: what each part but the last makes of a state, h -> P h + E; part 0 of the state it begins with.
+// A wave goes through its share of the part by itself, as above but for the outputs; the waves' results are joined at the end.
+template <int DT, int LP, int NS, int W, int TK, Access ACCESS>
+__global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int groups, const Parts parts)
+{
+    typedef typename Elem<DT>::T T;
+    constexpr int CH = 64 / LP, NP = LP * NS, PT = TK + 4;
+    constexpr int PER = CH * TK / 64, VE = ACCESS != VECTORS ? 1 : PER < 4 ? PER : 4, IT = PER / VE;
+    constexpr int PERB = NP * TK / 64, VB = ACCESS != VECTORS ? 1 : PERB < 4 ? PERB : 4, IB = PERB / VB;
+    __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT], Bs_all[W][TK * NP];
+    __shared__ Vec<float, NS> Ps[W * 64], Es[W * 64];
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
+    float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave];
+    const int b = blockIdx.x / groups, c0 = (blockIdx.x % groups) * CH;
+    const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
+    const long long slot = slot_of(a.slots, a.nslots, b);
+    const int len = slot < 0 ? 0 : length_of(a.lengths, b, L), first = blockIdx.y * parts.tokens;
+    const bool in = c0 + c < D;
+    const int live = in ? N - n0 : 0;
+    float *out = parts.at(b, blockIdx.y, c0 + c, D, N) + n0;
+    const long long step = (long long)D * N;
+    Vec<float, NS> begin = {};
+    if (first == 0) {
+        if (a.state && slot >= 0) begin = load_some<float, NS>(a.state + (slot * D + c0 + c) * N + n0, live);
+        if (wave == 0 && live > 0) store_some<float, NS>(out, live, begin);
+    }
+    if (len <= first + parts.tokens) return;        // all of the workgroup: no part behind this one
+
+    float A2[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) A2[i] = i < live ? a.A[(long long)(c0 + c) * N + n0 + i] * LOG2E : 0.f;
+    const int ec = lane % (CH / VE) * VE, et = lane / (CH / VE), nc = min(D - c0 - ec, VE);
+    const int bn = lane % (NP / VB) * VB, bt = lane / (NP / VB), nb = min(N - bn, VB);
+    constexpr int ET = 64 * VE / CH, BT = 64 * VB / NP;
+    float bias[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) bias[i] = a.delta_bias && i < nc ? a.delta_bias[c0 + ec + i] : 0.f;
+    constexpr unsigned S = sizeof(T);
+    const unsigned u_row = (unsigned)a.u_token * S, d_row = (unsigned)a.delta_token * S, b_row = (unsigned)a.b_token * S;
+    const unsigned u_at = nc > 0 ? et * u_row + ec * S : NOWHERE, d_at = nc > 0 ? et * d_row + ec * S : NOWHERE, b_at = nb > 0 ? bt * b_row + bn * S : NOWHERE;
+    const int width = min(CH, D - c0);
+    const Rows urows(static_cast<const T *>(a.u) + b * a.u_batch + c0, a.u_token, len, width, S), drows(static_cast<const T *>(a.delta) + b * a.delta_batch + c0, a.delta_token, len, width, S);
+    const Rows Brows(static_cast<const T *>(a.B) + b * a.b_batch, a.b_token, len, N, S);
+    Vec<T, VE> ur[IT], dr[IT];
+    Vec<T, VB> Br[IB];
+    auto fetch = [&](int t0) {
+#pragma unroll
+        for (int k = 0; k < IT; ++k) {
+            ur[k] = urows.template load<Vec<T, VE>>(u_at + k * ET * u_row, t0 * u_row);
+            dr[k] = drows.template load<Vec<T, VE>>(d_at + k * ET * d_row, t0 * d_row);
+        }
+#pragma unroll
+        for (int k = 0; k < IB; ++k) Br[k] = Brows.template load<Vec<T, VB>>(b_at + k * BT * b_row, t0 * b_row);
+    };
+    const int share = parts.tokens / W, t1 = first + wave * share, end = t1 + share;
+    Vec<float, NS> e = {}, p;
+    float total = 0.f;
+    fetch(t1);
+    for (int t0 = t1; t0 < end; t0 += TK) {
+#pragma unroll
+        for (int k = 0; k < IT; ++k) {
+            float d[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) d[i] = (float)dr[k][i] + bias[i];
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) d[i] = softplus(d[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                dl[(ec + i) * PT + et + k * ET] = d[i];
+                sx[(ec + i) * PT + et + k * ET] = d[i] * (float)ur[k][i];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < IB; ++k) {
+            Vec<float, VB> v;
+#pragma unroll
+            for (int i = 0; i < VB; ++i) v[i] = (float)Br[k][i];
+            *reinterpret_cast<Vec<float, VB> *>(&Bs[(bt + k * BT) * NP + bn]) = v;
+        }
+        if (t0 + TK < end) fetch(t0 + TK);
+        wave_sync();
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < TK; k += 4) {
+            const f32x4 d = *reinterpret_cast<const f32x4 *>(&dl[c * PT + k]), s = *reinterpret_cast<const f32x4 *>(&sx[c * PT + k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Vec<float, NS> B = *reinterpret_cast<const Vec<float, NS> *>(&Bs[(k + j) * NP + n0]);
+                sum += d[j];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) e[i] = __builtin_fmaf(exp2_fast(d[j] * A2[i]), e[i], s[j] * B[i]);
+            }
+        }
+        total += sum;
+        wave_sync();
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) p[i] = exp2_fast(total * A2[i]);
+    Ps[threadIdx.x] = p;
+    Es[threadIdx.x] = e;
+    __syncthreads();
+    if (wave != 0 || live <= 0) return;
+    e = begin;
+    p = Vec<float, NS>{} + 1.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const Vec<float, NS> pw = Ps[w * 64 + lane], ew = Es[w * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            e[i] = __builtin_fmaf(pw[i], e[i], ew[i]);
+            p[i] *= pw[i];
+        }
+    }
+    store_some<float, NS>(out + step, live, e);
+    store_some<float, NS>(out + step + parts.factors(a.batch, D, N), live, p);
 }
 
 template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, hipStream_t s)
@@ -336,12 +482,11 @@ template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, h
     return hipGetLastError();
 }
 
-template <int DT, int LP, int NS, int W, int TK> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s)
+template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s, Parts parts = {nullptr, 1, INT_MAX})
 {
     typedef typename Elem<DT>::T T;
     constexpr int CH = 64 / LP, PER = CH * TK / 64, VE = PER < 4 ? PER : 4, PERB = LP * NS * TK / 64, VB = PERB < 4 ? PERB : 4;
     const int groups = (int)((a.channels + CH - 1) / CH);
-    const dim3 grid((unsigned)(groups * a.batch));
     const unsigned long long at = (unsigned long long)a.u | (unsigned long long)a.delta | (unsigned long long)a.z | (unsigned long long)a.y;
     const unsigned long long steps = a.u_batch | a.u_token | a.delta_batch | a.delta_token | a.z_batch | a.z_token | a.y_batch | a.y_token;
     const unsigned long long at_bc = (unsigned long long)a.B | (unsigned long long)a.C, steps_bc = a.b_batch | a.b_token | a.c_batch | a.c_token;
@@ -354,9 +499,21 @@ template <int DT, int LP, int NS, int W, int TK> static hipError_t launch_tile(c
     };
     const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
     // 2 x 12321 x 2048 with 16 states in bf16: 283 us as vectors, 322 one by one, 561 scattered (these with four waves in every case)
-    if (!buffers) tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<grid, 64 * 4, 0, s>>>(a, groups);
-    else if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups);
-    else tile_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups);
+    const unsigned wide = (unsigned)(groups * a.batch);
+    if (!buffers) {
+        tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
+        return hipGetLastError();
+    }
+    if constexpr (SPLIT) {
+        const dim3 grid(wide, (unsigned)parts.count - 1);
+        if (vectors) part_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups, parts);
+        else part_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups, parts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const dim3 grid(wide, (unsigned)parts.count);
+    if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups, parts);
+    else tile_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups, parts);
     return hipGetLastError();
 }
 
@@ -364,6 +521,27 @@ static constexpr long long CUS = 256;
 
 // Workgroups of 64 / LP channels each.
 static long long groups_of(const xl_scan_args &a, int lp) { return a.batch * ((a.channels * lp + 63) / 64); }
+
+// Lanes of a channel that leave each four states (fewer where there are no more).
+static int lanes_of(const xl_scan_args &a) { return a.states <= 16 ? 4 : a.states <= 32 ? 8 : 16; }
+
+// Parts of a sequence: as many as it takes to give every compute unit a workgroup of eight waves, of at least 256 tokens, and whole tiles.  The second kernel
+// costs 8 us and the tokens' first run twice, so it takes four parts and some length (1 sequence, 16 states, us whole and in parts: 2048 tokens x 256 channels
+// 22, 17; 12321 x 256 114, 42; 4096 x 1024 50, 44; 2048 x 1024 28, 27; 12321 x 2048, two parts, 239, 221), less of it with up to eight states, which whole
+// sequences do not spread over more workgroups (3025 x 1001, 7 states 62, 31; 16 states 35, 39).
+static constexpr long long TILE = 128, MIN_PART = 256, MAX_PARTS = 32;
+static Parts parts_of(const xl_scan_args &a)
+{
+    const long long groups = groups_of(a, lanes_of(a)), most = groups > 0 ? std::min({CUS / groups, a.length / MIN_PART, MAX_PARTS}) : 0;
+    if (most < 4 || a.states > 64 || a.length < (a.states <= 8 ? 2048 : std::max(2048ll, 16384 / most))) return {nullptr, 1, INT_MAX};
+    const long long tokens = (a.length + most * TILE - 1) / (most * TILE) * TILE;
+    return {static_cast<float *>(a.workspace), (int)((a.length + tokens - 1) / tokens), (int)tokens};
+}
+long long scan_workspace(const xl_scan_args &a)
+{
+    const Parts p = parts_of(a);
+    return p.count > 1 ? (2ll * p.count * a.batch * a.channels * a.states * 4 + 15) / 16 * 16 : 0;
+}
 
 // Waves of a workgroup.  One that has a compute unit to itself (its registers leave room for two waves a SIMD) takes eight, four where two fit and two where there are
 // four and more to overlap.  16 states, 3025 tokens, us with 2, 4, 8 waves: 256 workgroups 199, 107, 80; 1024 workgroups 289, 293, 320.
@@ -385,6 +563,15 @@ template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream
         if (a.states <= 32) return launch_step<DT, 8>(a, s);
         if (a.states <= 64) return launch_step<DT, 16>(a, s);
         return launch_step<DT, 32>(a, s);
+    }
+    const long long bytes = scan_workspace(a);
+    if (bytes > 0 && a.workspace && a.workspace_bytes >= bytes) {
+        const Parts parts = parts_of(a);
+        if (a.states <= 4) return launch_tile<DT, 4, 1, 8, 16, true>(a, s, parts);
+        if (a.states <= 8) return launch_tile<DT, 4, 2, 8, 16, true>(a, s, parts);
+        if (a.states <= 16) return launch_tile<DT, 4, 4, 8, 16, true>(a, s, parts);
+        if (a.states <= 32) return launch_tile<DT, 8, 4, 8, 16, true>(a, s, parts);
+        return launch_tile<DT, 16, 4, 8, 16, true>(a, s, parts);
     }
     // Four states a lane cost the fewest operations.  With fewer the channels spread over more workgroups, which pays while each still has a compute unit to itself
     // (16 states, 3025 tokens, us with 4, 2, 1 states a lane: 1024 channels 77, 54, 45; 2048 channels 77, 61, 82; 4096 channels 80, 118, 170).

@@ -23,6 +23,7 @@ namespace {
 // Addresses of the library's functions and the exception that a refusal raises: set once by bind().
 decltype(&xl_causal_conv) g_conv;
 decltype(&xl_selective_scan) g_scan;
+decltype(&xl_selective_scan_workspace) g_scan_workspace;
 decltype(&xl_quantize_blocks) g_quantize;
 decltype(&xl_block_matmul) g_matmul;
 decltype(&xl_seq_last_error) g_last_error;
@@ -234,6 +235,9 @@ PyObject *selective_scan(const Args &in)    // u, delta, A, B, C, D, z, delta_bi
     a.lengths = op.dense_as<int>("lengths", lengths, at::kInt, {a.batch});
     a.slots = op.dense_as<int>("slots", slots, at::kInt, {a.batch});
     a.y = given->data_ptr();
+    at::Tensor workspace;
+    a.workspace_bytes = g_scan_workspace(&a);
+    if (a.workspace_bytes > 0) a.workspace = (workspace = at::empty({a.workspace_bytes}, u.options().dtype(at::kByte))).data_ptr();
     op.run(g_scan, a);
     return pair(in.args[13], *given, in.args[10] == Py_None && slots ? in.args[9] : in.args[10], *kept);
 }
@@ -351,17 +355,18 @@ template <PyObject *(*F)(const Args &), int N> PyObject *entry(PyObject *, PyObj
     END_HANDLE_TH_ERRORS
 }
 
-// bind(conv, scan, quantize, matmul, last_error, exception): the addresses of the library's functions
+// bind(conv, scan, scan_workspace, quantize, matmul, last_error, exception): the addresses of the library's functions
 PyObject *bind(PyObject *, PyObject *args)
 {
-    unsigned long long f[5];
+    unsigned long long f[6];
     PyObject *error;
-    if (!PyArg_ParseTuple(args, "KKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &error)) return nullptr;
     g_conv = reinterpret_cast<decltype(g_conv)>(f[0]);
     g_scan = reinterpret_cast<decltype(g_scan)>(f[1]);
-    g_quantize = reinterpret_cast<decltype(g_quantize)>(f[2]);
-    g_matmul = reinterpret_cast<decltype(g_matmul)>(f[3]);
-    g_last_error = reinterpret_cast<decltype(g_last_error)>(f[4]);
+    g_scan_workspace = reinterpret_cast<decltype(g_scan_workspace)>(f[2]);
+    g_quantize = reinterpret_cast<decltype(g_quantize)>(f[3]);
+    g_matmul = reinterpret_cast<decltype(g_matmul)>(f[4]);
+    g_last_error = reinterpret_cast<decltype(g_last_error)>(f[5]);
     Py_INCREF(error);
     Py_XSETREF(g_error, error);
     Py_RETURN_NONE;

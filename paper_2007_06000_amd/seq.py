@@ -1,7 +1,7 @@
 """Sequence operators on torch tensors: causal convolution, selective scan, block quantisation, block-scaled product.
 
 The names and the meaning of every argument mirror include/xl_seq.h; the arithmetic runs in the HIP kernels of libxl_seq.so, and there is no
-CPU fallback.  Each call enqueues one kernel (a large product two) on the current stream of its tensors' device and returns without waiting;
+CPU fallback.  Each call enqueues one kernel (a large product and a long scan of few channels two) on the current stream of its tensors' device and returns without waiting;
 what does not fit raises `XlError` before anything is launched.  Inference only: tensors that ask for gradients are refused.
 """
 from __future__ import annotations
@@ -22,7 +22,7 @@ XL_F32, XL_F16, XL_BF16 = 0, 1, 2
 SCALE_BLOCK = 128
 
 # every symbol include/xl_seq.h declares
-EXPORTS = ["xl_causal_conv", "xl_selective_scan", "xl_quantize_blocks", "xl_block_matmul", "xl_seq_last_error"]
+EXPORTS = ["xl_causal_conv", "xl_selective_scan", "xl_selective_scan_workspace", "xl_quantize_blocks", "xl_block_matmul", "xl_seq_last_error"]
 
 _lib = None
 _module = None
@@ -39,6 +39,8 @@ def lib() -> ctypes.CDLL:
             f = getattr(L, name)
             f.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
             f.restype = ctypes.c_int
+        L.xl_selective_scan_workspace.argtypes = [ctypes.c_char_p]
+        L.xl_selective_scan_workspace.restype = ctypes.c_longlong
         L.xl_seq_last_error.argtypes = []
         L.xl_seq_last_error.restype = ctypes.c_char_p
         _lib = L

@@ -38,6 +38,11 @@ hipError_t launch_selective_scan(const xl_scan_args &a, hipStream_t)
     CHECK((!a.state && !a.new_state) || a.slots || a.nslots >= a.batch);
     return hipSuccess;
 }
+long long scan_workspace(const xl_scan_args &a)
+{
+    CHECK(size(a.batch) && size(a.length) && size(a.channels) && a.states >= 1 && a.states <= XL_MAX_STATES && (__int128)a.batch * a.channels <= 1 << 30);
+    return 0;
+}
 hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t)
 {
     ++launched;
@@ -64,6 +69,8 @@ const char *hipGetErrorString(hipError_t) { return "an error"; }
 static std::mt19937_64 rng(1);
 
 /* Numbers, then pointers; most of them ordinary, so that a call gets past its first checks. */
+static void ask(const xl_scan_args *a) { CHECK(xl_selective_scan_workspace(a) == 0); }
+static void ask(const void *) {}
 template <typename A> static void run(xl_status (*f)(const A *, void *), int numbers)
 {
     static const long long ends[] = {-1, LLONG_MIN, LLONG_MAX, INT_MAX, INT_MAX - 4096ll, 1ll << 32, 1ll << 38, 1ll << 62, 0, 128};
@@ -80,6 +87,7 @@ template <typename A> static void run(xl_status (*f)(const A *, void *), int num
         }
         memcpy(a, v, sizeof(A));
         const xl_status st = f(a, nullptr);
+        ask(a);
         CHECK(st == XL_OK || strlen(xl_seq_last_error()) > 10);
     }
     free(a);
@@ -88,7 +96,7 @@ template <typename A> static void run(xl_status (*f)(const A *, void *), int num
 int main()
 {
     run(xl_causal_conv, 11);
-    run(xl_selective_scan, 19);
+    run(xl_selective_scan, 20);
     run(xl_quantize_blocks, 8);
     run(xl_block_matmul, 11);
     printf("%lld launches, %lld failures\n", launched, failures);

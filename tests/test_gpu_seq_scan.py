@@ -1,4 +1,6 @@
 """The selective scan against its definition in 64 bits."""
+import struct
+
 import numpy as np
 import pytest
 import torch
@@ -73,6 +75,54 @@ def test_sequences_of_their_own_lengths(lengths, states):
         assert not y[b, max(n, 0):].any()
         if n <= 0:
             assert torch.equal(new[b], p["state"][b])
+
+
+def asks_for_a_workspace(p):
+    batch, length, channels = p["u"].shape
+    sizes = struct.pack("=20q14Q", batch, length, channels, p["A"].shape[1], *[0] * 30)
+    return seq.lib().xl_selective_scan_workspace(sizes) > 0
+
+
+@pytest.mark.parametrize("dtype,batch,length,channels,states", [
+    (torch.bfloat16, 1, 2304, 64, 16), (torch.float32, 2, 2100, 33, 13), (torch.float16, 3, 2049, 20, 3), (torch.bfloat16, 1, 2500, 28, 8),
+    (torch.float32, 1, 2050, 12, 30), (torch.float16, 1, 2090, 11, 64)])
+def test_long_sequences_of_few_channels_are_worked_on_in_parts(dtype, batch, length, channels, states):
+    p = inputs(batch, length, channels, states, dtype, step=(-5.0, 1.0))
+    assert asks_for_a_workspace(p)
+    check(p, *run(p), "all")
+    bare = {k: p[k] for k in ("u", "delta", "A", "B", "C")}
+    check(bare, *run(bare), "bare")
+
+
+# 2100 tokens of six sequences of 33 channels: parts of 384
+@pytest.mark.parametrize("lengths", [[0, 1, 383, 384, 385, 2100], [768, 2099, 1537, 1536, -1, 5000]])
+def test_parts_of_sequences_of_their_own_lengths(lengths):
+    p = inputs(6, 2100, 33, 16, torch.bfloat16, step=(-5.0, 1.0))
+    assert asks_for_a_workspace(p)
+    clean = {k: v.clone() for k, v in p.items()}
+    for b, n in enumerate(lengths):
+        for k in ("u", "delta", "B", "C", "z"):
+            p[k][b, max(n, 0):] = float("nan")          # never used
+    state = p["state"]
+    y, new = run(p, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"), new_state=state, out=p["u"])      # everything in place
+    assert new is state and y is p["u"]
+    check(clean, y, new, "lengths", lengths)
+    for b, n in enumerate(lengths):
+        assert not y[b, max(n, 0):].any()
+        if n <= 0:
+            assert torch.equal(new[b], clean["state"][b])
+
+
+def test_parts_of_sequences_in_a_cache():
+    p = inputs(3, 2200, 40, 16, torch.float32, step=(-5.0, 1.0))
+    assert asks_for_a_workspace(p)
+    cache = torch.full((5, 40, 16), 7.0, device="cuda")
+    slots = [4, -1, 0]
+    cache[[4, 0]] = p["state"][[0, 2]]
+    y, new = seq.selective_scan(**{**p, "state": cache}, slots=torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    assert new is cache and not y[1].any() and (cache[1:4] == 7).all()
+    part = {k: v if k in ("A", "D", "delta_bias") else v[[0, 2]] for k, v in p.items()}
+    check(part, y[[0, 2]], cache[[4, 0]], "cache")
 
 
 def test_pieces_and_single_tokens_continue_a_sequence():

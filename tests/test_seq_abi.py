@@ -28,7 +28,7 @@ def fields(name):
 
 
 # the argument structs: 64-bit numbers, then pointers
-STRUCTS = {"xl_causal_conv": ("xl_causal_conv_args", struct.Struct("=11q8Q")), "xl_selective_scan": ("xl_scan_args", struct.Struct("=19q13Q")),
+STRUCTS = {"xl_causal_conv": ("xl_causal_conv_args", struct.Struct("=11q8Q")), "xl_selective_scan": ("xl_scan_args", struct.Struct("=20q14Q")),
            "xl_quantize_blocks": ("xl_quantize_args", struct.Struct("=8q3Q")), "xl_block_matmul": ("xl_block_matmul_args", struct.Struct("=11q6Q"))}
 
 
@@ -76,7 +76,7 @@ REFUSED = [
     ("xl_selective_scan", B.XL_E_UNSUPPORTED, dict(states=0)), ("xl_selective_scan", B.XL_E_UNSUPPORTED, dict(states=129)), ("xl_selective_scan", B.XL_E_UNSUPPORTED, dict(dtype=-1)),
     ("xl_selective_scan", B.XL_E_SHAPE, dict(delta_token=-1)), ("xl_selective_scan", B.XL_E_SHAPE, dict(y_token=4)), ("xl_selective_scan", B.XL_E_SHAPE, dict(z=P, z_batch=-1)),
     ("xl_selective_scan", B.XL_E_SHAPE, dict(nslots=1, new_state=P)), ("xl_selective_scan", B.XL_E_ALIGN, dict(state=P + 2)), ("xl_selective_scan", B.XL_E_ALIGN, dict(C=P + 1)),
-    ("xl_selective_scan", B.XL_E_ALIGN, dict(z=P + 1)), ("xl_selective_scan", B.XL_E_ALIGN, dict(D=P + 2)),
+    ("xl_selective_scan", B.XL_E_ALIGN, dict(z=P + 1)), ("xl_selective_scan", B.XL_E_ALIGN, dict(workspace=P + 8)), ("xl_selective_scan", B.XL_E_ALIGN, dict(D=P + 2)),
     ("xl_quantize_blocks", B.XL_E_NULL, dict(x=0)), ("xl_quantize_blocks", B.XL_E_NULL, dict(q=0)), ("xl_quantize_blocks", B.XL_E_NULL, dict(scales=0)),
     ("xl_quantize_blocks", B.XL_E_UNSUPPORTED, dict(block_rows=2)), ("xl_quantize_blocks", B.XL_E_UNSUPPORTED, dict(dtype=7)), ("xl_quantize_blocks", B.XL_E_SHAPE, dict(rows=-1)),
     ("xl_quantize_blocks", B.XL_E_SHAPE, dict(q_row=32)), ("xl_quantize_blocks", B.XL_E_SHAPE, dict(scale_block=-1)), ("xl_quantize_blocks", B.XL_E_SHAPE, dict(x_row=-40)),
@@ -101,6 +101,21 @@ def test_what_does_not_fit_is_refused(name, status, change):
                                         ("xl_quantize_blocks", dict(k=0)), ("xl_block_matmul", dict(m=0, a=0)), ("xl_block_matmul", dict(n=0))], ids=str)
 def test_nothing_to_do_is_no_error(name, empty):
     assert call(name, **{**BASE[name], **empty})[0] == B.XL_OK
+
+
+def test_a_scan_asks_for_a_workspace_where_it_can_use_one():
+    names = [f for f, _ in fields("xl_scan_args")]
+
+    def ask(**sizes):
+        return seq.lib().xl_selective_scan_workspace(STRUCTS["xl_selective_scan"][1].pack(*[{**SCAN, **sizes}.get(f, 0) for f in names]))
+
+    few = ask(batch=1, length=12321, channels=256, states=16)
+    assert few > 0 and few % 16 == 0 and few % (2 * 4 * 256 * 16) == 0
+    assert ask(batch=1, length=12321, channels=250, states=13) > 0
+    assert not ask(batch=1, length=1, channels=256, states=16) and not ask(batch=64, length=12321, channels=4096, states=16)
+    for bad in (dict(batch=-1), dict(length=1 << 40), dict(channels=1 << 62), dict(states=0), dict(states=129), dict(batch=0), dict(batch=1 << 30, channels=1 << 30)):
+        assert ask(**{**dict(batch=1, length=12321, channels=256, states=16), **bad}) == 0
+    assert seq.lib().xl_selective_scan_workspace(None) == 0
 
 
 @pytest.mark.parametrize("name", STRUCTS)
