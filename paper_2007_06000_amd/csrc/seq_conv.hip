@@ -14,7 +14,7 @@ __global__ __launch_bounds__(256) void conv_kernel(const xl_causal_conv_args a, 
 {
     typedef typename Elem<DT>::T T;
     const int C = (int)a.channels, L = (int)a.length, vecs = C / V;
-    const long long item = (long long)blockIdx.x * 256 + threadIdx.x, rest = item / vecs;
+    const long long item = (long long)neighbours_together(blockIdx.x, gridDim.x) * 256 + threadIdx.x, rest = item / vecs;
     const int c = (int)(item % vecs) * V, b = (int)(rest / runs), t0 = (int)(rest % runs) * run;
     if (b >= a.batch) return;
     const T *x = static_cast<const T *>(a.x) + b * a.x_batch + c;

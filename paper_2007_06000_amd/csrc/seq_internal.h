@@ -102,4 +102,11 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Workgroups go round the eight XCDs, each with a cache of its own; this numbers them so that neighbours are on the same one.
+__device__ __forceinline__ int neighbours_together(int block, int blocks)
+{
+    const int xcd = block % 8, per = blocks / 8, more = blocks % 8;
+    return xcd * per + min(xcd, more) + block / 8;
+}
+
 }  // namespace xls

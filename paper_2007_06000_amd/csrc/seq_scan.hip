@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
     float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave], *Cs = Cs_all[wave];
-    const int b = blockIdx.x / groups, c0 = (blockIdx.x % groups) * CH;
+    const int block = neighbours_together(blockIdx.x, gridDim.x), b = block / groups, c0 = (block % groups) * CH;
     const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
     const long long slot = slot_of(a.slots, a.nslots, b);
     const int whole = slot < 0 ? 0 : length_of(a.lengths, b, L);
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
     float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave];
-    const int b = blockIdx.x / groups, c0 = (blockIdx.x % groups) * CH;
+    const int block = neighbours_together(blockIdx.x, gridDim.x), b = block / groups, c0 = (block % groups) * CH;
     const int D = (int)a.channels, N = (int)a.states, L = (int)a.length;
     const long long slot = slot_of(a.slots, a.nslots, b);
     const int len = slot < 0 ? 0 : length_of(a.lengths, b, L), first = blockIdx.y * parts.tokens;
@@ -498,7 +498,7 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipE
         return true;
     };
     const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
-    // 2 x 12321 x 2048 with 16 states in bf16: 283 us as vectors, 322 one by one, 561 scattered (these with four waves in every case)
+    // 2 x 12321 x 2048 with 16 states in bf16: 276 us as vectors, 315 one by one, 560 scattered (these with four waves in every case)
     const unsigned wide = (unsigned)(groups * a.batch);
     if (!buffers) {
         tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
@@ -525,15 +525,15 @@ static long long groups_of(const xl_scan_args &a, int lp) { return a.batch * ((a
 // Lanes of a channel that leave each four states (fewer where there are no more).
 static int lanes_of(const xl_scan_args &a) { return a.states <= 16 ? 4 : a.states <= 32 ? 8 : 16; }
 
-// Parts of a sequence: as many as it takes to give every compute unit a workgroup of eight waves, of at least 256 tokens, and whole tiles.  The second kernel
-// costs 8 us and the tokens' first run twice, so it takes four parts and some length (1 sequence, 16 states, us whole and in parts: 2048 tokens x 256 channels
-// 22, 17; 12321 x 256 114, 42; 4096 x 1024 50, 44; 2048 x 1024 28, 27; 12321 x 2048, two parts, 239, 221), less of it with up to eight states, which whole
-// sequences do not spread over more workgroups (3025 x 1001, 7 states 62, 31; 16 states 35, 39).
+// Parts of a sequence: as many as it takes to give every compute unit a workgroup of eight waves, of at least 256 tokens, and whole tiles.  A second kernel and
+// the tokens' first run twice cost what eight parts bring (1 sequence, 16 states, us whole and in parts: 2048 tokens x 256 channels 20, 16; 12321 x 256 107,
+// 41; 12321 x 512 108, 64; 4096 x 1024, four parts, 39, 42), or four with up to eight states, which spread over fewer workgroups when whole
+// (3025 x 1001, 3 states 50, 23; 7 states 38, 29).
 static constexpr long long TILE = 128, MIN_PART = 256, MAX_PARTS = 32;
 static Parts parts_of(const xl_scan_args &a)
 {
     const long long groups = groups_of(a, lanes_of(a)), most = groups > 0 ? std::min({CUS / groups, a.length / MIN_PART, MAX_PARTS}) : 0;
-    if (most < 4 || a.states > 64 || a.length < (a.states <= 8 ? 2048 : std::max(2048ll, 16384 / most))) return {nullptr, 1, INT_MAX};
+    if (most < (a.states <= 8 ? 4 : 8) || a.states > 64 || a.length < 1536) return {nullptr, 1, INT_MAX};
     const long long tokens = (a.length + most * TILE - 1) / (most * TILE) * TILE;
     return {static_cast<float *>(a.workspace), (int)((a.length + tokens - 1) / tokens), (int)tokens};
 }
@@ -544,7 +544,8 @@ long long scan_workspace(const xl_scan_args &a)
 }
 
 // Waves of a workgroup.  One that has a compute unit to itself (its registers leave room for two waves a SIMD) takes eight, four where two fit and two where there are
-// four and more to overlap.  16 states, 3025 tokens, us with 2, 4, 8 waves: 256 workgroups 199, 107, 80; 1024 workgroups 289, 293, 320.
+// four and more to overlap.  16 states, 3025 tokens, us with 2, 4, 8 waves: 256 workgroups 183, 96, 70;
+// 512 workgroups 243, 134, 140; 1024 workgroups 258, 260, 276.
 template <int DT, int LP, int NS> static hipError_t launch_waves(const xl_scan_args &a, hipStream_t s)
 {
     const long long groups = groups_of(a, LP);
@@ -574,9 +575,13 @@ template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream
         return launch_tile<DT, 16, 4, 8, 16, true>(a, s, parts);
     }
     // Four states a lane cost the fewest operations.  With fewer the channels spread over more workgroups, which pays while each still has a compute unit to itself
-    // (16 states, 3025 tokens, us with 4, 2, 1 states a lane: 1024 channels 77, 54, 45; 2048 channels 77, 61, 82; 4096 channels 80, 118, 170).
+    // (16 states, 3025 tokens, us with 4, 2, 1 states a lane: 1024 channels 69, 45, 30; 2048 channels 69, 46, 57; 4096 channels 69, 73, 112; 7 states, 1900 tokens,
+    // with 2, 1: 1024 channels 38, 25; 4096 channels 39, 36).
     if (a.states <= 4) return launch_waves<DT, 4, 1>(a, s);
-    if (a.states <= 8) return launch_waves<DT, 4, 2>(a, s);
+    if (a.states <= 8) {
+        if (groups_of(a, 8) <= 2 * CUS) return launch_tile<DT, 8, 1, 8, 16>(a, s);
+        return launch_waves<DT, 4, 2>(a, s);
+    }
     if (a.states <= 16) {
         if (groups_of(a, 16) <= CUS) return launch_tile<DT, 16, 1, 16, 16>(a, s);
         if (groups_of(a, 8) <= CUS) return launch_tile<DT, 8, 2, 8, 16>(a, s);
