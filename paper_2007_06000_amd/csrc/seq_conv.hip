@@ -4,7 +4,7 @@
 //
 // Bound by memory: 2 K + 4 operations for a number read and one written.  A thread owns V channels and `run` tokens in a row, with the last K - 1 inputs and the
 // filter in registers, so a number is read once, but for the K - 1 tokens before each run (a cache hit: the run before them is a neighbour's).
-// 8 x 3025 x 2048 in bf16 (half of a wider tensor): 44.5 us, 4.5 TB/s; in fp32 79 us, 5.0 TB/s.
+// 8 x 3025 x 2048 in bf16 (half of a wider tensor): 38.7 us, 5.1 TB/s; in fp32 76 us, 5.2 TB/s.
 #include "seq_internal.h"
 
 namespace xls {
@@ -85,8 +85,8 @@ __global__ __launch_bounds__(256) void conv_kernel(const xl_causal_conv_args a, 
 template <int DT, int K, int V> static hipError_t launch(const xl_causal_conv_args &a, hipStream_t s)
 {
     const long long vecs = a.channels / V;
-    // Runs of 16 tokens read an input 1.2 times; shorter ones where there would be fewer than 2048 threads a compute unit.
-    long long run = 16;
+    // Runs of 32 tokens read an input 1.1 times (of 8, 16, 32 tokens: 42.7, 39.1, 38.7 us; 2047 channels 70, 56, 51); shorter ones where there would be fewer than 2048 threads a compute unit.
+    long long run = 32;
     while (run > 4 && a.batch * vecs * ((a.length + run - 1) / run) < 256ll * 2048) run /= 2;
     const long long runs = a.length > 0 ? (a.length + run - 1) / run : 1, blocks = (a.batch * vecs * runs + 255) / 256;
     conv_kernel<DT, K, V><<<dim3((unsigned)blocks), 256, 0, s>>>(a, (int)run, (int)runs);
@@ -95,11 +95,9 @@ template <int DT, int K, int V> static hipError_t launch(const xl_causal_conv_ar
 
 template <int DT, int K> static hipError_t launch_taps(const xl_causal_conv_args &a, hipStream_t s)
 {
-    // 4 bytes of a row a thread, 8 where there is plenty of work (us, bf16, with 4, 8, 16 bytes: 16 x 1 x 1024 2.9, 3.4, 4.8; 3025 x 1024 5.6, 6.5,
-    // 9.2; 8 x 3025 x 2048 47.7, 44.5, 71: with 16 a thread's registers leave three waves a SIMD), one number where those do not divide a row
-    // (8 x 3025 x 2047: 54)
+    // 4 bytes of a row a thread (8 x 3025 x 2048 in bf16, us with 4, 8: 38.6, 42; 3025 x 1024 5.6, 6.5 and with 16 9.2), one number where those do not divide
+    // a row (8 x 3025 x 2047: 51)
     constexpr int V = 4 / sizeof(typename Elem<DT>::T);
-    if (a.batch * a.length * a.channels >= 1 << 24 && a.channels % (2 * V) == 0) return launch<DT, K, 2 * V>(a, s);
     if (V == 1 || a.channels % V) return launch<DT, K, 1>(a, s);
     return launch<DT, K, V>(a, s);
 }
