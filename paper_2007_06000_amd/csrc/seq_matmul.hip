@@ -399,7 +399,9 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
     const long long limit = 1ll << 22;
     const bool near = a.a_row < limit && a.b_row < limit && a.a_scale_row < limit / 16 && a.a_scale_block < (1ll << 28) / (blocks + 1);
     if (a.m <= 16) return launch_thin<DT, 1>(a, s);
-    if (a.m <= 32 || !near) return launch_thin<DT, 2>(a, s);
+    // Thin tiles where each has a compute unit, and K is spread over its waves (us, bf16, thin and tiles of 64: 64 x 2048 x 1024 3.6, 4.4; 128 x 1024 x 4096 7.8, 9.5;
+    // 192 x 96 x 1024 3.5, 4.4; with more tiles 66 x 2048 x 1024 4.3, 4.4; 192 x 1024 x 4096 13.1, 9.8)
+    if (a.m <= 32 || !near || (a.m + 31) / 32 * ((a.n + 15) / 16) <= CUS) return launch_thin<DT, 2>(a, s);
     // The smallest tiles that still have a compute unit each, or share one by twos, then larger ones (us, bf16, k 2048, tiles of 64 alone / by twos, 128 alone / by twos, 256: 1024 x 1024 7.2, 8.5,
     // 11.9, 13.9, 25; 1024 x 2048 12.9, 10.5, 12.2, 14.2, 26; 1024 x 4096 24, 18.5, 13.0, 15.1, 26; 2048 x 4096 46, 34, 24, 21, 28; 4096 x 4096 90, 66, 46, 41, 33).
     auto tiles = [](long long m, long long n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
