@@ -5,6 +5,9 @@
 // A block's sum is one matrix operation 16 x 16 x 128 (or four of 16 x 16 x 32, below); it starts at zero, and its result is scaled into the fp32 sums by one
 // multiply-add for each of a lane's four.  The rows of b are the operation's rows and those of a its columns: a lane's four results are then neighbours in a row of
 // y, and share one scale of a (the lane's column) and one of b (its 16 rows lie in one block of 128).
+//
+// Large products are bound by the matrix operations, the four multiply-adds behind each (16.8 ns for both, 15.9 without) and the loads' issue: 24642 x 4096 x 4096 in
+// bf16 takes 366 us, 2.26 PFLOP/s; the operations and multiply-adds alone would take 207.
 #include <type_traits>
 
 #include "seq_internal.h"
@@ -399,9 +402,10 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
     const long long limit = 1ll << 22;
     const bool near = a.a_row < limit && a.b_row < limit && a.a_scale_row < limit / 16 && a.a_scale_block < (1ll << 28) / (blocks + 1);
     if (a.m <= 16) return launch_thin<DT, 1>(a, s);
-    // Thin tiles where each has a compute unit, and K is spread over its waves (us, bf16, thin and tiles of 64: 64 x 2048 x 1024 3.6, 4.4; 128 x 1024 x 4096 7.8, 9.5;
-    // 192 x 96 x 1024 3.5, 4.4; with more tiles 66 x 2048 x 1024 4.3, 4.4; 192 x 1024 x 4096 13.1, 9.8)
-    if (a.m <= 32 || !near || (a.m + 31) / 32 * ((a.n + 15) / 16) <= CUS) return launch_thin<DT, 2>(a, s);
+    // Thin tiles where each has a compute unit (in fp32, with four times the matrix operations, half of one), and K is spread over its waves (us, bf16, thin and tiles of 64: 64 x 2048 x 1024 3.6, 4.4; 128 x 1024 x 4096 7.8, 9.5;
+    // 192 x 96 x 1024 3.5, 4.4; with more tiles 66 x 2048 x 1024 4.3, 4.4; 192 x 1024 x 4096 13.1, 9.8,
+    // in fp32 13.2, 17.1)
+    if (a.m <= 32 || !near || (a.m + 31) / 32 * ((a.n + 15) / 16) <= (DT == XL_F32 ? 2 : 1) * CUS) return launch_thin<DT, 2>(a, s);
     // The smallest tiles that still have a compute unit each, or share one by twos, then larger ones (us, bf16, k 2048, tiles of 64 alone / by twos, 128 alone / by twos, 256: 1024 x 1024 7.2, 8.5,
     // 11.9, 13.9, 25; 1024 x 2048 12.9, 10.5, 12.2, 14.2, 26; 1024 x 4096 24, 18.5, 13.0, 15.1, 26; 2048 x 4096 46, 34, 24, 21, 28; 4096 x 4096 90, 66, 46, 41, 33).
     auto tiles = [](long long m, long long n, int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
@@ -413,7 +417,7 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
     } else {
         if (tiles(a.m, a.n, 128) <= 2 * CUS) return launch_tile<DT, 128, 128, 2, 4, 1, 2>(a, s);
         // Tiles of 256 go through the chip in rounds of one a compute unit, and the last round may have few.  Where smaller tiles can do with what is left in less than half a
-        // round, they do, in a second launch (24642 x 4096 x 4096: 386 us in seven rounds, 350 so).
+        // round, they do, in a second launch (24642 x 4096 x 4096: 386 us in seven rounds, 366 so).
         const long long tn = (a.n + 255) / 256, rows = tiles(a.m, a.n, 256) / CUS * CUS / tn * 256;
         if (rows > 0 && rows < a.m && blocks >= 8 && tiles(a.m - rows, a.n, 128) <= CUS) {
             xl_block_matmul_args part = a;
