@@ -113,6 +113,40 @@ def test_a_recorded_step_gives_what_the_eager_one_gives():
             assert torch.equal(got, y) and torch.equal(step.cache[0], state[0]) and torch.equal(step.cache[1], state[1]), t
 
 
+def test_every_operator_can_be_recorded():
+    """Also where a call has two kernels: a large product, and a scan in parts with its workspace."""
+    g = torch.Generator().manual_seed(6)
+    r = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()  # noqa: E731
+    x, w, filters = r(4200, 1024), r(4096, 1024), r(64, 4).float()
+    u, B, C = r(1, 4100, 64), r(1, 4100, 16), r(1, 4100, 16)
+    A = -torch.arange(1.0, 17).repeat(64, 1).cuda()
+    wq, ws = seq.quantize_weight(w)
+
+    def run():
+        h, _ = seq.causal_conv(u, filters)
+        y, state = seq.selective_scan(h, u - 4, A, B, C, z=u)
+        return seq.block_matmul(*seq.quantize_rows(x), wq, ws), y, state
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for i in range(4):
+        x.copy_(r(4200, 1024))
+        u.copy_(r(1, 4100, 64))
+        want = run()                                        # eager work between the replays
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), i
+
+
 def test_work_follows_the_current_stream():
     block = ScanBlock(random_weights(64, 128))
     x = torch.randn(2, 300, 64, generator=torch.Generator().manual_seed(4)).bfloat16()
