@@ -559,10 +559,21 @@ template <int DT, int LP, int NS> static hipError_t launch_waves(const xl_scan_a
     return launch_tile<DT, LP, NS, 2, 16>(a, s);
 }
 
+// The same where channels are spread over more lanes, so that workgroups have a compute unit each: as many waves as there are tokens for, MOST at most (1024
+// channels, 16 states, us with 4, 8, 16 waves: 64 tokens 3.4, 4.0, 5.8; 128 tokens 4.4, 4.0, 5.8; 400 tokens 9.1, 7.6, 7.9; 3136 tokens -, 34.7, 32.3).
+template <int DT, int LP, int NS, int MOST> static hipError_t launch_spread(const xl_scan_args &a, hipStream_t s)
+{
+    if (a.length <= 64) return launch_tile<DT, LP, NS, 4, 16>(a, s);
+    if (MOST == 8 || a.length <= 512) return launch_tile<DT, LP, NS, 8, 16>(a, s);
+    return launch_tile<DT, LP, NS, MOST, 16>(a, s);
+}
+
 template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream_t s)
 {
-    // A token after the other costs 0.8 us each until there is enough to overlap, a tile 6 us or more.
-    if (a.length <= (groups_of(a, 4) <= 4 * CUS ? 4 : 12)) {
+    // A token after the other costs 0.7 us and more each behind the launch, a tile the same for up to 64 (2048 channels, 16 states, us with 2, 4, 6, 12 tokens: 1 sequence
+    // 3.4, 4.9, 6.3, 10.7, tile 4.1; 8 sequences 3.6, 4.9, 6.3, 10.6, tile 6.5; 32 sequences 4.9, 6.4, 8.0, 17.2, tile 21).
+    const long long fours = groups_of(a, 4);
+    if (a.length <= (fours <= CUS ? 2 : fours <= 4 * CUS ? 6 : 14)) {
         if (a.states <= 4) return launch_step<DT, 1>(a, s);
         if (a.states <= 8) return launch_step<DT, 2>(a, s);
         if (a.states <= 16) return launch_step<DT, 4>(a, s);
@@ -584,16 +595,16 @@ template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream
     // with 2, 1: 1024 channels 38, 25; 4096 channels 39, 36).
     if (a.states <= 4) return launch_waves<DT, 4, 1>(a, s);
     if (a.states <= 8) {
-        if (groups_of(a, 8) <= 2 * CUS) return launch_tile<DT, 8, 1, 8, 16>(a, s);
+        if (groups_of(a, 8) <= 2 * CUS) return launch_spread<DT, 8, 1, 8>(a, s);
         return launch_waves<DT, 4, 2>(a, s);
     }
     if (a.states <= 16) {
-        if (groups_of(a, 16) <= CUS) return launch_tile<DT, 16, 1, 16, 16>(a, s);
-        if (groups_of(a, 8) <= CUS) return launch_tile<DT, 8, 2, 8, 16>(a, s);
+        if (groups_of(a, 16) <= CUS) return launch_spread<DT, 16, 1, 16>(a, s);
+        if (groups_of(a, 8) <= CUS) return launch_spread<DT, 8, 2, 8>(a, s);
         return launch_waves<DT, 4, 4>(a, s);
     }
     if (a.states <= 32) {
-        if (groups_of(a, 16) <= CUS) return launch_tile<DT, 16, 2, 8, 16>(a, s);
+        if (groups_of(a, 16) <= CUS) return launch_spread<DT, 16, 2, 8>(a, s);
         return launch_waves<DT, 8, 4>(a, s);
     }
     if (a.states <= 64) return launch_waves<DT, 16, 4>(a, s);
