@@ -47,7 +47,7 @@ static constexpr unsigned NOWHERE = 0x80000000u;       // past the end of every 
 enum Access { VECTORS, SINGLES, SCATTERED };
 
 // A token after the other: LP lanes a channel, four states (a 16-byte load) a lane, 256 / LP channels a workgroup.  One token of 64 sequences of 2048 channels and 16
-// states: 6.2 us for 17.8 MB (2.9 TB/s), of which an empty launch is 2.6.
+// states: 5.9 us for 17.8 MB, of which an empty launch is 2.4; of 256 sequences 15 us for 71 MB (4.7 TB/s).
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int groups)
 {
@@ -67,23 +67,42 @@ __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int gro
     const T *zp = static_cast<const T *>(a.z) + b * a.z_batch + c, *Bp = static_cast<const T *>(a.B) + b * a.b_batch + n0;
     const T *Cp = static_cast<const T *>(a.C) + b * a.c_batch + n0;
     T *yp = static_cast<T *>(a.y) + b * a.y_batch + c;
+    // a token's numbers are read while the one before it is worked on, the first one's together with the states
+    struct Token {
+        T u, d, z;
+        Vec<T, NS> B, C;
+    };
+    auto read = [&](int t) {
+        Token k = {};
+        if (in) {
+            k.u = up[t * a.u_token];
+            k.d = dp[t * a.delta_token];
+            if (a.z) k.z = zp[t * a.z_token];
+        }
+        k.B = load_some<T, NS>(Bp + t * a.b_token, N - n0);
+        k.C = load_some<T, NS>(Cp + t * a.c_token, N - n0);
+        return k;
+    };
+    Token next = {};
+    if (len > 0) next = read(0);
     for (int t = 0; t < len; ++t) {
-        const float u = in ? (float)up[t * a.u_token] : 0.f;
-        float d = in ? (float)dp[t * a.delta_token] + bias : 0.f;
+        const Token k = next;
+        if (t + 1 < len) next = read(t + 1);
+        const float u = (float)k.u;
+        float d = in ? (float)k.d + bias : 0.f;
         if (a.softplus) d = softplus(d);
         const float s = d * u;
         float y = 0.f;
-        const Vec<T, NS> B = load_some<T, NS>(Bp + t * a.b_token, N - n0), C = load_some<T, NS>(Cp + t * a.c_token, N - n0);
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            h[i] = __builtin_fmaf(exp2_fast(d * A2[i]), h[i], s * (float)B[i]);
-            y = __builtin_fmaf((float)C[i], h[i], y);
+            h[i] = __builtin_fmaf(exp2_fast(d * A2[i]), h[i], s * (float)k.B[i]);
+            y = __builtin_fmaf((float)k.C[i], h[i], y);
         }
 #pragma unroll
         for (int o = 1; o < LP; o *= 2) y += __shfl_xor(y, o);
         if (part == 0 && in) {
             if (a.D) y = __builtin_fmaf(skip, u, y);
-            if (a.z) y *= silu((float)zp[t * a.z_token]);
+            if (a.z) y *= silu((float)k.z);
             yp[t * a.y_token] = (T)y;
         }
     }
@@ -570,10 +589,10 @@ template <int DT, int LP, int NS, int MOST> static hipError_t launch_spread(cons
 
 template <int DT> static hipError_t launch_type(const xl_scan_args &a, hipStream_t s)
 {
-    // A token after the other costs 0.7 us and more each behind the launch, a tile the same for up to 64 (2048 channels, 16 states, us with 2, 4, 6, 12 tokens: 1 sequence
-    // 3.4, 4.9, 6.3, 10.7, tile 4.1; 8 sequences 3.6, 4.9, 6.3, 10.6, tile 6.5; 32 sequences 4.9, 6.4, 8.0, 17.2, tile 21).
+    // A token after the other costs 0.45 us and more each behind the launch, a tile the same for up to 32 (2048 channels, 16 states, us with 2, 4, 8, 24 tokens: 1 sequence
+    // 2.9, 3.8, 5.6, 12.6, tile 4.1; 8 sequences 3.1, 4.0, 5.8, 12.9, tile 6.5; 32 sequences 4.4, 5.7, 8.3, 20.3, tile 22).
     const long long fours = groups_of(a, 4);
-    if (a.length <= (fours <= CUS ? 2 : fours <= 4 * CUS ? 6 : 14)) {
+    if (a.length <= (fours <= CUS ? 3 : fours <= 4 * CUS ? 8 : 24)) {
         if (a.states <= 4) return launch_step<DT, 1>(a, s);
         if (a.states <= 8) return launch_step<DT, 2>(a, s);
         if (a.states <= 16) return launch_step<DT, 4>(a, s);
