@@ -3,8 +3,8 @@
 //   h[n] <- exp(d A[n]) h[n] + d u B[n],   y = sum_n C[n] h[n] + D u,   y *= z sigmoid(z)
 //
 // exp(d A) is taken as 2^(d A log2 e), one hardware exponential.  Many tokens are bound by the issue of vector instructions: a state and token take an exponential and
-// five others, a channel and token some fifty more (softplus, gate, layouts), 9.5 for each of 16 states in all.  2 x 12321 x 2048 with 16
-// states in bf16: 276 us, 2.9e12 states a second, the vector units busy for 78 % of it; its 404 MB alone would take 86 us.  Single tokens are bound by the states' bytes.
+// five others, a channel and token some fifty more (softplus, gate, layouts), 9.2 for each of 16 states in all.  2 x 12321 x 2048 with 16
+// states in bf16: 258 us, 3.1e12 states a second, the vector units issuing for 84 % of it; its 404 MB alone would take 86 us.  Single tokens are bound by the states' bytes.
 #include <algorithm>
 #include <climits>
 #include <initializer_list>
@@ -146,7 +146,7 @@ struct Parts {
 
 // Many tokens.  A workgroup owns CH = 64 / LP channels of a sequence and goes through it in tiles of W x TK tokens, TK of them a wave: the recurrence is linear, so a
 // wave runs its tokens from a state of zero (which gives E) and multiplies up their factors (P = exp(A sum d)); then the waves exchange (P, E), each
-// folds those of the waves before it into the state that it begins with, and runs its tokens again, the factors and inputs
+// takes the state that its last tokens ended with past those of the others in between, and runs its tokens again, the factors and inputs
 // still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
 // tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
 template <int DT, int LP, int NS, int W, int TK, Access ACCESS>
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     static_assert(PER >= 1 && PERB >= 1 && TK % LP == 0, "a wave's tokens divide among its lanes");
     __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT];    // steps, and step x input (later the outputs): [channel][token]
     __shared__ float Bs_all[W][TK * NP], Cs_all[W][TK * NP];    // [token][state]
-    __shared__ Vec<float, NS> Ps[2][W * 64], Es[2][W * 64];
+    __shared__ Vec<float, NS> Ps[3][W * 64], Es[3][W * 64];
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
     float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave], *Cs = Cs_all[wave];
@@ -253,7 +253,10 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     };
 
     if (first < len) fetch(first);
-    for (int t0 = first, set = 0; t0 < len; t0 += TT, set ^= 1) {
+    Ps[2][threadIdx.x] = Vec<float, NS>{} + 1.f;        // before the first tile: nothing
+    Es[2][threadIdx.x] = Vec<float, NS>{};
+    int before = 2, set = 0;
+    for (int t0 = first; t0 < len; t0 += TT) {
         Vec<T, VE> uc[IT], zc[IT];
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
@@ -314,18 +317,15 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
         }
 #pragma unroll
         for (int i = 0; i < NS; ++i) p[i] = exp2_fast(sum * A2[i]);
-        // Two sets in turn: a wave that writes one again has passed the next tile's barrier, and so has every reader of it.
+        // Three sets in turn: a wave that writes one again has passed the second barrier behind it, and every reader of it the first.
         Ps[set][threadIdx.x] = p;
         Es[set][threadIdx.x] = e;
         __syncthreads();
-        float g[NS];
+        // from where this wave's tokens of the tile before ended, past the other waves': those behind it there, those before it here
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if (w == wave) {
-#pragma unroll
-                for (int i = 0; i < NS; ++i) g[i] = h[i];
-            }
-            const Vec<float, NS> pw = Ps[set][w * 64 + lane], ew = Es[set][w * 64 + lane];
+        for (int j = 1; j < W; ++j) {
+            const int from = wave + j < W ? before * W + wave + j : set * W + wave + j - W;
+            const Vec<float, NS> pw = Ps[0][from * 64 + lane], ew = Es[0][from * 64 + lane];
 #pragma unroll
             for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(pw[i], h[i], ew[i]);
         }
@@ -343,12 +343,14 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
                 const Vec<float, NS> B = KEEP ? Vec<float, NS>{} : *reinterpret_cast<const Vec<float, NS> *>(&Bs[(k + j) * NP + n0]);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
-                    g[i] = __builtin_fmaf(av[k + j][i], g[i], KEEP ? bv[KEEP ? k + j : 0][i] : s[j] * B[i]);
-                    y[j] = i ? __builtin_fmaf(C[i], g[i], y[j]) : C[i] * g[i];
+                    h[i] = __builtin_fmaf(av[k + j][i], h[i], KEEP ? bv[KEEP ? k + j : 0][i] : s[j] * B[i]);
+                    y[j] = i ? __builtin_fmaf(C[i], h[i], y[j]) : C[i] * h[i];
                 }
             }
             sx[c * PT + k + part] = sum_over_lanes<LP>(y, part);
         }
+        before = set;
+        set = set == 2 ? 0 : set + 1;
         wave_sync();
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
@@ -373,6 +375,14 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             if (i < nc) yp[t * a.y_token + ec + i] = (T)0.f;
     }
     if (wave == 0 && a.new_state && slot >= 0 && (first < len || first == 0) && len == whole) {     // the sequence ends here
+        if (first < len) {
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                const Vec<float, NS> pw = Ps[before][w * 64 + lane], ew = Es[before][w * 64 + lane];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(pw[i], h[i], ew[i]);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NS; ++i)
             if (in && n0 + i < N) a.new_state[(slot * D + c0 + c) * N + n0 + i] = h[i];
@@ -522,7 +532,7 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipE
         return true;
     };
     const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
-    // 2 x 12321 x 2048 with 16 states in bf16: 276 us as vectors, 315 one by one, 560 scattered (these with four waves in every case)
+    // 2 x 12321 x 2048 with 16 states in bf16: 258 us as vectors, 303 one by one, 560 scattered (these with four waves in every case)
     const unsigned wide = (unsigned)(groups * a.batch);
     if (!buffers) {
         tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
@@ -567,14 +577,14 @@ long long scan_workspace(const xl_scan_args &a)
     return p.count > 1 ? (2ll * p.count * a.batch * a.channels * a.states * 4 + 15) / 16 * 16 : 0;
 }
 
-// Waves of a workgroup.  One that has a compute unit to itself (its registers leave room for two waves a SIMD) takes eight, four where two fit and two where there are
-// four and more to overlap.  16 states, 3025 tokens, us with 2, 4, 8 waves: 256 workgroups 183, 96, 70;
-// 512 workgroups 243, 134, 140; 1024 workgroups 258, 260, 276.
+// Waves of a workgroup.  One that has a compute unit to itself (its registers leave room for two waves a SIMD) takes eight, four where two fit, and where there are four and more
+// to overlap two, or four if they stay long (us with 2, 4, 8 waves: 16 states, 3025 tokens, 256 workgroups 183, 96, 70, 512 workgroups 243, 134, 140; with 2, 4: 2048
+// workgroups of 3025 tokens 536, 488, 4096 of 200 164, 190, 4096 of 50 114, 153; 64 states, whose registers are short with four, 904, 974).
 template <int DT, int LP, int NS> static hipError_t launch_waves(const xl_scan_args &a, hipStream_t s)
 {
     const long long groups = groups_of(a, LP);
     if (groups <= CUS && a.length > 64) return launch_tile<DT, LP, NS, 8, 16>(a, s);
-    if (groups < 4 * CUS && a.length > 32) return launch_tile<DT, LP, NS, 4, 16>(a, s);
+    if (a.length > (groups < 4 * CUS ? 32 : LP < 16 ? 512 : INT_MAX)) return launch_tile<DT, LP, NS, 4, 16>(a, s);
     return launch_tile<DT, LP, NS, 2, 16>(a, s);
 }
 
