@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
@@ -41,14 +42,33 @@ template <typename... Args> [[noreturn]] void refuse(xl_status status, const Arg
     throw Refused{status, s.str()};
 }
 
+// One call: on the device of its first tensor, which is the current one for as long.
 struct Op {
     const char *name;
-    c10::DeviceIndex device;
+    const at::Tensor &first;
+    const c10::DeviceGuard guard;
+    const c10::DeviceIndex device;
 
-    Op(const char *name, const at::Tensor &first) : name(name)
+    Op(const char *name, const at::Tensor &first) : name(name), first(first), guard(on_gpu(name, first)), device(first.get_device()) {}
+
+    static c10::Device on_gpu(const char *name, const at::Tensor &t)
     {
-        if (!first.is_cuda()) refuse(XL_E_DEVICE, name, ": tensors must be on a GPU (there is no CPU path)");
-        device = first.get_device();
+        if (!t.is_cuda()) refuse(XL_E_DEVICE, name, ": tensors must be on a GPU (there is no CPU path)");
+        return t.device();
+    }
+
+    // A result: from the allocator that the first tensor's memory came from, without the way through the dispatcher where it is known (0.4 us).
+    at::Tensor make(at::IntArrayRef shape, at::ScalarType type) const
+    {
+        c10::Allocator *allocator = first.storage().allocator();
+        if (!allocator) return at::empty(shape, first.options().dtype(type));
+        return at::Tensor(at::detail::empty_generic(shape, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
+    }
+    at::Tensor make(at::IntArrayRef shape, at::IntArrayRef steps, at::ScalarType type) const
+    {
+        c10::Allocator *allocator = first.storage().allocator();
+        if (!allocator) return at::empty_strided(shape, steps, first.options().dtype(type));
+        return at::Tensor(at::detail::empty_strided_generic(shape, steps, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type));
     }
 
     // On the device, of the type and shape, no gradient asked for.
@@ -85,7 +105,6 @@ struct Op {
     // Enqueued on the current stream of the tensors' device.
     template <typename A> void run(xl_status (*f)(const A *, void *), const A &args) const
     {
-        const c10::DeviceGuard guard(c10::Device(c10::DeviceType::CUDA, device));
         const xl_status st = f(&args, c10::hip::getCurrentHIPStream(device).stream());
         if (st != XL_OK) throw Refused{st, g_last_error()};
     }
@@ -167,8 +186,8 @@ PyObject *causal_conv(const Args &in)       // x, weight, bias, silu, state, new
     a.nslots = slots && state->dim() ? state->size(0) : a.batch;
     const int64_t shape[] = {a.nslots, a.taps > 0 ? a.taps - 1 : 0, a.channels};
     at::Tensor made, made_state;
-    if (!given) given = &(made = at::empty(x.sizes(), x.options()));
-    if (!kept) kept = &(made_state = at::empty(shape, x.options()));
+    if (!given) given = &(made = op.make(x.sizes(), type));
+    if (!kept) kept = &(made_state = op.make(shape, type));
     int64_t b, t;
     op.rows("x", x, type, x.sizes(), b, t);
     a.x_batch = b, a.x_token = t;
@@ -205,8 +224,8 @@ PyObject *selective_scan(const Args &in)    // u, delta, A, B, C, D, z, delta_bi
     a.nslots = slots && state->dim() ? state->size(0) : a.batch;
     const int64_t shape[] = {a.nslots, a.channels, a.states}, wide[] = {a.batch, a.length, a.states};
     at::Tensor made, made_state;
-    if (!given) given = &(made = at::empty(u.sizes(), u.options()));
-    if (!kept) kept = &(made_state = at::empty(shape, u.options().dtype(at::kFloat)));
+    if (!given) given = &(made = op.make(u.sizes(), type));
+    if (!kept) kept = &(made_state = op.make(shape, at::kFloat));
     int64_t b, t;
     op.rows("u", u, type, u.sizes(), b, t);
     a.u_batch = b, a.u_token = t;
@@ -237,7 +256,7 @@ PyObject *selective_scan(const Args &in)    // u, delta, A, B, C, D, z, delta_bi
     a.y = given->data_ptr();
     at::Tensor workspace;
     a.workspace_bytes = g_scan_workspace(&a);
-    if (a.workspace_bytes > 0) a.workspace = (workspace = at::empty({a.workspace_bytes}, u.options().dtype(at::kByte))).data_ptr();
+    if (a.workspace_bytes > 0) a.workspace = (workspace = op.make({a.workspace_bytes}, at::kByte)).data_ptr();
     op.run(g_scan, a);
     return pair(in.args[13], *given, in.args[10] == Py_None && slots ? in.args[9] : in.args[10], *kept);
 }
@@ -269,13 +288,13 @@ PyObject *quantize(const Args &in)          // name, x, block_rows, out, scales
     at::Tensor made, made_scales;
     if (!out) {
         const int64_t wide = (a.k + 15) / 16 * 16;
-        made = at::empty({a.rows, wide}, x.options().dtype(at::kFloat8_e4m3fn));
-        if (wide != a.k) made = made.narrow(1, 0, a.k);
+        made = op.make({a.rows, wide}, at::kFloat8_e4m3fn);
+        if (wide != a.k) made.unsafeGetTensorImpl()->set_sizes_and_strides(x.sizes(), at::IntArrayRef{wide, 1});
         out = &made;
     }
     if (!scales) {      // a column for each block: the product reads the scales of neighbouring rows together
         const int64_t step[] = {a.block_rows == 1 ? 1 : shape[1], a.block_rows == 1 ? shape[0] : 1};
-        scales = &(made_scales = at::empty_strided(shape, step, x.options().dtype(at::kFloat)));
+        scales = &(made_scales = op.make(shape, step, at::kFloat));
     }
     op.check("x", x, type, x.sizes());
     op.check("out", *out, at::kFloat8_e4m3fn, x.sizes());
@@ -312,7 +331,7 @@ PyObject *block_matmul(const Args &in)      // a, a_scales, b, b_scales, bias, d
     const int64_t shape[] = {g.m, g.n}, blocks = (g.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
     at::Tensor made;
     if (out) op.check("out", *out, type, shape);
-    else out = &(made = at::empty(shape, a.options().dtype(type)));
+    else out = &(made = op.make(shape, type));
     op.check("a", a, at::kFloat8_e4m3fn, a.sizes());
     op.check("b", b, at::kFloat8_e4m3fn, {g.n, g.k});
     op.check("a_scales", a_scales, at::kFloat, {g.m, blocks});

@@ -159,6 +159,28 @@ def test_work_follows_the_current_stream():
     assert torch.equal(got, want) and torch.equal(other[0], state[0]) and torch.equal(other[1], state[1])
 
 
+def test_results_are_ordinary_tensors():
+    x = torch.randn(5, 200, generator=torch.Generator().manual_seed(7)).cuda()
+    filters = torch.ones(200, 4, device="cuda")
+    before = torch.cuda.memory_allocated()
+    q, s = seq.quantize_rows(x)
+    y, state = seq.causal_conv(x[None], filters)
+    assert torch.cuda.memory_allocated() > before
+    assert q.device == x.device and q.untyped_storage().nbytes() >= 5 * 208 and s.stride() == (1, 5)
+    assert not y.is_inference() and not y.requires_grad and y.is_contiguous()
+    w = y.clone().requires_grad_()
+    (w * y).sum().backward()                                # a constant in somebody's graph
+    assert torch.equal(w.grad, y) and y.resize_(1, 2, 200).shape == (1, 2, 200)
+    with torch.inference_mode():
+        z = seq.causal_conv(x[None], filters)[0]
+        assert z.is_inference()
+    other = torch.from_dlpack(x)                            # memory that torch did not allocate, as far as the tensor knows
+    q2, s2 = seq.quantize_rows(other)
+    assert torch.equal(q2.float(), q.float()) and torch.equal(s2, s)
+    del q, s, y, state, w, z, q2, s2, other
+    assert torch.cuda.memory_allocated() == before
+
+
 def test_what_does_not_fit_a_block_is_refused():
     block = ScanBlock(random_weights(64, 128))
     x = torch.zeros(2, 3, 64, dtype=torch.bfloat16, device="cuda")
