@@ -94,7 +94,7 @@ class TokenStep:
             block(self.x, self.cache, slots=self.slots)
         torch.cuda.current_stream(block.dev).wait_stream(side)
         self.graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(self.graph):
+        with torch.cuda.graph(self.graph, stream=side):         # by itself it would take a stream of the device that is current
             self.y, _ = block(self.x, self.cache, slots=self.slots)
         self.reset()
 

@@ -1,0 +1,66 @@
+"""CPU checks of the recorded step: which stream it is recorded on.  The device, its streams and the graph are stand-ins that keep books."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2007_06000_amd.scan_block import TokenStep
+
+DEVICE = torch.device("meta")           # stands for a GPU that is not the current one
+
+
+class Stream:
+    def __init__(self, device="the current device"):
+        self.device = device
+
+    def wait_stream(self, other):
+        pass
+
+
+class Block:
+    """What a step needs of a scan block; notes the stream that is current on its device whenever it is called."""
+    dev, dtype, width = DEVICE, torch.float32, 8
+
+    def __init__(self, streams):
+        self.streams, self.calls = streams, []
+
+    def cache(self, rows):
+        return torch.zeros(rows, 3, 16, device=DEVICE), torch.zeros(rows, 16, 4, device=DEVICE)
+
+    def __call__(self, x, state, slots):
+        self.calls.append(self.streams[-1])
+        return x.clone(), state
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """The stack of current streams, with the calls of torch.cuda that a step makes replaced."""
+    stack, recordings = [Stream()], []
+
+    @contextlib.contextmanager
+    def use(stream):
+        stack.append(stream)
+        yield
+        stack.pop()
+
+    @contextlib.contextmanager
+    def graph(graph, pool=None, stream=None, **more):
+        stream = stream or Stream()     # a stream of whichever device is the current one
+        recordings.append(stream)
+        with use(stream):
+            yield
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(device))
+    monkeypatch.setattr(torch.cuda, "CUDAGraph", object)
+    monkeypatch.setattr(torch.cuda, "graph", graph)
+    return stack, recordings
+
+
+def test_a_step_is_recorded_on_a_stream_of_its_blocks_device(streams):
+    stack, recordings = streams
+    block = Block(stack)
+    TokenStep(block, 2)
+    assert len(recordings) == 1 and recordings[0].device == DEVICE
+    assert len(block.calls) == 2 and all(s.device == DEVICE for s in block.calls) and block.calls[1] is recordings[0]
