@@ -135,8 +135,20 @@ template <int LP> __device__ __forceinline__ float sum_over_lanes(float *p, int 
     return (up1 ? p[1] : p[0]) + from_partner<0xb1>(up1 ? p[0] : p[1]);                                             // lane ^ 1
 }
 
+// A run of tokens makes P h + E of a state h, with E what a state of zero becomes and P = 2^x, x the sum of its tokens' exponents.  P may lie outside fp32 where P h does not, and
+// 0 x inf would be NaN.  So a P that underflows is the smallest number (an infinite state stays infinite), and one that overflows the largest (a state that is still zero stays zero).
+// Steps that may be negative let states grow by any amount: there (ROOT) P is kept as its square root, between 2^-126 and 2^127, and applied twice, which is right up to a growth of
+// 2^254, behind which every normal number is infinite; what shrinks by more than 2^-252 is below 1e-37.  With steps out of softplus states grow where A is positive, which is not what
+// such models learn: there one that is not zero is followed up to a growth of 2^128 within a wave's 16 tokens.  (Roots for them too: 2 x 12321 x 2048 with 16 states 282 us, not 258; a
+// test of the signs in front of the loop 266.)
+template <bool ROOT> __device__ __forceinline__ float factor(float x)
+{
+    return ROOT ? exp2_fast(__builtin_amdgcn_fmed3f(0.5f * x, -126.f, 127.f)) : __builtin_amdgcn_fmed3f(exp2_fast(x), 0x1p-149f, 0x1.fffffep127f);
+}
+template <bool ROOT> __device__ __forceinline__ float past(float p, float h, float e) { return __builtin_fmaf(p, ROOT ? p * h : h, e); }
+
 // Where there are not enough channels for the chip a sequence is worked on in `count` parts of `tokens` each.  For every part but the first there is what the one
-// before it makes of a state, E and then, behind all E, P, [batch][part][channel][state]; for the first the state that it begins with.
+// before it makes of a state, E and then, behind all E, the root of P, [batch][part][channel][state]; for the first the state that it begins with.
 struct Parts {
     float *results;
     int count, tokens;
@@ -149,7 +161,7 @@ struct Parts {
 // takes the state that its last tokens ended with past those of the others in between, and runs its tokens again, the factors and inputs
 // still in registers, now with the outputs.  The exchange is all that waves have to do with each other: what they read through LDS otherwise (steps, inputs, B, C, outputs of their own
 // tokens, transposed there between a layout for memory and one for the recurrence) is theirs alone, so a tile has one barrier.
-template <int DT, int LP, int NS, int W, int TK, Access ACCESS>
+template <int DT, int LP, int NS, int W, int TK, Access ACCESS, bool ROOT>
 __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int groups, const Parts parts)
 {
     typedef typename Elem<DT>::T T;
@@ -188,7 +200,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             P += step;
             const Vec<float, NS> p = load_some<float, NS>(P, live), e = load_some<float, NS>(E, live);
 #pragma unroll
-            for (int i = 0; i < NS; ++i) v[i] = __builtin_fmaf(p[i], v[i], e[i]);
+            for (int i = 0; i < NS; ++i) v[i] = past<true>(p[i], v[i], e[i]);
         }
 #pragma unroll
         for (int i = 0; i < NS; ++i) h[i] = v[i];
@@ -316,7 +328,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             }
         }
 #pragma unroll
-        for (int i = 0; i < NS; ++i) p[i] = exp2_fast(sum * A2[i]);
+        for (int i = 0; i < NS; ++i) p[i] = factor<ROOT>(sum * A2[i]);
         // Three sets in turn: a wave that writes one again has passed the second barrier behind it, and every reader of it the first.
         Ps[set][threadIdx.x] = p;
         Es[set][threadIdx.x] = e;
@@ -327,7 +339,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             const int from = wave + j < W ? before * W + wave + j : set * W + wave + j - W;
             const Vec<float, NS> pw = Ps[0][from * 64 + lane], ew = Es[0][from * 64 + lane];
 #pragma unroll
-            for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(pw[i], h[i], ew[i]);
+            for (int i = 0; i < NS; ++i) h[i] = past<ROOT>(pw[i], h[i], ew[i]);
         }
         // and again from the state that they find
 #pragma unroll
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             for (int w = 1; w < W; ++w) {
                 const Vec<float, NS> pw = Ps[before][w * 64 + lane], ew = Es[before][w * 64 + lane];
 #pragma unroll
-                for (int i = 0; i < NS; ++i) h[i] = __builtin_fmaf(pw[i], h[i], ew[i]);
+                for (int i = 0; i < NS; ++i) h[i] = past<ROOT>(pw[i], h[i], ew[i]);
             }
         }
 #pragma unroll
@@ -399,7 +411,8 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
     constexpr int PER = CH * TK / 64, VE = ACCESS != VECTORS ? 1 : PER < 4 ? PER : 4, IT = PER / VE;
     constexpr int PERB = NP * TK / 64, VB = ACCESS != VECTORS ? 1 : PERB < 4 ? PERB : 4, IB = PERB / VB;
     __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT], Bs_all[W][TK * NP];
-    __shared__ Vec<float, NS> Ps[W * 64], Es[W * 64];
+    __shared__ Vec<float, NS> Es[W * 64];
+    __shared__ float totals[W * 64];
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), c = lane / LP, part = lane % LP, n0 = part * NS;
     float *dl = dl_all[wave], *sx = sx_all[wave], *Bs = Bs_all[wave];
@@ -488,23 +501,21 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
         total += sum;
         wave_sync();
     }
-#pragma unroll
-    for (int i = 0; i < NS; ++i) p[i] = exp2_fast(total * A2[i]);
-    Ps[threadIdx.x] = p;
+    totals[threadIdx.x] = total;
     Es[threadIdx.x] = e;
     __syncthreads();
     if (wave != 0 || live <= 0) return;
     e = begin;
-    p = Vec<float, NS>{} + 1.f;
-#pragma unroll
+    total = 0.f;
     for (int w = 0; w < W; ++w) {
-        const Vec<float, NS> pw = Ps[w * 64 + lane], ew = Es[w * 64 + lane];
+        const float t = totals[w * 64 + lane];
+        const Vec<float, NS> ew = Es[w * 64 + lane];
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            e[i] = __builtin_fmaf(pw[i], e[i], ew[i]);
-            p[i] *= pw[i];
-        }
+        for (int i = 0; i < NS; ++i) e[i] = past<true>(factor<true>(t * A2[i]), e[i], ew[i]);
+        total += t;
     }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) p[i] = factor<true>(total * A2[i]);
     store_some<float, NS>(out + step, live, e);
     store_some<float, NS>(out + step + parts.factors(a.batch, D, N), live, p);
 }
@@ -516,7 +527,7 @@ template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, h
     return hipGetLastError();
 }
 
-template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s, Parts parts = {nullptr, 1, INT_MAX})
+template <int DT, int LP, int NS, int W, int TK, bool SPLIT, bool ROOT> static hipError_t launch_tile_as(const xl_scan_args &a, hipStream_t s, const Parts &parts)
 {
     typedef typename Elem<DT>::T T;
     constexpr int CH = 64 / LP, PER = CH * TK / 64, VE = PER < 4 ? PER : 4, PERB = LP * NS * TK / 64, VB = PERB < 4 ? PERB : 4;
@@ -535,7 +546,7 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipE
     // 2 x 12321 x 2048 with 16 states in bf16: 258 us as vectors, 303 one by one, 560 scattered (these with four waves in every case)
     const unsigned wide = (unsigned)(groups * a.batch);
     if (!buffers) {
-        tile_kernel<DT, LP, NS, 4, TK, SCATTERED><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
+        tile_kernel<DT, LP, NS, 4, TK, SCATTERED, ROOT><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
         return hipGetLastError();
     }
     if constexpr (SPLIT) {
@@ -546,9 +557,14 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipE
         if (e != hipSuccess) return e;
     }
     const dim3 grid(wide, (unsigned)parts.count);
-    if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups, parts);
-    else tile_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups, parts);
+    if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS, ROOT><<<grid, 64 * W, 0, s>>>(a, groups, parts);
+    else tile_kernel<DT, LP, NS, W, TK, SINGLES, ROOT><<<grid, 64 * W, 0, s>>>(a, groups, parts);
     return hipGetLastError();
+}
+
+template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s, const Parts &parts = {nullptr, 1, INT_MAX})
+{
+    return a.softplus ? launch_tile_as<DT, LP, NS, W, TK, SPLIT, false>(a, s, parts) : launch_tile_as<DT, LP, NS, W, TK, SPLIT, true>(a, s, parts);
 }
 
 static constexpr long long CUS = 256;
