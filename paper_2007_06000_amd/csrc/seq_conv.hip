@@ -89,8 +89,7 @@ template <int DT, int K, int V> static hipError_t launch(const xl_causal_conv_ar
     long long run = 32;
     while (run > 4 && a.batch * vecs * ((a.length + run - 1) / run) < 256ll * 2048) run /= 2;
     const long long runs = a.length > 0 ? (a.length + run - 1) / run : 1, blocks = (a.batch * vecs * runs + 255) / 256;
-    conv_kernel<DT, K, V><<<dim3((unsigned)blocks), 256, 0, s>>>(a, (int)run, (int)runs);
-    return hipGetLastError();
+    return launch_kernel(conv_kernel<DT, K, V>, dim3((unsigned)blocks), 256, s, a, (int)run, (int)runs);
 }
 
 template <int DT, int K> static hipError_t launch_taps(const xl_causal_conv_args &a, hipStream_t s)

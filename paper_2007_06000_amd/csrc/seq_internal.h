@@ -10,6 +10,16 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// A kernel's launch and its own status.  (The runtime's last error may be one that somebody else's call has left.)
+template <typename T> struct Same {
+    typedef T Type;
+};
+template <typename... P> static hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, unsigned threads, hipStream_t s, typename Same<P>::Type... args)
+{
+    void *list[] = {&args...};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), list, 0, s);
+}
+
 static constexpr float LOG2E = 1.44269504088896340736f;
 
 // Activations in memory <-> fp32.  Conversions to 16 bits round to nearest, ties to even.

@@ -381,8 +381,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const xl_block_matmu
 template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError_t launch_tile(const xl_block_matmul_args &a, hipStream_t s)
 {
     const long long tm = (a.m + BM - 1) / BM, tn = (a.n + BN - 1) / BN;
-    tile_kernel<DT, BM, BN, WM, WN, KS, S><<<dim3((unsigned)(tm * tn)), 64 * WM * WN, 0, s>>>(a, (int)tm, (int)tn);
-    return hipGetLastError();
+    return launch_kernel(tile_kernel<DT, BM, BN, WM, WN, KS, S>, dim3((unsigned)(tm * tn)), 64 * WM * WN, s, a, (int)tm, (int)tn);
 }
 
 static constexpr long long CUS = 256;
@@ -390,8 +389,7 @@ static constexpr long long CUS = 256;
 template <int DT, int MT> static hipError_t launch_thin(const xl_block_matmul_args &a, hipStream_t s)
 {
     const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 16 * MT - 1) / (16 * MT));
-    thin_kernel<DT, MT><<<dim3((unsigned)tiles), 512, 0, s>>>(a, (int)tiles_n);
-    return hipGetLastError();
+    return launch_kernel(thin_kernel<DT, MT>, dim3((unsigned)tiles), 512, s, a, (int)tiles_n);
 }
 
 template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)

@@ -109,23 +109,17 @@ __global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
     }
 }
 
-template <int DT, int PER> static void launch_rows(const xl_quantize_args &a, hipStream_t s)
+template <int DT, int PER> static hipError_t launch_rows(const xl_quantize_args &a, hipStream_t s)
 {
     const long long blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK, under = 16 / PER;
-    rows_kernel<DT, PER><<<grid_of((blocks + PER - 1) / PER, (a.rows + under - 1) / under), 256, 0, s>>>(a);
+    return launch_kernel(rows_kernel<DT, PER>, grid_of((blocks + PER - 1) / PER, (a.rows + under - 1) / under), 256, s, a);
 }
 
 template <int DT> static hipError_t launch_type(const xl_quantize_args &a, hipStream_t s)
 {
     const long long blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
-    if (a.block_rows == 1) {
-        if (blocks == 1) launch_rows<DT, 1>(a, s);
-        else if (blocks == 2) launch_rows<DT, 2>(a, s);
-        else launch_rows<DT, 4>(a, s);
-    } else {
-        blocks_kernel<DT><<<grid_of(blocks, (a.rows + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK), 256, 0, s>>>(a);
-    }
-    return hipGetLastError();
+    if (a.block_rows != 1) return launch_kernel(blocks_kernel<DT>, grid_of(blocks, (a.rows + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK), 256, s, a);
+    return blocks == 1 ? launch_rows<DT, 1>(a, s) : blocks == 2 ? launch_rows<DT, 2>(a, s) : launch_rows<DT, 4>(a, s);
 }
 
 hipError_t launch_quantize(const xl_quantize_args &a, hipStream_t s)

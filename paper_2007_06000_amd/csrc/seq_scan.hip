@@ -523,8 +523,7 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
 template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, hipStream_t s)
 {
     const int per = 256 / LP, groups = (int)((a.channels + per - 1) / per);
-    step_kernel<DT, LP><<<dim3((unsigned)(groups * a.batch)), 256, 0, s>>>(a, groups);
-    return hipGetLastError();
+    return launch_kernel(step_kernel<DT, LP>, dim3((unsigned)(groups * a.batch)), 256, s, a, groups);
 }
 
 template <int DT, int LP, int NS, int W, int TK, bool SPLIT, bool ROOT> static hipError_t launch_tile_as(const xl_scan_args &a, hipStream_t s, const Parts &parts)
@@ -545,21 +544,14 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT, bool ROOT> static h
     const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
     // 2 x 12321 x 2048 with 16 states in bf16: 258 us as vectors, 303 one by one, 560 scattered (these with four waves in every case)
     const unsigned wide = (unsigned)(groups * a.batch);
-    if (!buffers) {
-        tile_kernel<DT, LP, NS, 4, TK, SCATTERED, ROOT><<<dim3(wide), 64 * 4, 0, s>>>(a, groups, Parts{nullptr, 1, INT_MAX});
-        return hipGetLastError();
-    }
+    if (!buffers) return launch_kernel(tile_kernel<DT, LP, NS, 4, TK, SCATTERED, ROOT>, dim3(wide), 64 * 4, s, a, groups, Parts{nullptr, 1, INT_MAX});
     if constexpr (SPLIT) {
         const dim3 grid(wide, (unsigned)parts.count - 1);
-        if (vectors) part_kernel<DT, LP, NS, W, TK, VECTORS><<<grid, 64 * W, 0, s>>>(a, groups, parts);
-        else part_kernel<DT, LP, NS, W, TK, SINGLES><<<grid, 64 * W, 0, s>>>(a, groups, parts);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_kernel(vectors ? part_kernel<DT, LP, NS, W, TK, VECTORS> : part_kernel<DT, LP, NS, W, TK, SINGLES>, grid, 64 * W, s, a, groups, parts);
         if (e != hipSuccess) return e;
     }
     const dim3 grid(wide, (unsigned)parts.count);
-    if (vectors) tile_kernel<DT, LP, NS, W, TK, VECTORS, ROOT><<<grid, 64 * W, 0, s>>>(a, groups, parts);
-    else tile_kernel<DT, LP, NS, W, TK, SINGLES, ROOT><<<grid, 64 * W, 0, s>>>(a, groups, parts);
-    return hipGetLastError();
+    return launch_kernel(vectors ? tile_kernel<DT, LP, NS, W, TK, VECTORS, ROOT> : tile_kernel<DT, LP, NS, W, TK, SINGLES, ROOT>, grid, 64 * W, s, a, groups, parts);
 }
 
 template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s, const Parts &parts = {nullptr, 1, INT_MAX})
