@@ -110,6 +110,12 @@ struct Op {
     }
 };
 
+// A tensor of the caller's has new contents: whoever has saved it for a backward pass has to find out.
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int64_t type_code(const char *name, const char *what, at::ScalarType t)
 {
     switch (t) {
@@ -202,6 +208,8 @@ PyObject *causal_conv(const Args &in)       // x, weight, bias, silu, state, new
     a.slots = op.dense_as<int>("slots", slots, at::kInt, {a.batch});
     a.y = given->data_ptr();
     op.run(g_conv, a);
+    if (given != &made) written(*given);
+    if (kept != &made_state) written(*kept);
     return pair(in.args[8], *given, in.args[5] == Py_None && slots ? in.args[4] : in.args[5], *kept);
 }
 
@@ -258,6 +266,8 @@ PyObject *selective_scan(const Args &in)    // u, delta, A, B, C, D, z, delta_bi
     a.workspace_bytes = g_scan_workspace(&a);
     if (a.workspace_bytes > 0) a.workspace = (workspace = op.make({a.workspace_bytes}, at::kByte)).data_ptr();
     op.run(g_scan, a);
+    if (given != &made) written(*given);
+    if (kept != &made_state) written(*kept);
     return pair(in.args[13], *given, in.args[10] == Py_None && slots ? in.args[9] : in.args[10], *kept);
 }
 
@@ -309,6 +319,8 @@ PyObject *quantize(const Args &in)          // name, x, block_rows, out, scales
     a.q = out->data_ptr();
     a.scales = static_cast<float *>(scales->data_ptr());
     op.run(g_quantize, a);
+    if (out != &made) written(*out);
+    if (scales != &made_scales) written(*scales);
     return pair(in.args[3], *out, in.args[4], *scales);
 }
 
@@ -354,6 +366,7 @@ PyObject *block_matmul(const Args &in)      // a, a_scales, b, b_scales, bias, d
     g.bias = op.dense_as<float>("bias", bias, at::kFloat, {g.n});
     g.y = out->data_ptr();
     op.run(g_matmul, g);
+    if (out != &made) written(*out);
     PyObject *result = in.args[6] == Py_None ? THPVariable_Wrap(*out) : Py_NewRef(in.args[6]);
     if (!result) throw python_error();
     return result;

@@ -96,6 +96,7 @@ class TokenStep:
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph, stream=side):         # by itself it would take a stream of the device that is current
             self.y, _ = block(self.x, self.cache, slots=self.slots)
+        self.written = [t for t in (self.y, *self.cache) if not t.is_inference()]
         self.reset()
 
     def reset(self):
@@ -106,6 +107,7 @@ class TokenStep:
         """x [batch, 1, width]; the result is overwritten by the next step."""
         self.x.copy_(x)
         self.graph.replay()
+        torch.autograd.graph.increment_version(self.written)    # for whoever has saved one of them for a backward pass
         return self.y
 
 

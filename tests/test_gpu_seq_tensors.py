@@ -32,3 +32,64 @@ def test_an_error_that_another_call_left_is_not_this_calls():
         finally:
             hip.hipGetLastError()
         assert all(torch.equal(a.float(), b.float()) for a, b in zip(got, want)), name
+
+
+def versions(*tensors):
+    return [t._version for t in tensors]
+
+
+def test_tensors_that_a_call_writes_get_a_new_version():
+    x, w, B = torch.randn(2, 9, 16, device="cuda"), torch.randn(16, 4, device="cuda"), torch.randn(2, 9, 4, device="cuda")
+    A, slots = -torch.rand(16, 4, device="cuda"), torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    for make, call in ((lambda: torch.zeros(3, 3, 16, device="cuda"), lambda **k: seq.causal_conv(x, w, **k)),
+                       (lambda: torch.zeros(3, 16, 4, device="cuda"), lambda **k: seq.selective_scan(x, x, A, B, B, **k))):
+        out, cache = torch.empty_like(x), make()
+        before, inputs = versions(out, cache), versions(x, w, B, A, slots)
+        call(state=cache, slots=slots, out=out)
+        assert [a > b for a, b in zip(versions(out, cache), before)] == [True, True]
+        state, new = make()[:2].clone(), make()[:2].clone()
+        before = versions(state, new)
+        call(state=state, new_state=new)
+        assert versions(state) == before[:1] and versions(new)[0] > before[1]
+        before = versions(out)
+        with pytest.raises(seq.XlError):
+            call(state=state[:1], out=out)
+        assert versions(out) == before and versions(x, w, B, A, slots) == inputs
+    q, s = seq.quantize_rows(x[0])
+    for call, given in ((lambda: seq.quantize_rows(x[0], out=q, scales=s), (q, s)), (lambda: seq.quantize_weight(x[0], out=q), (q,)),
+                        (lambda: seq.block_matmul(q, s, q, s[:1], out=room), (room := torch.empty(9, 9, device="cuda"),))):
+        before = versions(*given)
+        call()
+        assert all(a > b for a, b in zip(versions(*given), before))
+
+
+def test_somebody_elses_backward_pass_notices_that_its_tensor_was_overwritten():
+    x, w = torch.randn(2, 9, 16, device="cuda"), torch.randn(16, 4, device="cuda")
+    out, leaf = torch.randn(2, 9, 16, device="cuda"), torch.ones(2, 9, 16, device="cuda", requires_grad=True)
+    loss = (leaf * out).sum()           # keeps out for the gradient of leaf
+    seq.causal_conv(x, w, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_results_made_in_inference_mode_may_be_written_again():
+    x, w = torch.randn(2, 9, 16, device="cuda"), torch.randn(16, 4, device="cuda")
+    with torch.inference_mode():
+        out, state = seq.causal_conv(x, w)
+    assert out.is_inference()
+    want = out.clone()
+    seq.causal_conv(x, w, out=out, new_state=state)
+    assert torch.equal(out, want)
+
+
+def test_a_recorded_steps_tensors_get_a_new_version_with_every_step():
+    from paper_2007_06000_amd.scan_block import ScanBlock, TokenStep, random_weights
+    step = TokenStep(ScanBlock(random_weights(64, 128)), 2)
+    x = torch.randn(2, 1, 64, device="cuda").bfloat16()
+    leaf = torch.ones(2, 1, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    loss = (leaf * step(x)).sum()
+    before = versions(step.y, *step.cache)
+    step(x)
+    assert all(a > b for a, b in zip(versions(step.y, *step.cache), before))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
