@@ -9,6 +9,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
@@ -71,13 +72,14 @@ struct Op {
         return at::Tensor(at::detail::empty_strided_generic(shape, steps, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type));
     }
 
-    // On the device, of the type and shape, no gradient asked for.
+    // On the device, of the type and shape, no gradient asked for, backwards or forwards.
     void check(const char *what, const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape) const
     {
         if (!t.is_cuda() || t.get_device() != device) refuse(XL_E_DEVICE, name, ": ", what, " is on ", t.device(), ", not on cuda:", int(device));
         if (t.scalar_type() != type) refuse(XL_E_UNSUPPORTED, name, ": ", what, " is ", t.scalar_type(), ", not ", type);
         if (t.sizes() != shape) refuse(XL_E_SHAPE, name, ": ", what, " has shape ", t.sizes(), ", not ", shape);
         if (t.requires_grad() && c10::GradMode::is_enabled()) refuse(XL_E_UNSUPPORTED, name, ": ", what, " asks for a gradient: inference only");
+        if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode()) refuse(XL_E_UNSUPPORTED, name, ": ", what, " carries a tangent: inference only");
     }
 
     // [batch, length, width] with a contiguous last dimension: its steps between sequences and tokens.

@@ -93,3 +93,21 @@ def test_a_recorded_steps_tensors_get_a_new_version_with_every_step():
     assert all(a > b for a, b in zip(versions(step.y, *step.cache), before))
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_tensors_that_carry_a_tangent_are_refused():
+    from torch.autograd import forward_ad
+    x, w, B = torch.randn(2, 9, 16, device="cuda"), torch.randn(16, 4, device="cuda"), torch.randn(2, 9, 4, device="cuda")
+    A = -torch.rand(16, 4, device="cuda")
+    q, s = seq.quantize_rows(x[0])
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: seq.causal_conv(dual(x), w), lambda: seq.causal_conv(x, dual(w)), lambda: seq.causal_conv(x, w, dual(w[:, 0].contiguous())),
+                     lambda: seq.selective_scan(dual(x), x, A, B, B), lambda: seq.selective_scan(x, x, dual(A), B, B), lambda: seq.selective_scan(x, x, A, B, dual(B)),
+                     lambda: seq.selective_scan(x, x, A, B, B, z=dual(x)), lambda: seq.quantize_rows(dual(x[0])), lambda: seq.quantize_weight(dual(x[0])),
+                     lambda: seq.block_matmul(q, dual(s), q, s[:1]), lambda: seq.block_matmul(q, s, q, s[:1], bias=dual(x[0, :, 0].contiguous()))):
+            with torch.no_grad(), pytest.raises(seq.XlError, match="tangent"):      # no_grad is about backward passes only
+                call()
+        with torch.inference_mode():
+            seq.causal_conv(dual(x), w)         # no gradients of any kind are asked for here
+        seq.causal_conv(x, w)
