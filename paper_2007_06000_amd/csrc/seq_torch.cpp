@@ -78,6 +78,7 @@ struct Op {
         if (!t.is_cuda() || t.get_device() != device) refuse(XL_E_DEVICE, name, ": ", what, " is on ", t.device(), ", not on cuda:", int(device));
         if (t.scalar_type() != type) refuse(XL_E_UNSUPPORTED, name, ": ", what, " is ", t.scalar_type(), ", not ", type);
         if (t.sizes() != shape) refuse(XL_E_SHAPE, name, ": ", what, " has shape ", t.sizes(), ", not ", shape);
+        if (t.is_neg()) refuse(XL_E_UNSUPPORTED, name, ": ", what, " is a view of numbers that are to be negated (resolve_neg makes a tensor of it)");
         if (t.requires_grad() && c10::GradMode::is_enabled()) refuse(XL_E_UNSUPPORTED, name, ": ", what, " asks for a gradient: inference only");
         if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode()) refuse(XL_E_UNSUPPORTED, name, ": ", what, " carries a tangent: inference only");
     }

@@ -111,3 +111,16 @@ def test_tensors_that_carry_a_tangent_are_refused():
         with torch.inference_mode():
             seq.causal_conv(dual(x), w)         # no gradients of any kind are asked for here
         seq.causal_conv(x, w)
+
+
+def test_views_whose_numbers_are_to_be_negated_are_refused():
+    pairs = torch.randn(2, 9, 1, 2, device="cuda")
+    x, w = torch.view_as_complex(pairs).conj().imag, torch.randn(1, 4, device="cuda")       # -pairs[..., 1], read through a mark on the tensor
+    assert x.is_neg()
+    with pytest.raises(seq.XlError, match="negated"):
+        seq.causal_conv(x, w)
+    y, _ = seq.causal_conv(x.resolve_neg(), w)
+    want, _ = seq.causal_conv(-pairs[..., 1].contiguous(), w)
+    assert torch.equal(y, want)
+    with pytest.raises(seq.XlError, match="negated"):
+        seq.quantize_rows(x[..., 0][:, :1])
