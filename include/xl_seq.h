@@ -70,8 +70,8 @@ xl_status xl_causal_conv(const xl_causal_conv_args *args, void *stream);
  *   h[n] = exp(d * A[c,n]) * h[n] + d * u[t,c] * B[t,n]
  *   y    = (sum over n of C[t,n] * h[n]  +  D[c] * u[t,c]) * z[t,c] * sigmoid(z[t,c])
  * delta_bias, D and z may be NULL (left out).  u, delta, B, C, z and y are of type `dtype`; A, D, delta_bias and the
- * states [nslots, channels, states] are fp32, and so is all arithmetic.  y may be u's or z's memory with the
- * same steps, and must not overlap the inputs otherwise.
+ * states [nslots, channels, states] are fp32, and so is all arithmetic.  y may be u's, delta's or z's memory with
+ * the same steps, and must not overlap the inputs otherwise.
  * A token's factor exp(d * A) has to be an fp32 number.  States may grow: without `softplus` by as much as fp32 holds; with it, where A is positive, by up to 2^128 within 16
  * tokens (a state of zero stays zero whatever the growth).  What an infinite or NaN input makes of its channel is not finite from its token on; infinity or NaN is not said.
  */

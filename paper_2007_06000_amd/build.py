@@ -71,13 +71,13 @@ def _compile(item, headers, force: bool) -> str:
 
 def _build_module(force: bool) -> str:
     src = os.path.join(CSRC, "seq_torch.cpp")
-    newest = max(os.path.getmtime(p) for p in [src] + SEQ_HEADERS[2:])
+    newest = max(os.path.getmtime(p) for p in [src, os.path.join(CSRC, "seq_overlap.h")] + SEQ_HEADERS[2:])
     if not force and os.path.exists(MODULE) and os.path.getmtime(MODULE) >= newest:
         return MODULE
     from torch.utils.cpp_extension import include_paths, library_paths     # both name only files of the installed torch
     system = [*include_paths(), sysconfig.get_path("include"), "/opt/rocm/include"]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", *[f for p in system for f in ("-isystem", p)],
-           "-I" + os.path.join(ROOT, "include"), "-shared", "-o", MODULE, src, *["-L" + p for p in library_paths()],
+           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-shared", "-o", MODULE, src, *["-L" + p for p in library_paths()],
            "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.stderr.strip():

@@ -15,9 +15,11 @@
 #include <c10/hip/HIPStream.h>
 
 #include <cstdint>
+#include <initializer_list>
 #include <sstream>
 #include <string>
 
+#include "seq_overlap.h"
 #include "xl_seq.h"
 
 namespace {
@@ -42,6 +44,25 @@ template <typename... Args> [[noreturn]] void refuse(xl_status status, const Arg
     (s << ... << args);
     throw Refused{status, s.str()};
 }
+
+// Where tensors lie: rows of [batch, length, width], a contiguous block (or nothing), rows of [rows, k] that take `width` bytes each, and single numbers of [rows, columns].
+int64_t address(const at::Tensor &t) { return reinterpret_cast<int64_t>(t.data_ptr()); }
+xls::Span rows_of(const at::Tensor &t)
+{
+    const int64_t size = t.element_size();
+    return {address(t), t.size(0), t.size(1), t.stride(0) * size, t.stride(1) * size, t.size(2) * size};
+}
+xls::Span block_of(const at::Tensor *t) { return t ? xls::Span{address(*t), 1, 1, 0, 0, int64_t(t->nbytes())} : xls::Span{}; }
+xls::Span rows_of(const at::Tensor &t, int64_t width) { return {address(t), 1, t.size(0), 0, t.stride(0) * int64_t(t.element_size()), width}; }
+xls::Span numbers_of(const at::Tensor &t)
+{
+    const int64_t size = t.element_size();
+    return {address(t), t.size(0), t.size(1), t.stride(0) * size, t.stride(1) * size, size};
+}
+struct Named {
+    const char *what;
+    xls::Span span;
+};
 
 // One call: on the device of its first tensor, which is the current one for as long.
 struct Op {
@@ -103,6 +124,13 @@ struct Op {
     template <typename T> T *dense_as(const char *what, const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape) const
     {
         return static_cast<T *>(dense(what, t, type, shape));
+    }
+
+    // A tensor of the caller's that the call writes, apart from what it reads and writes otherwise.
+    void apart(const char *what, const xls::Span &written, std::initializer_list<Named> others) const
+    {
+        for (const Named &o : others)
+            if (xls::overlap(written, o.span)) refuse(XL_E_SHAPE, name, ": ", what, " shares memory with ", o.what);
     }
 
     // Enqueued on the current stream of the tensors' device.
@@ -210,6 +238,12 @@ PyObject *causal_conv(const Args &in)       // x, weight, bias, silu, state, new
     a.lengths = op.dense_as<int>("lengths", lengths, at::kInt, {a.batch});
     a.slots = op.dense_as<int>("slots", slots, at::kInt, {a.batch});
     a.y = given->data_ptr();
+    if (given != &made || kept != &made_state) {
+        const Named old = {"state (or is it, as a whole)", a.state != a.new_state ? block_of(state) : xls::Span{}}, input = {"x", rows_of(x)};
+        const Named shared[] = {{"weight", block_of(&weight)}, {"bias", block_of(bias)}, {"lengths", block_of(lengths)}, {"slots", block_of(slots)}};
+        if (given != &made) op.apart("out", rows_of(*given), {input, old, {"new_state", block_of(kept)}, shared[0], shared[1], shared[2], shared[3]});
+        if (kept != &made_state) op.apart("new_state", block_of(kept), {input, old, shared[0], shared[1], shared[2], shared[3]});
+    }
     op.run(g_conv, a);
     if (given != &made) written(*given);
     if (kept != &made_state) written(*kept);
@@ -265,6 +299,19 @@ PyObject *selective_scan(const Args &in)    // u, delta, A, B, C, D, z, delta_bi
     a.lengths = op.dense_as<int>("lengths", lengths, at::kInt, {a.batch});
     a.slots = op.dense_as<int>("slots", slots, at::kInt, {a.batch});
     a.y = given->data_ptr();
+    if (given != &made || kept != &made_state) {
+        const Named old = {"state (or is it, as a whole)", a.state != a.new_state ? block_of(state) : xls::Span{}};
+        const Named shared[] = {{"A", block_of(&A)}, {"D", block_of(D)}, {"delta_bias", block_of(delta_bias)}, {"B", rows_of(B)}, {"C", rows_of(C)}, {"lengths", block_of(lengths)}, {"slots", block_of(slots)}};
+        Named tokens[] = {{"u (or is it, as a whole)", rows_of(u)}, {"delta (or is it, as a whole)", rows_of(delta)}, {"z (or is it, as a whole)", z ? rows_of(*z) : xls::Span{}}};
+        if (kept != &made_state)
+            op.apart("new_state", block_of(kept), {tokens[0], tokens[1], tokens[2], old, shared[0], shared[1], shared[2], shared[3], shared[4], shared[5], shared[6]});
+        if (given != &made) {       // may take the place of an input of its shape, as a whole: a token's numbers are read before its result is written
+            const xls::Span y = rows_of(*given);
+            for (Named &t : tokens)
+                if (t.span == y) t.span = {};
+            op.apart("out", y, {tokens[0], tokens[1], tokens[2], old, {"new_state", block_of(kept)}, shared[0], shared[1], shared[2], shared[3], shared[4], shared[5], shared[6]});
+        }
+    }
     at::Tensor workspace;
     a.workspace_bytes = g_scan_workspace(&a);
     if (a.workspace_bytes > 0) a.workspace = (workspace = op.make({a.workspace_bytes}, at::kByte)).data_ptr();
@@ -321,6 +368,9 @@ PyObject *quantize(const Args &in)          // name, x, block_rows, out, scales
     a.x = x.data_ptr();
     a.q = out->data_ptr();
     a.scales = static_cast<float *>(scales->data_ptr());
+    const xls::Span input = rows_of(x, a.k * int64_t(x.element_size()));
+    if (out != &made) op.apart("out", rows_of(*out, (a.k + 15) / 16 * 16), {{"x", input}, {"scales", numbers_of(*scales)}});
+    if (scales != &made_scales) op.apart("scales", numbers_of(*scales), {{"x", input}});
     op.run(g_quantize, a);
     if (out != &made) written(*out);
     if (scales != &made_scales) written(*scales);
@@ -368,6 +418,9 @@ PyObject *block_matmul(const Args &in)      // a, a_scales, b, b_scales, bias, d
     g.b_scales = static_cast<const float *>(b_scales.data_ptr());
     g.bias = op.dense_as<float>("bias", bias, at::kFloat, {g.n});
     g.y = out->data_ptr();
+    if (out != &made)
+        op.apart("out", rows_of(*out, g.n * int64_t(out->element_size())),
+                 {{"a", rows_of(a, g.k)}, {"b", rows_of(b, g.k)}, {"a_scales", numbers_of(a_scales)}, {"b_scales", numbers_of(b_scales)}, {"bias", block_of(bias)}});
     op.run(g_matmul, g);
     if (out != &made) written(*out);
     PyObject *result = in.args[6] == Py_None ? THPVariable_Wrap(*out) : Py_NewRef(in.args[6]);

@@ -67,7 +67,9 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
 
     Returns the result and the state [batch, taps - 1, channels] for the next call: the last inputs, oldest first.  `new_state`
     receives it if given (`state` itself may be). With `slots` (int32, one per sequence) the state is a cache of any number of
-    rows, updated in place: a sequence reads and writes the row it names, and one outside the cache is absent."""
+    rows, updated in place: a sequence reads and writes the row it names, and one outside the cache is absent.
+
+    `out` must not share memory with x: a token's inputs are those of the tokens before it too."""
     return (_module or module()).causal_conv(x, weight, bias, silu, state, new_state, lengths, slots, out)
 
 
@@ -80,7 +82,7 @@ def selective_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: tor
 
     z is the gate; D, delta_bias [channels] and A are fp32, everything else but the states is of u's type.  Returns the result and the
     states [batch, channels, states] (fp32) for the next call; `state`, `new_state`, `slots` as for `causal_conv`.  One token or many: a
-    call of length 1 is the step of a generation."""
+    call of length 1 is the step of a generation.  `out` may be u, delta or z itself, and must not share memory with an input otherwise."""
     return (_module or module()).selective_scan(u, delta, A, B, C, D, z, delta_bias, softplus, state, new_state, lengths, slots, out)
 
 

@@ -124,3 +124,69 @@ def test_views_whose_numbers_are_to_be_negated_are_refused():
     assert torch.equal(y, want)
     with pytest.raises(seq.XlError, match="negated"):
         seq.quantize_rows(x[..., 0][:, :1])
+
+
+F8 = torch.float8_e4m3fn
+
+
+def refused(call, what):
+    with pytest.raises(seq.XlError, match=f"shares memory with {what}"):
+        call()
+
+
+def test_results_that_share_memory_with_what_is_still_to_be_read_are_refused():
+    wide = torch.randn(2, 40, 96, device="cuda")
+    x, w = wide[:, :, :32], torch.randn(32, 4, device="cuda")
+    before = wide.clone()
+    refused(lambda: seq.causal_conv(x, w, out=x), "x")
+    refused(lambda: seq.causal_conv(x, w, out=wide[:, :, 31:63]), "x")
+    refused(lambda: seq.causal_conv(x[:, 1:], w, out=x[:, :-1]), "x")
+    refused(lambda: seq.causal_conv(x[:1], w, out=wide.view(-1)[:40 * 32].view(1, 40, 32)), "x")
+    states = torch.randn(1000, device="cuda")
+    refused(lambda: seq.causal_conv(x, w, state=states[:192].view(2, 3, 32), new_state=states[96:288].view(2, 3, 32)), "state")
+    refused(lambda: seq.causal_conv(x, w, new_state=wide.view(-1)[:192].view(2, 3, 32)), "x")
+    refused(lambda: seq.causal_conv(x, w, out=wide[:, :, 32:64], new_state=wide.view(-1)[96 * 10 + 32:96 * 10 + 32 + 192].view(2, 3, 32)), "new_state")
+    refused(lambda: seq.causal_conv(x[:1, :30], states[:128].view(32, 4), out=states[:960].view(1, 30, 32)), "weight")
+
+    A, state = -torch.rand(32, 32, device="cuda"), torch.randn(3, 32, 32, device="cuda")
+    u, B, C = (torch.randn(2, 40, 32, device="cuda") for _ in range(3))
+    refused(lambda: seq.selective_scan(u, u, A, B, C, out=B), "B")
+    refused(lambda: seq.selective_scan(u, u, A, B, C, out=C), "C")
+    refused(lambda: seq.selective_scan(x, u, A, B, C, out=wide[:, :, 16:48]), "u")
+    refused(lambda: seq.selective_scan(u, x, A, B, C, out=wide[:, :, 16:48]), "delta")
+    refused(lambda: seq.selective_scan(u, u, A, B, C, z=x, out=wide[:, :, 16:48]), "z")
+    refused(lambda: seq.selective_scan(u, u, A, B, C, new_state=B.view(-1)[:2048].view(2, 32, 32)), "B")
+    refused(lambda: seq.selective_scan(u, u, A, B, C, state=state[:2], new_state=state[1:]), "state")
+
+    memory = torch.randn(40, 48, device="cuda")
+    refused(lambda: seq.quantize_rows(memory, out=memory.view(torch.uint8).view(-1)[:40 * 48].view(40, 48).view(F8)), "x")
+    refused(lambda: seq.quantize_rows(memory, scales=memory[:, 5:6]), "x")
+    room = torch.zeros(40, 48, dtype=torch.uint8, device="cuda")
+    refused(lambda: seq.quantize_rows(memory[:, :40], out=room.view(F8)[:, :40], scales=room.view(torch.float32)[:, 10:11]), "scales")       # in the bytes behind a row
+    q, s = seq.quantize_rows(memory)
+    numbers = q.view(torch.uint8).view(torch.float32)
+    refused(lambda: seq.block_matmul(q, s, q[:12], s[:1], out=numbers), "a")
+    refused(lambda: seq.block_matmul(q[:20], s[:20], q[28:], s[:1], out=numbers[20:]), "b")
+    torch.cuda.synchronize()
+    assert torch.equal(wide, before)
+
+
+@pytest.mark.parametrize("length", [1, 2, 90, 2304])
+def test_results_may_lie_beside_the_inputs_and_in_their_place_as_a_whole(length):
+    g = torch.Generator("cuda").manual_seed(length)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    wide, w, A = r(2, length, 64), r(32, 4), -torch.rand(32, 8, generator=g, device="cuda")
+    B, C = r(2, length, 8), r(2, length, 8)
+    left, right = wide[:, :, :32], wide[:, :, 32:]
+    y, state = seq.causal_conv(left, w)
+    got, other = seq.causal_conv(left, w, out=right)
+    assert torch.equal(got, y) and torch.equal(other, state)
+    delta = right.clone() - 3
+    y, state = seq.selective_scan(left, delta, A, B, C)
+    got, other = seq.selective_scan(left, delta, A, B, C, out=delta)
+    assert got is delta and torch.equal(got, y) and torch.equal(other, state)
+    rows = left.reshape(-1, 32)
+    q, s = seq.quantize_rows(rows)
+    both = torch.zeros(2 * length, 96, dtype=torch.uint8, device="cuda").view(F8)
+    got, _ = seq.quantize_rows(rows, out=both[:, 32:64])
+    assert torch.equal(got.float(), q.float()) and not both.float()[:, :32].any() and not both.float()[:, 64:].any()
