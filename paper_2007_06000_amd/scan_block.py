@@ -105,6 +105,8 @@ class TokenStep:
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
         """x [batch, 1, width]; the result is overwritten by the next step."""
+        if x.shape != self.x.shape:
+            raise XlError(XL_E_SHAPE, f"token step: x has shape {tuple(x.shape)}, not {tuple(self.x.shape)}")
         self.x.copy_(x)
         self.graph.replay()
         torch.autograd.graph.increment_version(self.written)    # for whoever has saved one of them for a backward pass

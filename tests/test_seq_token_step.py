@@ -1,9 +1,10 @@
-"""CPU checks of the recorded step: which stream it is recorded on.  The device, its streams and the graph are stand-ins that keep books."""
+"""CPU checks of the recorded step: which stream it is recorded on, and which tokens it takes.  The device, its streams and the graph are stand-ins that keep books."""
 import contextlib
 
 import pytest
 import torch
 
+from paper_2007_06000_amd.binding import XlError
 from paper_2007_06000_amd.scan_block import TokenStep
 
 DEVICE = torch.device("meta")           # stands for a GPU that is not the current one
@@ -64,3 +65,22 @@ def test_a_step_is_recorded_on_a_stream_of_its_blocks_device(streams):
     TokenStep(block, 2)
     assert len(recordings) == 1 and recordings[0].device == DEVICE
     assert len(block.calls) == 2 and all(s.device == DEVICE for s in block.calls) and block.calls[1] is recordings[0]
+
+
+class Graph:
+    replays = 0
+
+    def replay(self):
+        Graph.replays += 1
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 8), (1, 8), (8,), (2, 2, 8), (2, 1, 1), (3, 1, 8), (2, 8)])
+def test_a_step_takes_one_token_for_each_row_and_nothing_else(streams, monkeypatch, shape):
+    monkeypatch.setattr(torch.cuda, "CUDAGraph", Graph)
+    step = TokenStep(Block(streams[0]), 2)
+    before = Graph.replays
+    with pytest.raises(XlError):
+        step(torch.zeros(shape, device=DEVICE))
+    assert Graph.replays == before
+    step(torch.zeros(2, 1, 8, device=DEVICE))
+    assert Graph.replays == before + 1
