@@ -18,9 +18,10 @@ import math
 from typing import Dict, Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import seq
-from .binding import XL_E_SHAPE, XlError
+from .binding import XL_E_SHAPE, XL_E_UNSUPPORTED, XlError
 
 State = Tuple[torch.Tensor, torch.Tensor]
 
@@ -107,6 +108,8 @@ class TokenStep:
         """x [batch, 1, width]; the result is overwritten by the next step."""
         if x.shape != self.x.shape:
             raise XlError(XL_E_SHAPE, f"token step: x has shape {tuple(x.shape)}, not {tuple(self.x.shape)}")
+        if (x.requires_grad and torch.is_grad_enabled()) or forward_ad.unpack_dual(x).tangent is not None:
+            raise XlError(XL_E_UNSUPPORTED, "token step: x asks for a gradient: inference only")
         self.x.copy_(x)
         self.graph.replay()
         torch.autograd.graph.increment_version(self.written)    # for whoever has saved one of them for a backward pass

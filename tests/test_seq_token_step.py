@@ -3,6 +3,7 @@ import contextlib
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2007_06000_amd.binding import XlError
 from paper_2007_06000_amd.scan_block import TokenStep
@@ -84,3 +85,16 @@ def test_a_step_takes_one_token_for_each_row_and_nothing_else(streams, monkeypat
     assert Graph.replays == before
     step(torch.zeros(2, 1, 8, device=DEVICE))
     assert Graph.replays == before + 1
+
+
+def test_a_step_refuses_tokens_that_ask_for_a_gradient(streams, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "CUDAGraph", Graph)
+    step = TokenStep(Block(streams[0]), 2)
+    x = torch.zeros(2, 1, 8, device=DEVICE, requires_grad=True)
+    with pytest.raises(XlError):
+        step(x)
+    with torch.no_grad():
+        step(x)
+    with forward_ad.dual_level(), pytest.raises(XlError):
+        step(forward_ad.make_dual(x.detach(), torch.ones_like(x)))
+    assert not step.x.requires_grad
