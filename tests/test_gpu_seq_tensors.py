@@ -1,8 +1,12 @@
 """The sequence operators as calls among others: errors, versions and gradients of tensors, memory that results share."""
 import ctypes
+import os
+import subprocess
+import sysconfig
 
 import pytest
 import torch
+from torch.utils.cpp_extension import include_paths, library_paths
 
 from paper_2007_06000_amd import seq
 
@@ -190,3 +194,25 @@ def test_results_may_lie_beside_the_inputs_and_in_their_place_as_a_whole(length)
     both = torch.zeros(2 * length, 96, dtype=torch.uint8, device="cuda").view(F8)
     got, _ = seq.quantize_rows(rows, out=both[:, 32:64])
     assert torch.equal(got.float(), q.float()) and not both.float()[:, :32].any() and not both.float()[:, 64:].any()
+
+
+def test_results_come_from_the_devices_allocator_wherever_the_inputs_came_from(tmp_path):
+    lib = os.path.join(tmp_path, "foreign.so")
+    system = [*include_paths(), sysconfig.get_path("include"), "/opt/rocm/include"]
+    subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", *[f for p in system for f in ("-isystem", p)], "-shared", "-o", lib,
+                    os.path.join(os.path.dirname(os.path.abspath(__file__)), "native", "foreign_allocator.cpp"), *["-L" + p for p in library_paths()],
+                    "-ltorch_python", "-ltorch_cpu", "-lc10"], check=True, capture_output=True, text=True)
+    foreign = ctypes.PyDLL(lib)
+    foreign.foreign_float_tensor.restype, foreign.foreign_float_tensor.argtypes = ctypes.py_object, [ctypes.c_longlong, ctypes.c_longlong]
+    foreign.foreign_calls.restype = ctypes.c_longlong
+    x = foreign.foreign_float_tensor(40, 100)
+    made = foreign.foreign_calls()
+    assert made == 1
+    x.copy_(torch.randn(40, 100))
+    w, B, A = torch.randn(100, 4, device="cuda"), torch.randn(1, 40, 4, device="cuda"), -torch.rand(100, 4, device="cuda")
+    y, state = seq.causal_conv(x[None], w)
+    _, scan_state = seq.selective_scan(x[None], x[None], A, B, B)
+    q, s = seq.quantize_rows(x)
+    assert foreign.foreign_calls() == made and y.device == state.device == q.device == s.device == x.device
+    want = x.clone()
+    assert torch.equal(y, seq.causal_conv(want[None], w)[0]) and torch.equal(q.float(), seq.quantize_rows(want)[0].float()) and scan_state.shape == (1, 100, 4)
