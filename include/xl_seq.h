@@ -11,7 +11,7 @@
  *   xl_block_matmul      product of two such operands
  *
  * Every call takes one struct of 64-bit numbers and DEVICE pointers, enqueues one kernel (a large
- * product and a scan with a workspace two) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
+ * product and a scan with a workspace two, sizes that take 2^32 threads and more several) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
  * nothing and keeps nothing between calls.  Calls never throw or abort.  The current HIP device must be a gfx950 (XL_E_DEVICE) that can reach the
  * pointers.  Inference only: there are no gradients.
  *

@@ -37,6 +37,7 @@ static xl_status check_device()
 
 static xl_status launched(hipError_t e)
 {
+    if (e == hipErrorInvalidConfiguration) return fail(XL_E_SHAPE, "the sizes take a larger launch than the device has");
     return e == hipSuccess ? XL_OK : fail(XL_E_LAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
 }
 
@@ -50,7 +51,7 @@ static bool product_fits(long long a, long long b, long long c, long long limit)
     long long p;
     return !__builtin_mul_overflow(a, b, &p) && !__builtin_mul_overflow(p, c, &p) && p <= limit;
 }
-static constexpr long long MAX_ITEMS = 1ll << 38;      // 2^30 workgroups of 256
+static constexpr long long MAX_ITEMS = 1ll << 38;      // numbers of an activation or a result: more than a device has memory for
 
 static xl_status check_sequences(const char *what, long long batch, long long length, long long channels, long long dtype, long long &nslots,
                                  const void *state, const void *new_state, const int *slots, const int *lengths)

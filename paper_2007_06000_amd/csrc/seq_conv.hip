@@ -82,14 +82,25 @@ __global__ __launch_bounds__(256) void conv_kernel(const xl_causal_conv_args a, 
     }
 }
 
+static xl_causal_conv_args piece_of(const xl_causal_conv_args &a, long long first, long long count)
+{
+    const int size = a.dtype == XL_F32 ? 4 : 2;
+    xl_causal_conv_args p = piece_of_states(a, first, count, (a.taps - 1) * a.channels, size);
+    p.x = behind(a.x, first * a.x_batch, size);
+    p.y = behind(a.y, first * a.y_batch, size);
+    return p;
+}
+
 template <int DT, int K, int V> static hipError_t launch(const xl_causal_conv_args &a, hipStream_t s)
 {
     const long long vecs = a.channels / V;
     // Runs of 32 tokens read an input 1.1 times (of 8, 16, 32 tokens: 42.7, 39.1, 38.7 us; 2047 channels 70, 56, 51); shorter ones where there would be fewer than 2048 threads a compute unit.
     long long run = 32;
     while (run > 4 && a.batch * vecs * ((a.length + run - 1) / run) < 256ll * 2048) run /= 2;
-    const long long runs = a.length > 0 ? (a.length + run - 1) / run : 1, blocks = (a.batch * vecs * runs + 255) / 256;
-    return launch_kernel(conv_kernel<DT, K, V>, dim3((unsigned)blocks), 256, s, a, (int)run, (int)runs);
+    const long long runs = a.length > 0 ? (a.length + run - 1) / run : 1;
+    return in_pieces(a, vecs * runs, piece_of, [&](const xl_causal_conv_args &p) {
+        return launch_kernel(conv_kernel<DT, K, V>, dim3((unsigned)((p.batch * vecs * runs + 255) / 256)), 256, s, p, (int)run, (int)runs);
+    });
 }
 
 template <int DT, int K> static hipError_t launch_taps(const xl_causal_conv_args &a, hipStream_t s)

@@ -20,6 +20,39 @@ template <typename... P> static hipError_t launch_kernel(void (*kernel)(P...), d
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), list, 0, s);
 }
 
+// A launch has fewer than 2^32 threads along x.  A batch that needs more goes in pieces of sequences, each of `threads` threads, rounded up to a workgroup's.
+static constexpr long long MAX_THREADS = (1ll << 32) - 1024;
+template <typename A, typename F> static hipError_t in_pieces(const A &a, long long threads, A (*piece_of)(const A &, long long, long long), F launch)
+{
+    if (threads > MAX_THREADS) return hipErrorInvalidConfiguration;         // one sequence by itself
+    const long long most = threads > 0 ? MAX_THREADS / threads : a.batch;
+    if (a.batch <= most) return launch(a);
+    for (long long b = 0; b < a.batch; b += most) {
+        const hipError_t e = launch(piece_of(a, b, a.batch - b < most ? a.batch - b : most));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+// `count` elements of `size` bytes behind p, or still nothing
+template <typename T> static T *behind(T *p, long long count, long long size)
+{
+    return p ? reinterpret_cast<T *>(reinterpret_cast<unsigned long long>(p) + (unsigned long long)(count * size)) : p;
+}
+// What all batches have: their own lengths and slots, or the next rows of the states.
+template <typename A> static A piece_of_states(A a, long long first, long long count, long long row, long long size)
+{
+    a.batch = count;
+    a.lengths = behind(a.lengths, first, sizeof(int));
+    if (a.slots) {
+        a.slots += first;
+    } else {
+        a.nslots -= first;
+        a.state = behind(a.state, first * row, size);
+        a.new_state = behind(a.new_state, first * row, size);
+    }
+    return a;
+}
+
 static constexpr float LOG2E = 1.44269504088896340736f;
 
 // Activations in memory <-> fp32.  Conversions to 16 bits round to nearest, ties to even.

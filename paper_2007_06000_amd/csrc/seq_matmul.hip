@@ -8,6 +8,7 @@
 //
 // Large products are bound by the matrix operations, the four multiply-adds behind each (16.8 ns for both, 15.9 without) and the loads' issue: 24642 x 4096 x 4096 in
 // bf16 takes 366 us, 2.26 PFLOP/s; the operations and multiply-adds alone would take 207.
+#include <algorithm>
 #include <type_traits>
 
 #include "seq_internal.h"
@@ -386,15 +387,38 @@ template <int DT, int BM, int BN, int WM, int WN, int KS, int S> static hipError
 
 static constexpr long long CUS = 256;
 
+// Rows from `i` and columns from `j` on, a multiple of 128.
+static xl_block_matmul_args part_of(const xl_block_matmul_args &a, long long i, long long m, long long j, long long n)
+{
+    const int size = a.dtype == XL_F32 ? 4 : 2;
+    xl_block_matmul_args p = a;
+    p.m = m;
+    p.n = n;
+    p.a = behind(a.a, i * a.a_row, 1);
+    p.a_scales = behind(a.a_scales, i * a.a_scale_row, 4);
+    p.b = behind(a.b, j * a.b_row, 1);
+    p.b_scales = behind(a.b_scales, j / XL_SCALE_BLOCK * a.b_scale_row, 4);
+    p.bias = behind(a.bias, j, 4);
+    p.y = behind(a.y, i * a.y_row + j, size);
+    return p;
+}
+
 template <int DT, int MT> static hipError_t launch_thin(const xl_block_matmul_args &a, hipStream_t s)
 {
-    const long long tiles_n = (a.n + 15) / 16, tiles = tiles_n * ((a.m + 16 * MT - 1) / (16 * MT));
-    return launch_kernel(thin_kernel<DT, MT>, dim3((unsigned)tiles), 512, s, a, (int)tiles_n);
+    // a launch has fewer than 2^32 threads, 512 for each tile: more go in pieces
+    const long long columns = std::min(a.n, 1ll << 26), tiles_n = (columns + 15) / 16, rows = std::min(a.m, MAX_THREADS / 512 / tiles_n * (16 * MT));
+    for (long long j = 0; j < a.n; j += columns)
+        for (long long i = 0; i < a.m; i += rows) {
+            const xl_block_matmul_args p = part_of(a, i, std::min(rows, a.m - i), j, std::min(columns, a.n - j));
+            const long long wide = (p.n + 15) / 16, tiles = wide * ((p.m + 16 * MT - 1) / (16 * MT));
+            const hipError_t e = launch_kernel(thin_kernel<DT, MT>, dim3((unsigned)tiles), 512, s, p, (int)wide);
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
 }
 
 template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, hipStream_t s)
 {
-    typedef typename Elem<DT>::T T;
     const long long blocks = (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK;
     // a tile of the tile kernel lies within 31 bits, and so do its scales
     const long long limit = 1ll << 22;
@@ -418,15 +442,8 @@ template <int DT> static hipError_t launch_type(const xl_block_matmul_args &a, h
         // round, they do, in a second launch (24642 x 4096 x 4096: 386 us in seven rounds, 366 so).
         const long long tn = (a.n + 255) / 256, rows = tiles(a.m, a.n, 256) / CUS * CUS / tn * 256;
         if (rows > 0 && rows < a.m && blocks >= 8 && tiles(a.m - rows, a.n, 128) <= CUS) {
-            xl_block_matmul_args part = a;
-            part.m = rows;
-            const hipError_t e = launch_tile<DT, 256, 256, 2, 4, 1, 2>(part, s);
-            if (e != hipSuccess) return e;
-            part.m = a.m - rows;
-            part.a = static_cast<const char *>(a.a) + rows * a.a_row;
-            part.a_scales = a.a_scales + rows * a.a_scale_row;
-            part.y = static_cast<T *>(a.y) + rows * a.y_row;
-            return launch_type<DT>(part, s);
+            const hipError_t e = launch_tile<DT, 256, 256, 2, 4, 1, 2>(part_of(a, 0, rows, 0, a.n), s);
+            return e != hipSuccess ? e : launch_type<DT>(part_of(a, rows, a.m - rows, 0, a.n), s);
         }
         return launch_tile<DT, 256, 256, 2, 4, 1, 2>(a, s);
     }

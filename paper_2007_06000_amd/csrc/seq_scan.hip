@@ -520,10 +520,23 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
     store_some<float, NS>(out + step + parts.factors(a.batch, D, N), live, p);
 }
 
+static xl_scan_args piece_of(const xl_scan_args &a, long long first, long long count)
+{
+    const int size = a.dtype == XL_F32 ? 4 : 2;
+    xl_scan_args p = piece_of_states(a, first, count, a.channels * a.states, 4);
+    p.u = behind(a.u, first * a.u_batch, size);
+    p.delta = behind(a.delta, first * a.delta_batch, size);
+    p.B = behind(a.B, first * a.b_batch, size);
+    p.C = behind(a.C, first * a.c_batch, size);
+    p.z = behind(a.z, first * a.z_batch, size);
+    p.y = behind(a.y, first * a.y_batch, size);
+    return p;
+}
+
 template <int DT, int LP> static hipError_t launch_step(const xl_scan_args &a, hipStream_t s)
 {
     const int per = 256 / LP, groups = (int)((a.channels + per - 1) / per);
-    return launch_kernel(step_kernel<DT, LP>, dim3((unsigned)(groups * a.batch)), 256, s, a, groups);
+    return in_pieces(a, groups * 256ll, piece_of, [&](const xl_scan_args &p) { return launch_kernel(step_kernel<DT, LP>, dim3((unsigned)(groups * p.batch)), 256, s, p, groups); });
 }
 
 template <int DT, int LP, int NS, int W, int TK, bool SPLIT, bool ROOT> static hipError_t launch_tile_as(const xl_scan_args &a, hipStream_t s, const Parts &parts)
@@ -543,15 +556,18 @@ template <int DT, int LP, int NS, int W, int TK, bool SPLIT, bool ROOT> static h
     };
     const bool buffers = rows(a.channels, {a.u_token, a.delta_token, a.y_token}) && (!a.z || rows(a.channels, {a.z_token})) && rows(a.states, {a.b_token, a.c_token});
     // 2 x 12321 x 2048 with 16 states in bf16: 258 us as vectors, 303 one by one, 560 scattered (these with four waves in every case)
-    const unsigned wide = (unsigned)(groups * a.batch);
-    if (!buffers) return launch_kernel(tile_kernel<DT, LP, NS, 4, TK, SCATTERED, ROOT>, dim3(wide), 64 * 4, s, a, groups, Parts{nullptr, 1, INT_MAX});
-    if constexpr (SPLIT) {
+    const Parts whole = {nullptr, 1, INT_MAX};
+    if (!buffers)
+        return in_pieces(a, groups * 64 * 4ll, piece_of, [&](const xl_scan_args &p) { return launch_kernel(tile_kernel<DT, LP, NS, 4, TK, SCATTERED, ROOT>, dim3((unsigned)(groups * p.batch)), 64 * 4, s, p, groups, whole); });
+    const auto tiles = vectors ? tile_kernel<DT, LP, NS, W, TK, VECTORS, ROOT> : tile_kernel<DT, LP, NS, W, TK, SINGLES, ROOT>;
+    if constexpr (SPLIT) {          // few workgroups
+        const unsigned wide = (unsigned)(groups * a.batch);
         const dim3 grid(wide, (unsigned)parts.count - 1);
         const hipError_t e = launch_kernel(vectors ? part_kernel<DT, LP, NS, W, TK, VECTORS> : part_kernel<DT, LP, NS, W, TK, SINGLES>, grid, 64 * W, s, a, groups, parts);
-        if (e != hipSuccess) return e;
+        return e != hipSuccess ? e : launch_kernel(tiles, dim3(wide, (unsigned)parts.count), 64 * W, s, a, groups, parts);
+    } else {
+        return in_pieces(a, groups * 64ll * W, piece_of, [&](const xl_scan_args &p) { return launch_kernel(tiles, dim3((unsigned)(groups * p.batch)), 64 * W, s, p, groups, whole); });
     }
-    const dim3 grid(wide, (unsigned)parts.count);
-    return launch_kernel(vectors ? tile_kernel<DT, LP, NS, W, TK, VECTORS, ROOT> : tile_kernel<DT, LP, NS, W, TK, SINGLES, ROOT>, grid, 64 * W, s, a, groups, parts);
 }
 
 template <int DT, int LP, int NS, int W, int TK, bool SPLIT = false> static hipError_t launch_tile(const xl_scan_args &a, hipStream_t s, const Parts &parts = {nullptr, 1, INT_MAX})
