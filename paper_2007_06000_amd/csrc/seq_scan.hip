@@ -169,6 +169,7 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     constexpr int PER = CH * TK / 64, VE = ACCESS != VECTORS ? 1 : PER < 4 ? PER : 4, IT = PER / VE;    // a thread's part of a tile's u, delta, z and y
     constexpr int PERB = NP * TK / 64, VB = ACCESS != VECTORS ? 1 : PERB < 4 ? PERB : 4, IB = PERB / VB; // and of its B and C
     static_assert(PER >= 1 && PERB >= 1 && TK % LP == 0, "a wave's tokens divide among its lanes");
+    constexpr int ACROSS = NP > 64 * VB ? NP / (64 * VB) : 1;   // a lane's items in a row of B and C, 64 VB apart: more than one where a row has more items than there are lanes
     __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT];    // steps, and step x input (later the outputs): [channel][token]
     __shared__ float Bs_all[W][TK * NP], Cs_all[W][TK * NP];    // [token][state]
     __shared__ Vec<float, NS> Ps[3][W * 64], Es[3][W * 64];
@@ -207,8 +208,9 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
     }
     // this lane's numbers of its wave's tokens: VE channels of IT tokens
     const int ec = lane % (CH / VE) * VE, et = lane / (CH / VE), nc = min(D - c0 - ec, VE), tw = wave * TK;
-    const int bn = lane % (NP / VB) * VB, bt = lane / (NP / VB), nb = min(N - bn, VB);
-    constexpr int ET = 64 * VE / CH, BT = 64 * VB / NP;         // tokens between a lane's items
+    const int bn = lane % (NP / VB) * VB, bt = lane / (NP / VB), nb = N - bn;
+    constexpr int ET = 64 * VE / CH, BT = 64 * VB * ACROSS / NP;        // tokens between a lane's items (its rows of items)
+    static_assert(BT >= 1 && BT * (IB / ACROSS) == TK, "the items cover the tile");
     float bias[VE], skip[VE];
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
@@ -242,8 +244,9 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             }
 #pragma unroll
             for (int k = 0; k < IB; ++k) {
-                Br[k] = Brows.template load<Vec<T, VB>>(b_at + k * BT * b_row, t0 * b_row);
-                Cr[k] = Crows.template load<Vec<T, VB>>(c_at + k * BT * c_row, t0 * c_row);
+                const unsigned side = k % ACROSS * 64 * VB * S;      // past the end of the row: nowhere
+                Br[k] = Brows.template load<Vec<T, VB>>(side && k % ACROSS * 64 * VB >= nb ? NOWHERE : b_at + k / ACROSS * BT * b_row + side, t0 * b_row);
+                Cr[k] = Crows.template load<Vec<T, VB>>(side && k % ACROSS * 64 * VB >= nb ? NOWHERE : c_at + k / ACROSS * BT * c_row + side, t0 * c_row);
             }
         } else {
 #pragma unroll
@@ -256,10 +259,10 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
             }
 #pragma unroll
             for (int k = 0; k < IB; ++k) {
-                const long long t = t0 + tw + bt + k * BT;
-                const int n = t < len ? nb : 0;
-                Br[k] = load_some<T, VB>(Bp + t * a.b_token + bn, n);
-                Cr[k] = load_some<T, VB>(Cp + t * a.c_token + bn, n);
+                const long long t = t0 + tw + bt + k / ACROSS * BT;
+                const int side = k % ACROSS * 64 * VB, n = t < len ? nb - side : 0;
+                Br[k] = load_some<T, VB>(Bp + t * a.b_token + bn + side, n);
+                Cr[k] = load_some<T, VB>(Cp + t * a.c_token + bn + side, n);
             }
         }
     };
@@ -301,8 +304,8 @@ __global__ __launch_bounds__(64 * W) void tile_kernel(const xl_scan_args a, int 
                 vb[i] = (float)Br[k][i];
                 vc[i] = (float)Cr[k][i];
             }
-            *reinterpret_cast<Vec<float, VB> *>(&Bs[(bt + k * BT) * NP + bn]) = vb;
-            *reinterpret_cast<Vec<float, VB> *>(&Cs[(bt + k * BT) * NP + bn]) = vc;
+            *reinterpret_cast<Vec<float, VB> *>(&Bs[(bt + k / ACROSS * BT) * NP + bn + k % ACROSS * 64 * VB]) = vb;
+            *reinterpret_cast<Vec<float, VB> *>(&Cs[(bt + k / ACROSS * BT) * NP + bn + k % ACROSS * 64 * VB]) = vc;
         }
         if (t0 + TT < len) fetch(t0 + TT);                      // the next tile's numbers come in the meantime
         wave_sync();
@@ -410,6 +413,7 @@ __global__ __launch_bounds__(64 * W) void part_kernel(const xl_scan_args a, int 
     constexpr int CH = 64 / LP, NP = LP * NS, PT = TK + 4;
     constexpr int PER = CH * TK / 64, VE = ACCESS != VECTORS ? 1 : PER < 4 ? PER : 4, IT = PER / VE;
     constexpr int PERB = NP * TK / 64, VB = ACCESS != VECTORS ? 1 : PERB < 4 ? PERB : 4, IB = PERB / VB;
+    static_assert(NP <= 64 * VB, "a row of B has no more items than there are lanes");
     __shared__ float dl_all[W][CH * PT], sx_all[W][CH * PT], Bs_all[W][TK * NP];
     __shared__ Vec<float, NS> Es[W * 64];
     __shared__ float totals[W * 64];
