@@ -1,0 +1,223 @@
+"""Every kernel that the sequence operators' rules on sizes can choose, against the definitions: sizes that reach it at little cost.
+
+A scan's tile kernel is <lanes a channel, states a lane, waves>; large results are compared in samples, at steps that go through all lanes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import seq as ref
+from paper_2007_06000_amd import seq
+from test_gpu_seq_conv import HALF, f64
+from test_gpu_seq_conv import check as check_conv
+from test_gpu_seq_conv import inputs as conv_inputs
+from test_gpu_seq_matmul import F8, operands
+from test_gpu_seq_matmul import check as check_product
+from test_gpu_seq_scan import check, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def sample(n, about, least=1):
+    """Some `about` of n, in steps of an odd number, and the last 40."""
+    step = max(least, n // about) | 1
+    return torch.unique(torch.cat([torch.arange(0, n, step), torch.arange(max(0, n - 40), n)])).cuda()
+
+
+def check_channels(p, y, new, what, **more):
+    at = sample(p["u"].shape[2], 150)
+    some = {k: v[:, :, at] if k in ("u", "delta", "z") else v[at] if k in ("A", "D", "delta_bias") else v[:, at] if k == "state" else v for k, v in p.items()}
+    check(some, y[:, :, at], new[:, at], what, **more)
+    assert torch.isfinite(y).all() and torch.isfinite(new).all(), what
+
+
+SCANS = [  # batch, length, channels, states
+    (1, 70, 4000, 3),       # <4,1,8>
+    (2, 60, 5000, 4),       # <4,1,4>
+    (1, 520, 17000, 2),     # <4,1,4>, many workgroups that stay long
+    (1, 30, 5001, 1),       # <4,1,2>
+    (2, 40, 17000, 4),      # <4,1,2>, many workgroups
+    (2, 50, 1000, 7),       # <8,1,4>
+    (1, 100, 4088, 8),      # <8,1,8>
+    (3, 40, 3000, 8),       # <4,2,4>
+    (1, 520, 17000, 5),     # <4,2,4>
+    (3, 30, 3000, 6),       # <4,2,2>
+    (1, 60, 1024, 16),      # <16,1,4>
+    (1, 400, 1000, 16),     # <16,1,8>
+    (1, 600, 1024, 16),     # <16,1,16>
+    (1, 700, 1001, 13),     # <16,1,16>
+    (1, 50, 1500, 13),      # <8,2,4>
+    (1, 100, 1504, 16),     # <8,2,8>
+    (5, 120, 333, 13),      # <8,2,8>
+    (1, 70, 4000, 16),      # <4,4,8>
+    (1, 300, 3999, 13),     # <4,4,8>
+    (1, 40, 4200, 16),      # <4,4,4>
+    (1, 520, 16500, 11),    # <4,4,4>
+    (1, 30, 4200, 12),      # <4,4,2>
+    (2, 30, 17000, 16),     # <4,4,2>
+    (1, 50, 1000, 30),      # <16,2,4>
+    (1, 100, 1000, 20),     # <16,2,8>
+    (1, 70, 1500, 32),      # <8,4,8>
+    (1, 40, 2100, 24),      # <8,4,4>
+    (1, 530, 8200, 17),     # <8,4,4>, many workgroups that stay long
+    (1, 30, 2100, 32),      # <8,4,2>
+    (2, 60, 5000, 17),      # <8,4,2>
+    (1, 80, 1000, 64),      # <16,4,8>
+    (1, 40, 1100, 50),      # <16,4,4>
+    (1, 30, 1100, 64),      # <16,4,2>
+    (2, 80, 2100, 40),      # <16,4,2>, many workgroups
+    (2, 40, 500, 128),      # <16,8,4>
+    (1, 90, 301, 100)]      # <16,8,4>
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("batch,length,channels,states", SCANS)
+def test_tiles_of_a_scan(batch, length, channels, states, dtype):
+    p = inputs(batch, length, channels, states, dtype, seed=states)
+    check_channels(p, *seq.selective_scan(**p), "all")
+    lengths = [length - 7 - 20 * b for b in range(batch)]
+    state = p["state"].clone()
+    q = {**p, "state": state, "u": p["u"].clone()}
+    for b, n in enumerate(lengths):
+        for k in ("delta", "B", "C", "z"):
+            q[k] = q[k].clone()
+            q[k][b, max(n, 0):] = float("nan")
+    y, new = seq.selective_scan(**q, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"), new_state=state, out=q["u"])
+    assert new is state and y is q["u"]
+    check_channels(p, y, new, "lengths, in place", lengths=lengths)
+    p["delta"], p["delta_bias"] = p["delta"].abs() * 0.1, p["delta_bias"].abs() * 0.1
+    check_channels(p, *seq.selective_scan(**p, softplus=False), "plain steps", softplus=False)
+
+
+@pytest.mark.parametrize("batch,length,channels,states", [s for s in SCANS if s[1] <= 100])
+def test_tiles_of_a_scan_whose_rows_lie_across_each_other(batch, length, channels, states):
+    """An input that every token shares, and another whose rows overlap: no buffers, 64-bit addresses."""
+    p = inputs(batch, length, channels, states, torch.bfloat16, seed=states)
+    p["u"] = p["u"][:, :1].expand(batch, length, channels)
+    memory = p["B"].reshape(-1)
+    p["B"] = memory.as_strided((batch, length, states), (length, 1, 1)) if batch * length + states <= memory.numel() else p["B"]
+    check_channels(p, *seq.selective_scan(**p), "all")
+    check_channels(p, *seq.selective_scan(**p, softplus=True, lengths=torch.full((batch,), length - 3, dtype=torch.int32, device="cuda")), "lengths", lengths=[length - 3] * batch)
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("states", [3, 6, 13, 24, 50, 100, 4, 8, 16, 32, 64, 128])           # 1, 2, 4, 8, 16, 32 lanes a channel
+@pytest.mark.parametrize("batch,length,channels", [(1, 1, 1), (3, 1, 100), (4, 3, 77), (2, 8, 2500), (1, 24, 17000)])
+def test_tokens_one_after_the_other(batch, length, channels, states, dtype):
+    p = inputs(batch, length, channels, states, dtype, seed=states)
+    check_channels(p, *seq.selective_scan(**p), "all")
+    bare = {k: p[k] for k in ("u", "delta", "A", "B", "C")}
+    check_channels(bare, *seq.selective_scan(**bare, softplus=True), "bare")
+    if batch == 1:
+        return
+    cache = torch.full((batch + 2, channels, states), 7.0, device="cuda")
+    slots, lengths = [batch + 1, -1, 0, 2][:batch], [length, length, 0, length - 1][:batch]
+    rows = [b for b in range(batch) if slots[b] >= 0]
+    cache[[slots[b] for b in rows]] = p["state"][rows]
+    y, new = seq.selective_scan(**{**p, "state": cache}, slots=torch.tensor(slots, dtype=torch.int32, device="cuda"), lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    assert new is cache and not y[1].any() and (cache[[r for r in range(batch + 2) if r not in slots]] == 7).all()
+    some = {k: v if k in ("A", "D", "delta_bias") else v[rows] for k, v in p.items()}
+    check_channels(some, y[rows], cache[[slots[b] for b in rows]], "cache", lengths=[lengths[b] for b in rows])
+
+
+@pytest.mark.parametrize("dtype,batch,length,channels,states", [(torch.bfloat16, 1, 1536, 128, 4), (torch.float32, 1, 1999, 60, 2), (torch.float16, 2, 1600, 96, 8), (torch.float32, 1, 1700, 50, 7),
+                                                                (torch.float32, 1, 2048, 256, 16), (torch.bfloat16, 1, 2100, 100, 32), (torch.float16, 1, 2048, 64, 50)])
+def test_parts_of_a_scan(dtype, batch, length, channels, states):
+    p = inputs(batch, length, channels, states, dtype, seed=states, step=(-5.0, 1.0))
+    check_channels(p, *seq.selective_scan(**p), "all")
+    p["delta"], p["delta_bias"] = p["delta"].abs() * 0.01, p["delta_bias"].abs() * 0.01
+    check_channels(p, *seq.selective_scan(**p, softplus=False), "plain steps", softplus=False)
+
+
+# runs of 8, 16, 32 and 32 tokens (2 bytes), of 32, 16 and 8 (4 bytes); pairs of channels or single ones
+@pytest.mark.parametrize("batch,length,channels,taps,dtype", [
+    (2, 2101, 2048, 4, torch.bfloat16), (3, 1000, 4095, 3, torch.float16), (8, 3025, 2048, 4, torch.bfloat16), (6, 1003, 2731, 2, torch.bfloat16),
+    (5, 1003, 3300, 4, torch.float32), (3, 1000, 4095, 2, torch.float32), (4, 600, 2048, 3, torch.float32)])
+def test_long_runs_of_a_convolution(batch, length, channels, taps, dtype):
+    _, w, bias, state = conv_inputs(batch, 1, channels, taps, dtype)
+    wide = torch.randn(batch, length, 2 * channels, device="cuda").to(dtype)
+    x, at = wide[:, :, channels:], sample(channels, 40)
+
+    def compare(y, new, old, lengths, what):
+        check_conv(x[:, :, at].nan_to_num(), w[at], bias[at], old[:, :, at], lengths, True, y[:, :, at], new[:, :, at], what)
+        assert torch.isfinite(y).all(), what
+
+    y, new = seq.causal_conv(x, w, bias, state=state)
+    compare(y, new, state, None, "all")
+    lengths = [(length - 1) * b // max(1, batch - 1) for b in range(batch)]         # none to all but one: inside runs
+    for b, n in enumerate(lengths):
+        x[b, n:] = float("nan")
+    old = state.clone()
+    y, new = seq.causal_conv(x, w, bias, state=state, new_state=state, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    assert new is state
+    compare(y, new, old, lengths, "lengths, in place")
+    for b, n in enumerate(lengths):
+        assert not y[b, n:].any()
+
+
+def bytes_of(q):
+    return q.contiguous().view(torch.uint8).cpu().numpy()
+
+
+@pytest.mark.parametrize("quantize,rows,k", [
+    (seq.quantize_rows, 65535 * 16 + 37, 96), (seq.quantize_rows, 65535 * 8 + 9, 200), (seq.quantize_rows, 65535 * 4 + 5, 300), (seq.quantize_weight, 65535 * 128 + 130, 8)])
+def test_a_quantiser_of_more_groups_of_rows_than_a_grid_is_wide(quantize, rows, k):
+    g = torch.Generator("cuda").manual_seed(k)
+    x = (torch.randn(rows, k, generator=g, device="cuda") * torch.exp(torch.randn(rows, 1, generator=g, device="cuda"))).bfloat16()
+    q, s = quantize(x)
+    block = 1 if quantize is seq.quantize_rows else 128
+    for first in (0, rows // 2 // 128 * 128, 65535 * (rows // 65535) - 128, 65535 * (rows // 65535), rows - (rows - 1) % 128 - 1):
+        first = first // block * block
+        part = x[first:first + 256]
+        want, scales = ref.quantize(part.float().cpu().numpy(), block)
+        assert np.array_equal(s[first // block:first // block + len(scales)].cpu().numpy(), scales), first
+        assert np.array_equal(bytes_of(q[first:first + 256]), bytes_of(torch.from_numpy(want).to(F8))), first
+    for first in range(0, rows, 1 << 17):           # the rest as in smaller calls
+        some, scales = quantize(x[first:first + (1 << 17)])
+        assert torch.equal(some.view(torch.uint8), q[first:first + (1 << 17)].contiguous().view(torch.uint8)) if k % 16 == 0 else torch.equal(some.float(), q[first:first + (1 << 17)].float())
+        assert torch.equal(scales, s[first // block:first // block + len(scales)])
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+def test_quantised_numbers_keep_their_signs(dtype):
+    """Bit for bit, zeros of either sign among them: what is too small for eight bits, and zeros."""
+    x = torch.randn(64, 400, generator=torch.Generator().manual_seed(1)) * torch.exp(4 * torch.randn(64, 400, generator=torch.Generator().manual_seed(2)))
+    x[::5, ::7], x[1::5, ::7] = 0.0, -0.0
+    x = x.clamp(-6e4, 6e4).to(dtype)
+    for f, block in ((seq.quantize_rows, 1), (seq.quantize_weight, 128)):
+        q, s = f(x.cuda())
+        want, scales = ref.quantize(x.float().numpy(), block)
+        got, want = bytes_of(q), bytes_of(torch.from_numpy(want).to(F8))
+        assert (got == 0x80).any() and (got == 0).any() and np.array_equal(got, want) and np.array_equal(s.cpu().numpy(), scales), f.__name__
+
+
+PRODUCTS = [  # m, n, k; in 16 bits, in 32
+    (1500, 1100, 520),      # tiles of 64 in two stages
+    (1400, 1399, 128),
+    (2048, 2000, 1000),     # tiles of 128 in four stages
+    (1990, 2047, 200),
+    (2500, 2500, 384),      # tiles of 128 in two stages; of four waves
+    (3000, 3000, 1030),     # tiles of 256; of 128 and four waves
+    (4200, 4096, 1024),     # tiles of 256 for 4096 rows and smaller ones for the rest
+    (4400, 4095, 1150)]
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+def test_tiles_of_a_product(m, n, k, dtype):
+    a, sa, b, sb, bias = operands(m, n, k, seed=m)
+    wa = torch.full((m, (k + 15) // 16 * 16 + 48), float("nan"), device="cuda").to(F8)          # numbers behind the rows, and rows further apart
+    wa[:, :k] = a
+    room = torch.full((m, n + 24), 7.0, dtype=dtype, device="cuda")
+    rows = torch.unique(torch.cat([sample(m, 60), torch.arange(max(0, min(4096, m) - 8), min(4104, m)).cuda()]))
+    blocks = sorted({0, n // 256, (n - 1) // 128})
+
+    def compare(y, bias, what):
+        check_product(a.view(torch.uint8)[rows].view(F8), sa[rows], b, sb, bias, y[rows], f"{what}: rows")
+        for j in blocks:
+            at = slice(128 * j, min(n, 128 * (j + 1)))
+            check_product(a, sa, b[at], sb[j:j + 1], None if bias is None else bias[at], y[:, at], f"{what}: columns of block {j}")
+
+    compare(seq.block_matmul(a, sa, b, sb, bias=bias, dtype=dtype), bias, "bias")
+    y = seq.block_matmul(wa[:, :k], sa.contiguous(), b, sb.t().contiguous().t(), out=room[:, 8:8 + n])
+    compare(y, None, "wider, scales by rows")
+    assert (room[:, :8] == 7).all() and (room[:, 8 + n:] == 7).all()
