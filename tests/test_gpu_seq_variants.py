@@ -221,3 +221,45 @@ def test_tiles_of_a_product(m, n, k, dtype):
     y = seq.block_matmul(wa[:, :k], sa.contiguous(), b, sb.t().contiguous().t(), out=room[:, 8:8 + n])
     compare(y, None, "wider, scales by rows")
     assert (room[:, :8] == 7).all() and (room[:, 8 + n:] == 7).all()
+
+
+def laid_out(p, how):
+    """The same numbers where rows are read as vectors (as they are), one number at a time (from odd places of wider rows), or through addresses (the first token's u for all)."""
+    if how == "single":
+        for k in ("u", "B", "C"):
+            wide = torch.full((*p[k].shape[:2], p[k].shape[2] + 3), float("nan"), dtype=p[k].dtype, device="cuda")
+            wide[:, :, 1:-2] = p[k]
+            p[k] = wide[:, :, 1:-2]
+    elif how == "across":
+        p["u"] = p["u"][:, :1].expand(p["u"].shape)
+    return p
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("how", ["vectors", "single", "across"])
+@pytest.mark.parametrize("batch,length,channels,states", sorted({(b, n, -(-c // 4) * 4, -(-s // 4) * 4) for b, n, c, s in SCANS}))
+def test_tiles_of_a_scan_in_every_way_of_reading(batch, length, channels, states, how, dtype):
+    p = laid_out(inputs(batch, length, channels, states, dtype, seed=states), how)
+    check_channels(p, *seq.selective_scan(**p), "softplus")
+    p["delta"], p["delta_bias"] = p["delta"].abs() * 0.1, p["delta_bias"].abs() * 0.1
+    check_channels(p, *seq.selective_scan(**p, softplus=False), "plain steps", softplus=False)
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("how", ["vectors", "single"])
+@pytest.mark.parametrize("channels,states", [(60, 4), (80, 8), (60, 16), (40, 32), (24, 64)])
+def test_parts_of_a_scan_in_every_way_of_reading(channels, states, how, dtype):
+    p = laid_out(inputs(1, 2050, channels, states, dtype, seed=states, step=(-5.0, 1.0)), how)
+    check_channels(p, *seq.selective_scan(**p), "softplus")
+    p["delta"], p["delta_bias"] = p["delta"].abs() * 0.01, p["delta_bias"].abs() * 0.01
+    check_channels(p, *seq.selective_scan(**p, softplus=False), "plain steps", softplus=False)
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("taps", [2, 3, 4])
+@pytest.mark.parametrize("channels", [37, 38])
+def test_all_taps_of_a_convolution(channels, taps, dtype):
+    x, w, bias, state = conv_inputs(3, 50, channels, taps, dtype, seed=taps)
+    lengths = torch.tensor([50, 0, 23], dtype=torch.int32, device="cuda")
+    y, new = seq.causal_conv(x, w, bias, state=state, lengths=lengths)
+    check_conv(x, w, bias, state, [50, 0, 23], True, y, new, "lengths")
