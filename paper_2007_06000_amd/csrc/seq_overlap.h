@@ -81,4 +81,12 @@ inline bool overlap(const Span &a_, const Span &b_)
     return false;
 }
 
+// True where two rows of one tensor share a byte.
+inline bool overlaps_itself(const Span &s)
+{
+    if (s.batch <= 0 || s.length <= 0 || s.width <= 0) return false;
+    return (s.length > 1 && s.token_step < s.width) ||
+           (s.batch > 1 && overlap_detail::meets(0, s.batch_step, 1, s.batch - 1, s.token_step, 1 - s.length, s.length - 1, -s.width, s.width));
+}
+
 }  // namespace xls

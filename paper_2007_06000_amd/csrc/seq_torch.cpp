@@ -132,9 +132,10 @@ struct Op {
         return static_cast<T *>(dense(what, t, type, shape));
     }
 
-    // A tensor of the caller's that the call writes, apart from what it reads and writes otherwise.
+    // A tensor of the caller's that the call writes: every number in a place of its own, apart from what the call reads and writes otherwise.
     void apart(const char *what, const xls::Span &written, std::initializer_list<Named> others) const
     {
+        if (xls::overlaps_itself(written)) refuse(XL_E_SHAPE, name, ": rows of ", what, " share memory with each other");
         for (const Named &o : others)
             if (xls::overlap(written, o.span)) refuse(XL_E_SHAPE, name, ": ", what, " shares memory with ", o.what);
     }

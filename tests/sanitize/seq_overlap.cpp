@@ -24,6 +24,16 @@ static bool by_bytes(const Span &a, const Span &b)
     return false;
 }
 
+static bool twice(const Span &s)
+{
+    std::set<int64_t> bytes;
+    for (int64_t i = 0; i < s.batch; ++i)
+        for (int64_t j = 0; j < s.length; ++j)
+            for (int64_t k = 0; k < s.width; ++k)
+                if (!bytes.insert(s.at + i * s.batch_step + j * s.token_step + k).second) return true;
+    return false;
+}
+
 int main()
 {
     std::mt19937_64 rng(1);
@@ -35,6 +45,7 @@ int main()
         if (draw(3) == 0) s[1].batch_step = s[0].batch_step, s[1].token_step = s[0].token_step;
         const bool want = by_bytes(s[0], s[1]);
         met += want;
+        CHECK(xls::overlaps_itself(s[0]) == twice(s[0]));
         if (overlap(s[0], s[1]) != want || overlap(s[1], s[0]) != want) {
             ++failures;
             for (const Span &p : s) fprintf(stderr, "%lld: %lld x %lld rows of %lld, steps %lld %lld\n", (long long)p.at, (long long)p.batch, (long long)p.length, (long long)p.width, (long long)p.batch_step, (long long)p.token_step);
@@ -48,6 +59,7 @@ int main()
     CHECK(!overlap(left, right) && overlap(left, left) && left == left && !(left == right));
     CHECK(overlap(left, Span{base + 4, B, L, 2 * C * L, 2 * C, C}) && overlap(right, Span{base + C - 1, B, L, 2 * C * L, 2 * C, C}));
     CHECK(overlap(left, Span{base + 2 * C * L * 3, B, L, 2 * C * L, 2 * C, C}) && !overlap(left, Span{base + 2 * C * L * B, B, L, 2 * C * L, 2 * C, C}));
+    CHECK(!overlaps_itself(left) && overlaps_itself(Span{base, B, L, 2 * C * (L - 1), 2 * C, C}) && !overlaps_itself(Span{base, B, L, C, 2 * C * B, C}) && overlaps_itself(Span{base, B, L, 0, C, C}));
     const Span outermost = {base, B, L, 2 * C, 2 * C * B, C};
     CHECK(!overlap(outermost, Span{base + C, B, L, 2 * C, 2 * C * B, C}) && overlap(outermost, Span{base + C - 1, B, L, 2 * C, 2 * C * B, C}));
     /* memory without gaps against rows with gaps */

@@ -216,3 +216,18 @@ def test_results_come_from_the_devices_allocator_wherever_the_inputs_came_from(t
     assert foreign.foreign_calls() == made and y.device == state.device == q.device == s.device == x.device
     want = x.clone()
     assert torch.equal(y, seq.causal_conv(want[None], w)[0]) and torch.equal(q.float(), seq.quantize_rows(want)[0].float()) and scan_state.shape == (1, 100, 4)
+
+
+def test_results_whose_rows_share_memory_are_refused():
+    x, w, memory = torch.randn(3, 5, 16, device="cuda"), torch.randn(16, 4, device="cuda"), torch.zeros(4000, device="cuda")
+    B, A = torch.randn(3, 5, 4, device="cuda"), -torch.rand(16, 4, device="cuda")
+    for steps in ((16, 16, 1), (64, 16, 1), (40, 20, 1), (16, 40, 1)):
+        out = memory.as_strided((3, 5, 16), steps)
+        for call in (lambda: seq.causal_conv(x, w, out=out), lambda: seq.selective_scan(x, x, A, B, B, out=out)):
+            with pytest.raises(seq.XlError, match="share memory with each other"):
+                call()
+    y, _ = seq.causal_conv(x, w)
+    for steps in ((80, 16, 1), (100, 20, 1), (16, 48, 1), (20, 90, 1)):         # sequences outermost or tokens, with gaps or without
+        assert torch.equal(seq.causal_conv(x, w, out=memory.as_strided((3, 5, 16), steps))[0], y)
+    with pytest.raises(seq.XlError, match="share memory with each other"):
+        seq.quantize_rows(x[0], scales=memory[:1].expand(5, 1))
