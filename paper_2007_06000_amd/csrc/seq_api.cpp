@@ -35,10 +35,10 @@ static xl_status check_device()
     return k == 1 ? XL_OK : fail(XL_E_DEVICE, "device %d is not a gfx950 GPU", dev);
 }
 
-static xl_status launched(hipError_t e)
+static xl_status launched(const char *what, hipError_t e)
 {
-    if (e == hipErrorInvalidConfiguration) return fail(XL_E_SHAPE, "the sizes take a larger launch than the device has");
-    return e == hipSuccess ? XL_OK : fail(XL_E_LAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+    if (e == hipErrorInvalidConfiguration) return fail(XL_E_SHAPE, "%s: the sizes take a larger launch than the device has", what);
+    return e == hipSuccess ? XL_OK : fail(XL_E_LAUNCH, "%s: kernel launch failed: %s", what, hipGetErrorString(e));
 }
 
 static int size_of(long long dtype) { return dtype == XL_F32 ? 4 : dtype == XL_F16 || dtype == XL_BF16 ? 2 : 0; }
@@ -103,7 +103,7 @@ xl_status xl_causal_conv(const xl_causal_conv_args *args, void *stream)
         return fail(XL_E_ALIGN, "%s: a filter, bias or state is not aligned to its elements", w);
     if (a.length == 0 && !a.new_state) return XL_OK;
     if ((st = check_device()) != XL_OK) return st;
-    return launched(xls::launch_causal_conv(a, static_cast<hipStream_t>(stream)));
+    return launched(w, xls::launch_causal_conv(a, static_cast<hipStream_t>(stream)));
 }
 
 xl_status xl_selective_scan(const xl_scan_args *args, void *stream)
@@ -129,7 +129,7 @@ xl_status xl_selective_scan(const xl_scan_args *args, void *stream)
     if (!aligned(a.workspace, 16)) return fail(XL_E_ALIGN, "%s: the workspace is not aligned to 16 bytes", w);
     if (a.length == 0 && !a.new_state) return XL_OK;
     if ((st = check_device()) != XL_OK) return st;
-    return launched(xls::launch_selective_scan(a, static_cast<hipStream_t>(stream)));
+    return launched(w, xls::launch_selective_scan(a, static_cast<hipStream_t>(stream)));
 }
 
 long long xl_selective_scan_workspace(const xl_scan_args *args)
@@ -157,7 +157,7 @@ xl_status xl_quantize_blocks(const xl_quantize_args *args, void *stream)
         return fail(XL_E_SHAPE, "%s: steps %lld (x), %lld (q), %lld, %lld (scales) do not fit rows of %lld", w, a.x_row, a.q_row, a.scale_row, a.scale_block, a.k);
     const xl_status st = check_device();
     if (st != XL_OK) return st;
-    return launched(xls::launch_quantize(a, static_cast<hipStream_t>(stream)));
+    return launched(w, xls::launch_quantize(a, static_cast<hipStream_t>(stream)));
 }
 
 xl_status xl_block_matmul(const xl_block_matmul_args *args, void *stream)
@@ -179,7 +179,7 @@ xl_status xl_block_matmul(const xl_block_matmul_args *args, void *stream)
         return fail(XL_E_SHAPE, "%s: steps %lld (a), %lld (b), %lld (y) do not fit %lld x %lld x %lld", w, a.a_row, a.b_row, a.y_row, a.m, a.n, a.k);
     const xl_status st = check_device();
     if (st != XL_OK) return st;
-    return launched(xls::launch_block_matmul(a, static_cast<hipStream_t>(stream)));
+    return launched(w, xls::launch_block_matmul(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
