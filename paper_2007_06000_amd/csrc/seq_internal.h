@@ -110,7 +110,7 @@ __device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * LOG2E)
 __device__ __forceinline__ float silu(float v) { return v * __builtin_amdgcn_rcpf(1.f + exp_fast(-v)); }
 
 // log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|) in (0, 1].  log(1 + e) = 2 artanh(r), r = e / (2 + e) <= 1/3, with artanh(r) / r a polynomial in
-// r^2 fitted to within 4e-9.  (The hardware logarithm of 1 + e would lose the digits of a small e, and small steps are the usual
+// r^2 fitted to within 8e-9.  (The hardware logarithm of 1 + e would lose the digits of a small e, and small steps are the usual
 // ones.)  NaN and infinities come through.
 __device__ __forceinline__ float softplus(float x)
 {

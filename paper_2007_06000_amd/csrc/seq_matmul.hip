@@ -7,7 +7,7 @@
 // y, and share one scale of a (the lane's column) and one of b (its 16 rows lie in one block of 128).
 //
 // Large products are bound by the matrix operations, the four multiply-adds behind each (16.8 ns for both, 15.9 without) and the loads' issue: 24642 x 4096 x 4096 in
-// bf16 takes 366 us, 2.26 PFLOP/s; the operations and multiply-adds alone would take 207.
+// bf16 takes 368 us, 2.25 PFLOP/s; the operations and multiply-adds alone would take 207.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,9 +25,11 @@ union Part {
     i32x8 v;
 };
 
-// The sum of one block.  The 8-bit operation adds its 128 products with fewer bits than fp32 has: measured on normal numbers its result
-// is 1.3e-5 off (at most 9e-6 of the sum of the products' magnitudes), which a result of 16 bits (2e-4 to 2e-3) hides.  A result of 32 bits does not, so it is
-// computed on bf16 operations instead, whose products and sums are fp32: e4m3 is exact in bf16.  They take twice the time.
+// The sum of one block.  The 8-bit operation does not add its 128 products in fp32: of every eight neighbours it drops, towards zero, what lies more than 13 bits below the largest product's
+// exponent (256 + 2^-6 gives 256, 256 + 2^-5 is kept), and adds the eights' sums in fp32.  Measured, of the result's norm: 1.4e-5 on normal numbers, 3e-5 to 7e-5 on bytes of random exponents and
+// on rows with one number of 448 and small ones; at worst, on random bytes, 1e-3 of the sum of the magnitudes of a few products and 2e-4 of that of 128.  A result of 16 bits is rounded by
+// 2e-4 (fp16) to 1.1e-3 (bf16) of its norm, so there the operation is used: single results in which much cancels may be off by more than their own last place.  A result of 32 bits does
+// not hide it, and is computed on bf16 operations, whose products and sums are fp32 (e4m3 is exact in bf16).  They take twice the time (4096 x 4096 x 4096: 60 and 130 us).
 template <bool EXACT> struct BlockProduct;
 template <> struct BlockProduct<false> {
     typedef Part Operand;
@@ -92,7 +94,7 @@ template <int DT> __device__ __forceinline__ void store4(const xl_block_matmul_a
 }
 
 // Few rows of a: what costs is reading b once.  16 rows of b and MT x 16 of a a workgroup, whose eight waves take the blocks in turn; their sums meet in LDS, in the
-// same order every time.  (16 x 4096 x 2048: 3.9 us, of which an empty launch is 2.6; 16 x 8192 x 8192: 17.0 us, 4.0 TB/s.  Four or sixteen waves, or the
+// same order every time.  (16 x 4096 x 2048: 3.9 us, of which a launch is 1.9; 16 x 8192 x 8192: 17.4 us, 3.9 TB/s.  Four or sixteen waves, or the
 // operands of two or four blocks on their way at once, measured the same within 5 %.)
 template <int DT, int MT>
 __global__ __launch_bounds__(512) void thin_kernel(const xl_block_matmul_args a, int tiles_n)

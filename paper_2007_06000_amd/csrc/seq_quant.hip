@@ -46,8 +46,8 @@ static dim3 grid_of(long long blocks, long long groups)
 __device__ __forceinline__ long long group_of_rows() { return (long long)blockIdx.z * GRID_Y + blockIdx.y; }
 
 // 16 lanes a block, 8 numbers a lane, PER neighbouring blocks of 16 / PER rows a workgroup; workgroups next to each other go on along the rows.
-// With four blocks a wave reads a kilobyte of a row in one go; 24642 x 4096 in bf16 takes 64 us (4.8 TB/s; a copy of as many bytes 55), in fp32 (x 4000)
-// 87.  One block of sixteen rows, workgroups going down the rows: 70 and 123.  Fewer blocks where a row has no four.
+// With four blocks a wave reads a kilobyte of a row in one go; 24642 x 4096 in bf16 takes 65 us for 303 MB (4.7 TB/s, as a copy of 4 GB; a copy of 300 MB whose source the
+// last-level cache holds 55), in fp32 (x 4000) 88.  One block of sixteen rows, workgroups going down the rows: 70 and 123.  Fewer blocks where a row has no four.
 template <int DT, int PER>
 __global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
 {

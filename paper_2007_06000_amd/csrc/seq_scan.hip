@@ -2,9 +2,10 @@
 //
 //   h[n] <- exp(d A[n]) h[n] + d u B[n],   y = sum_n C[n] h[n] + D u,   y *= z sigmoid(z)
 //
-// exp(d A) is taken as 2^(d A log2 e), one hardware exponential.  Many tokens are bound by the issue of vector instructions: a state and token take an exponential and
-// five others, a channel and token some fifty more (softplus, gate, layouts), 9.2 for each of 16 states in all.  2 x 12321 x 2048 with 16
-// states in bf16: 258 us, 3.1e12 states a second, the vector units issuing for 84 % of it; its 404 MB alone would take 86 us.  Single tokens are bound by the states' bytes.
+// exp(d A) is taken as 2^(d A log2 e), one hardware exponential.  Many tokens are bound by the issue of vector instructions: a state and token take an exponential, which takes two
+// issue slots, and five others (four are the least: two runs), a channel and token some fifty more (softplus, gate, layouts), 10.7 slots for each of 16 states in all.  2 x 12321 x 2048
+// with 16 states in bf16: 259 us, 3.1e12 states a second, the vector units issuing for 83 % of it (steps without softplus 274 us); its 404 MB alone would take 86 us.  Single tokens are bound
+// by the states' bytes.
 #include <algorithm>
 #include <climits>
 #include <initializer_list>
@@ -47,7 +48,7 @@ static constexpr unsigned NOWHERE = 0x80000000u;       // past the end of every 
 enum Access { VECTORS, SINGLES, SCATTERED };
 
 // A token after the other: LP lanes a channel, four states (a 16-byte load) a lane, 256 / LP channels a workgroup.  One token of 64 sequences of 2048 channels and 16
-// states: 5.9 us for 17.8 MB, of which an empty launch is 2.4; of 256 sequences 15 us for 71 MB (4.7 TB/s).
+// states: 5.9 us for 17.8 MB, of which a launch is 1.9; of 256 sequences 15 us for 71 MB (4.7 TB/s).
 template <int DT, int LP>
 __global__ __launch_bounds__(256) void step_kernel(const xl_scan_args a, int groups)
 {

@@ -41,7 +41,10 @@ def random_weights(width: int, inner: int, states: int = 16, rank: Optional[int]
 
 
 class ScanBlock:
-    """Weights as `random_weights` names them; activations in `dtype`."""
+    """Weights as `random_weights` names them; activations in `dtype`.
+
+    The four products have 8-bit operands in every `dtype`, those that make the steps and state vectors too: what a step depends on is
+    rounded to four significant bits for each product.  float32 takes the sums and the activations between the operators to 32 bits."""
 
     def __init__(self, weights: Dict[str, torch.Tensor], device: int = 0, dtype: torch.dtype = torch.bfloat16):
         self.dev, self.dtype = torch.device("cuda", device), dtype
