@@ -127,7 +127,7 @@ xl_status xl_quantize_blocks(const xl_quantize_args *args, void *stream);
  * Rows of a and b begin at multiples of 16 bytes and can be read to the next multiple of 16 behind their k numbers; what
  * lies there does not matter.  A scale for each block is applied to the block's sum, and the blocks are summed in fp32.  Inside a block of 128 products sums are fp32 where y is.  Where y has 16
  * bits they are those of the 8-bit matrix operation, which drops, of eight neighbours, what lies more than 13 bits below the largest product: 1e-5 to 7e-5 of the result's norm, less than y's rounding,
- * but more than the last place of a single result in which much cancels.  y must not overlap a or b.
+ * but more than the last place of a single result in which much cancels.  The product of a scale of a and one of b has to be an fp32 number.  y must not overlap a or b.
  */
 typedef struct xl_block_matmul_args {
     long long m, n, k;
