@@ -9,9 +9,12 @@
  *   xl_selective_scan    state-space recurrence whose step and input/output vectors depend on the token
  *   xl_quantize_blocks   numbers -> 8-bit floating point (e4m3) with one scale for each block of 128
  *   xl_block_matmul      product of two such operands
+ *   xl_rms_norm          root-mean-square norm with the residual's addition, the result as numbers or as such an operand
+ *   xl_add_adapters      low-rank adapters of many sequences beside a shared product
+ *   xl_gated_delta_rule  recurrence of matrices that every token decays, corrects and reads
  *
  * Every call takes one struct of 64-bit numbers and DEVICE pointers, enqueues one kernel (a large
- * product and a scan with a workspace two, sizes that take 2^32 threads and more several) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
+ * product and calls with a workspace two, sizes that take 2^32 threads and more several) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
  * nothing and keeps nothing between calls.  Calls never throw or abort.  The current HIP device must be a gfx950 (XL_E_DEVICE) that can reach the
  * pointers.  Inference only: there are no gradients.
  *
@@ -40,6 +43,8 @@ enum { XL_F32 = 0, XL_F16 = 1, XL_BF16 = 2 };
 #define XL_SCALE_BLOCK   128    /* numbers along a row that share a scale           */
 #define XL_MAX_TAPS      4
 #define XL_MAX_STATES    128
+#define XL_MAX_RANK      128    /* of an adapter                                    */
+#define XL_MAX_KEY       256    /* numbers of a delta rule's key                    */
 
 /*
  * y[b,t,c] = act(bias[c] + sum over j < taps of weight[c,j] * x[b, t - (taps - 1) + j, c]),  act = v * sigmoid(v) or none.
@@ -142,6 +147,85 @@ typedef struct xl_block_matmul_args {
     void *y;
 } xl_block_matmul_args;
 xl_status xl_block_matmul(const xl_block_matmul_args *args, void *stream);
+
+/*
+ * r = x + residual (fp32; residual may be NULL: r = x),  new_residual = r rounded to its type,
+ * y[i,j] = r[i,j] / sqrt(sum over j of r[i,j]^2 / k + eps) * weight[j]
+ * x [rows, k] is of type `dtype`, residual and new_residual are of type `residual_dtype`: x's or XL_F32.  y is of type `dtype`; with `quantized` it is q and
+ * scales as xl_quantize_blocks makes them of the fp32 y with blocks of one row: rows of q begin at multiples of 16 bytes, and the bytes between a row's end and the next multiple of 16
+ * are set to zero.  The norm is that of r, not of what is kept of it; sums are fp32, and right also where squares leave its range.  eps is a positive fp32 number, 2^-126 at least.  A row with an
+ * infinity or a NaN comes out as NaN and zeros (q: as the quantiser has them).  new_residual may be residual, and y may be x, each with the same steps; they must not overlap otherwise.
+ */
+typedef struct xl_rms_norm_args {
+    long long rows, k;
+    long long dtype, residual_dtype;
+    long long quantized;
+    long long x_row, residual_row, new_residual_row;    /* elements between rows                            */
+    long long y_row;                                    /* elements, or bytes (a multiple of 16) with `quantized` */
+    long long scale_row, scale_block;
+    double eps;
+    const void *x;
+    const void *residual;
+    void *new_residual;                                 /* NULL: not kept                                   */
+    const float *weight;                                /* [k]                                              */
+    void *y;
+    float *scales;                                      /* with `quantized`                                 */
+} xl_rms_norm_args;
+xl_status xl_rms_norm(const xl_rms_norm_args *args, void *stream);
+
+/*
+ * For every token of sequence b, whose adapter is e = index[b]:
+ *   out[b,t] = y[b,t] + scales[e] * up[e] (down[e] x[b,t]),   out[b,t] = y[b,t] where e lies outside [0, adapters)
+ * x [batch, length, k], y and out [batch, length, n], down [adapters, rank, k] and up [adapters, n, rank] are of type `dtype`, scales [adapters] fp32 (NULL: ones).
+ * rank is 1 to 128; adapters of a smaller one are filled up with zeros.  Sums are fp32, and so is down x, which is never rounded to fewer bits than 16.  Infinities and NaN stay in their token's row.  out may be
+ * y with the same steps and must not overlap x, down or up.
+ * The workspace is xl_add_adapters_workspace bytes, aligned to 16; it holds nothing between calls.
+ */
+typedef struct xl_adapters_args {
+    long long batch, length, k, n, rank, adapters;
+    long long dtype;
+    long long x_batch, x_token, y_batch, y_token, out_batch, out_token;
+    long long workspace_bytes;
+    const void *x, *y;
+    const void *down, *up;
+    const int *index;                       /* [batch]                                  */
+    const float *scales;
+    const int *lengths;
+    void *out;
+    void *workspace;
+} xl_adapters_args;
+xl_status xl_add_adapters(const xl_adapters_args *args, void *stream);
+long long xl_add_adapters_workspace(const xl_adapters_args *args);
+
+/*
+ * For every sequence and head h, with a matrix of states S [dk, dv] and the key head h / (heads / key_heads):
+ *   S <- exp(g[t]) S,   S <- S + beta[t] k[t] (v[t] - S^T k[t])^T,   y[t] = scale * S^T q[t]
+ * q and k are [batch, length, key_heads, dk], v and y [batch, length, heads, dv], of type `dtype`; g and beta [batch, length, heads] and the states
+ * [nslots, heads, dk, dv] are fp32.  heads is a multiple of key_heads, dk is 1 to 256.  With `normalize` q[t] and k[t] are divided by
+ * sqrt(sum of their squares + 1e-6).  g is at most 0: what is greater counts as 0, and below -128 nothing is left of the states, as of exp(-128) in fp32.  Keys longer than one make
+ * states that grow; they are followed as far as fp32 goes.  What an infinite or NaN input makes of its states' columns is not finite from its token on; infinity or NaN is not said.
+ * Arithmetic is fp32, also on the matrix units, which get fp32 operands as sums of bf16 parts: three where states come of it, two for what only makes a y of 16 bits.
+ * y must not overlap the inputs.  The workspace is xl_gated_delta_rule_workspace bytes, aligned to 16; it holds nothing between calls.
+ */
+typedef struct xl_delta_args {
+    long long batch, length, key_heads, heads, dk, dv;
+    long long dtype;
+    long long normalize;
+    long long q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, y_batch, y_token, y_head;
+    long long g_batch, g_token, beta_batch, beta_token;
+    long long nslots;
+    long long workspace_bytes;
+    double scale;
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const float *state;
+    float *new_state;
+    const int *lengths, *slots;
+    void *y;
+    void *workspace;
+} xl_delta_args;
+xl_status xl_gated_delta_rule(const xl_delta_args *args, void *stream);
+long long xl_gated_delta_rule_workspace(const xl_delta_args *args);
 
 const char *xl_seq_last_error(void);
 

@@ -95,3 +95,66 @@ def block_matmul(a, a_scales, b, b_scales, bias):
         y = y + s * (a[:, at] @ b[:, at].T)
         mag = mag + np.abs(s) * (np.abs(a[:, at]) @ np.abs(b[:, at]).T)
     return y, mag
+
+
+def rms_norm(x, residual, weight, eps):
+    """y, its bound, and the sum x + residual."""
+    r = x if residual is None else x + residual
+    root = np.sqrt((r ** 2).mean(1, keepdims=True) + eps)
+    y = r / root * weight
+    # the sum's rounding, at most 64 squares one after the other in each of some lanes that meet in pairs (half of it: a root), root, three products
+    return y, (52 + x.shape[1] / 1024 + 10) * U * np.abs(y) + 2.0 ** -149, r
+
+
+def add_adapters(y, x, down, up, scales, index, lengths, parts):
+    """out and its bound; with `parts` down x counts as rounded to 16 bits."""
+    out, bound = np.array(y, copy=True), np.zeros(y.shape)
+    k, rank = x.shape[2], up.shape[2]
+    for b, n in enumerate(lengths):
+        e = index[b]
+        if 0 <= e < len(down):
+            s = 1.0 if scales is None else scales[e]
+            t, mag = x[b, :n] @ down[e].T * s, np.abs(x[b, :n]) @ np.abs(down[e]).T * abs(s)
+            off = (k + 6) * U * mag + (2.0 ** -16 if parts else 0) * np.abs(t)
+            more = np.abs(t) @ np.abs(up[e]).T
+            out[b, :n] += t @ up[e].T
+            bound[b, :n] = off @ np.abs(up[e]).T + (rank + 6) * U * (more + np.abs(y[b, :n]))
+        out[b, n:] = 0
+    return out, bound
+
+
+def gated_delta_rule(q, k, v, g, beta, scale, normalize, state, lengths, parts):
+    """y, its bound, the new states, and the bound of their columns' 2-norms.
+
+    A token multiplies what the columns of the states are off by with exp(g) (I - beta k k^T), whose 2-norm is max(1, |1 - beta k.k|), and adds
+    its own rounding: sums over the numbers of a key and over the up to 64 tokens that are worked on together, of the states' and the correction's size.
+    With `parts` the result's own sums are of operands rounded to 16 bits."""
+    batch, length, heads, dv = v.shape
+    dk, group = q.shape[3], heads // q.shape[2]
+    if normalize:
+        q, k = (t / np.sqrt((t ** 2).sum(-1, keepdims=True) + 1e-6) for t in (q, k))
+    y, bound = np.zeros(v.shape), np.zeros(v.shape)
+    new, new_bound = np.zeros((batch, heads, dk, dv)), np.zeros((batch, heads, dv))
+    c = 2 * (dk + 64) * U
+    at = np.arange(heads) // group
+    with np.errstate(under="ignore"):
+        for b in range(batch):
+            S = np.zeros((heads, dk, dv)) if state is None else state[b].copy()
+            off = np.zeros((heads, dv))
+            recent = np.sqrt((S ** 2).sum(1))           # the largest states of the last 64 tokens, decayed: what is added up inside a chunk
+            for t in range(lengths[b]):
+                gt = np.clip(g[b, t], -128, 0)
+                e = np.exp(gt)[:, None]
+                S = S * e[..., None]
+                kt, qt, bt = k[b, t, at], q[b, t, at], beta[b, t][:, None]
+                nk, nq = np.sqrt((kt ** 2).sum(1))[:, None], np.sqrt((qt ** 2).sum(1))[:, None]
+                size = np.sqrt((S ** 2).sum(1))
+                d = bt * (v[b, t] - np.einsum("hij,hi->hj", S, kt))
+                grow = np.maximum(1, np.abs(1 - bt * nk ** 2))
+                recent = np.maximum(recent * e, size) + np.abs(bt) * nk * np.abs(v[b, t])
+                off = grow * e * off + c * (recent + np.abs(bt) * nk * (nk * recent + np.abs(v[b, t])))
+                S = S + kt[..., None] * d[:, None, :]
+                y[b, t] = scale * np.einsum("hij,hi->hj", S, qt)
+                bound[b, t] = abs(scale) * nq * (off + (c + (3 * 2.0 ** -16 if parts else 0)) * (recent + np.abs(d) * nk))
+            new[b], new_bound[b] = S, off
+    return y, bound, new, new_bound

@@ -29,8 +29,10 @@ HEADERS = [os.path.join(CSRC, "xl_internal.h"), os.path.join(CSRC, "plan.h"), os
            os.path.join(ROOT, "include", "xl.h")]
 SEQ_LIB = os.path.join(HERE, "libxl_seq.so")
 SEQ_SOURCES = [("seq_api.cpp", "seq_api", []), ("seq_conv.hip", "seq_conv", []), ("seq_scan.hip", "seq_scan", []),
-               ("seq_quant.hip", "seq_quant", []), ("seq_matmul.hip", "seq_matmul", [])]
-SEQ_HEADERS = [os.path.join(CSRC, "seq_internal.h"), os.path.join(CSRC, "seq_launch.h"), os.path.join(ROOT, "include", "xl_seq.h"), os.path.join(ROOT, "include", "xl.h")]
+               ("seq_quant.hip", "seq_quant", []), ("seq_matmul.hip", "seq_matmul", []), ("seq_mix_api.cpp", "seq_mix_api", []),
+               ("seq_norm.hip", "seq_norm", []), ("seq_adapters.hip", "seq_adapters", []), ("seq_delta.hip", "seq_delta", [])]
+SEQ_HEADERS = [os.path.join(CSRC, "seq_internal.h"), os.path.join(CSRC, "seq_launch.h"), os.path.join(CSRC, "seq_checks.h"), os.path.join(CSRC, "seq_e4m3.h"),
+               os.path.join(ROOT, "include", "xl_seq.h"), os.path.join(ROOT, "include", "xl.h")]
 MODULE = os.path.join(HERE, "_xl_seq.so")
 
 # packed-fp32 instructions are switched off for all device code
@@ -71,7 +73,7 @@ def _compile(item, headers, force: bool) -> str:
 
 def _build_module(force: bool) -> str:
     src = os.path.join(CSRC, "seq_torch.cpp")
-    newest = max(os.path.getmtime(p) for p in [src, os.path.join(CSRC, "seq_overlap.h")] + SEQ_HEADERS[2:])
+    newest = max(os.path.getmtime(p) for p in [src, os.path.join(CSRC, "seq_overlap.h")] + SEQ_HEADERS[-2:])
     if not force and os.path.exists(MODULE) and os.path.getmtime(MODULE) >= newest:
         return MODULE
     from torch.utils.cpp_extension import include_paths, library_paths     # both name only files of the installed torch

@@ -1,0 +1,191 @@
+// Root-mean-square norm of rows, with the residual's addition in front and eight-bit numbers behind.
+//
+//   r = x + residual,  y = r / sqrt(mean(r^2) + eps) * weight,  and with 8 bits  scale = max(max|y| / 448, 2^-126), q = e4m3(y / scale)
+//
+// Bound by memory.  A row's numbers stay in the registers of the lanes that have loaded them until its sum is known: eight neighbours a lane and load, so that sixteen
+// lanes hold a block of 128 with its scale.
+#include "seq_e4m3.h"
+#include "seq_internal.h"
+
+namespace xls {
+
+struct Row {
+    const char *x, *residual;
+    char *kept, *y;
+    float *scales;
+};
+
+template <int DT> __device__ __forceinline__ void load8f(const void *row, int k, int K, float *v)
+{
+    typedef typename Elem<DT>::T T;
+    const Vec<T, 8> w = load_some<T, 8>(static_cast<const T *>(row) + k, K - k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
+}
+template <int DT> __device__ __forceinline__ void store8f(void *row, int k, int K, const float *v)
+{
+    typedef typename Elem<DT>::T T;
+    Vec<T, 8> w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = (T)v[i];
+    store_some<T, 8>(static_cast<T *>(row) + k, K - k, w);
+}
+
+// r of eight neighbours from column k on; zeros past the end
+template <int DT> __device__ __forceinline__ void load_sum(const xl_rms_norm_args &a, const Row &row, int k, int K, float *r)
+{
+    load8f<DT>(row.x, k, K, r);
+    if (!row.residual) return;
+    float more[8];
+    if (a.residual_dtype == XL_F32) load8f<XL_F32>(row.residual, k, K, more);
+    else load8f<DT>(row.residual, k, K, more);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] += more[i];
+}
+template <int DT> __device__ __forceinline__ void keep(const xl_rms_norm_args &a, const Row &row, int k, int K, const float *r)
+{
+    if (!row.kept || k >= K) return;
+    if (a.residual_dtype == XL_F32) store8f<XL_F32>(row.kept, k, K, r);
+    else store8f<DT>(row.kept, k, K, r);
+}
+
+template <int W> __device__ __forceinline__ float sum_of_row(float s, float *shared)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) s += __shfl_xor(s, o);
+    if constexpr (W > 1) {
+        __syncthreads();        // the sums before have been read
+        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = s;
+        __syncthreads();
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s += shared[i];
+    }
+    return s;
+}
+
+// Squares of numbers above 2^64 leave fp32.  Then the sum is taken of numbers that are scaled down: those whose squares vanish, and eps, do not count beside it.
+static constexpr float DOWN = 0x1p-80f;
+
+// y, or q and a scale, of eight neighbours; by = {1 / root, and what r is to be multiplied with before}
+template <int DT, bool Q> __device__ __forceinline__ void finish(const xl_rms_norm_args &a, const Row &row, int k, int K, float *v, float down, float inverse)
+{
+    float w[8];
+    load8f<XL_F32>(a.weight, k, K, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] * down * inverse * w[i];
+    if constexpr (Q) {
+        unsigned most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) most = max(most, (unsigned)__shfl_xor((int)most, o));
+        const float scale = scale_of(most);
+        if (threadIdx.x % 16 == 0 && k < K) row.scales[k / XL_SCALE_BLOCK * a.scale_block] = scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] / scale;
+        if (k < (K + 15) / 16 * 16) *reinterpret_cast<u32x2 *>(row.y + k) = u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
+    } else if (k < K) {
+        store8f<DT>(row.y, k, K, v);
+    }
+}
+
+template <int DT, bool Q> __device__ __forceinline__ Row row_of(const xl_rms_norm_args &a, long long i)
+{
+    const int size = sizeof(typename Elem<DT>::T), kept = a.residual_dtype == XL_F32 ? 4 : size;
+    return {static_cast<const char *>(a.x) + i * a.x_row * size, a.residual ? static_cast<const char *>(a.residual) + i * a.residual_row * kept : nullptr,
+            a.new_residual ? static_cast<char *>(a.new_residual) + i * a.new_residual_row * kept : nullptr, static_cast<char *>(a.y) + i * a.y_row * (Q ? 1 : size),
+            Q ? a.scales + i * a.scale_row : nullptr};
+}
+
+// W waves a row, N times eight numbers a lane: rows of up to 512 W N numbers.
+template <int DT, bool Q, int W, int N>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_kernel(const xl_rms_norm_args a)
+{
+    constexpr int ROWS = W == 1 ? 4 : 1;
+    __shared__ float shared[W];
+    const int lane = threadIdx.x % (64 * W), K = (int)a.k;
+    const float k_inverse = 1.f / (float)K, eps = (float)a.eps;
+    for (long long i = (long long)blockIdx.x * ROWS + threadIdx.x / (64 * W); i < a.rows; i += (long long)gridDim.x * ROWS) {
+        const Row row = row_of<DT, Q>(a, i);
+        float r[N][8], s = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) load_sum<DT>(a, row, (n * 64 * W + lane) * 8, K, r[n]);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = __builtin_fmaf(r[n][j], r[n][j], s);
+        s = sum_of_row<W>(s, shared);
+        float down = 1.f, inverse = __builtin_amdgcn_rsqf(s * k_inverse + eps);
+        if (!(s < __builtin_inff())) {
+            s = 0.f;
+            down = DOWN;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s = __builtin_fmaf(r[n][j] * DOWN, r[n][j] * DOWN, s);
+            inverse = __builtin_amdgcn_rsqf(sum_of_row<W>(s, shared) * k_inverse);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) keep<DT>(a, row, (n * 64 * W + lane) * 8, K, r[n]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) finish<DT, Q>(a, row, (n * 64 * W + lane) * 8, K, r[n], down, inverse);
+    }
+}
+
+// Longer rows are read twice.
+template <int DT, bool Q>
+__global__ __launch_bounds__(1024) void long_norm_kernel(const xl_rms_norm_args a)
+{
+    __shared__ float shared[16];
+    const int K = (int)a.k, last = (K + 127) / 128 * 128;        // all lanes of a block of 128 take part in its scale
+    const float k_inverse = 1.f / (float)K, eps = (float)a.eps;
+    for (long long i = blockIdx.x; i < a.rows; i += gridDim.x) {
+        const Row row = row_of<DT, Q>(a, i);
+        float r[8], s = 0.f, t = 0.f;
+        for (int k = threadIdx.x * 8; k < K; k += 8192) {
+            load_sum<DT>(a, row, k, K, r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s = __builtin_fmaf(r[j], r[j], s);
+                t = __builtin_fmaf(r[j] * DOWN, r[j] * DOWN, t);
+            }
+        }
+        s = sum_of_row<16>(s, shared);
+        t = sum_of_row<16>(t, shared);
+        const bool large = !(s < __builtin_inff());
+        const float inverse = __builtin_amdgcn_rsqf(large ? t * k_inverse : s * k_inverse + eps);
+        for (int k = threadIdx.x * 8; k < last; k += 8192) {
+            load_sum<DT>(a, row, k, K, r);
+            keep<DT>(a, row, k, K, r);
+            finish<DT, Q>(a, row, k, K, r, large ? DOWN : 1.f, inverse);
+        }
+    }
+}
+
+template <int DT, bool Q, int W, int N> static hipError_t launch_rows(const xl_rms_norm_args &a, hipStream_t s)
+{
+    const long long groups = W == 1 ? (a.rows + 3) / 4 : a.rows;
+    return launch_kernel(norm_kernel<DT, Q, W, N>, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), W == 1 ? 256 : 64 * W, s, a);
+}
+
+template <int DT, bool Q> static hipError_t launch_type(const xl_rms_norm_args &a, hipStream_t s)
+{
+    if (a.k <= 512) return launch_rows<DT, Q, 1, 1>(a, s);
+    if (a.k <= 1024) return launch_rows<DT, Q, 1, 2>(a, s);
+    if (a.k <= 2048) return launch_rows<DT, Q, 4, 1>(a, s);
+    if (a.k <= 4096) return launch_rows<DT, Q, 4, 2>(a, s);
+    if (a.k <= 8192) return launch_rows<DT, Q, 4, 4>(a, s);
+    if (a.k <= 16384) return launch_rows<DT, Q, 4, 8>(a, s);
+    if (a.k <= 32768) return launch_rows<DT, Q, 16, 4>(a, s);
+    return launch_kernel(long_norm_kernel<DT, Q>, dim3((unsigned)(a.rows < 1 << 20 ? a.rows : 1 << 20)), 1024, s, a);
+}
+
+template <int DT> static hipError_t launch_result(const xl_rms_norm_args &a, hipStream_t s) { return a.quantized ? launch_type<DT, true>(a, s) : launch_type<DT, false>(a, s); }
+
+hipError_t launch_rms_norm(const xl_rms_norm_args &a, hipStream_t s)
+{
+    return a.dtype == XL_F32 ? launch_result<XL_F32>(a, s) : a.dtype == XL_F16 ? launch_result<XL_F16>(a, s) : launch_result<XL_BF16>(a, s);
+}
+
+}  // namespace xls

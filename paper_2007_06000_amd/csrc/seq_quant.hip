@@ -4,25 +4,10 @@
 //
 // Bound by memory.  The division is a true one (about ten operations a number, hidden behind the loads): a product with the reciprocal lands on the
 // other side of a tie now and then, and q would depend on how it was computed.
+#include "seq_e4m3.h"
 #include "seq_internal.h"
 
 namespace xls {
-
-static constexpr float E4M3_MAX = 448.f, MIN_SCALE = 1.17549435e-38f;
-
-// The largest |x| as the bits of a float: the order of the bits is the order of the numbers, infinity and then NaN above them.
-__device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
-__device__ __forceinline__ float scale_of(unsigned most)
-{
-    const float s = __builtin_bit_cast(float, most) / E4M3_MAX;
-    return s < MIN_SCALE ? MIN_SCALE : s;      // a NaN stays
-}
-
-__device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)
-{
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
 
 // Eight numbers of a row from column k on; those past its end are zeros.
 template <int DT> __device__ __forceinline__ void load8(const typename Elem<DT>::T *x, long long at, int k, int K, float *v)

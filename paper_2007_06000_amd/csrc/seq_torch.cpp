@@ -15,10 +15,12 @@
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPStream.h>
 
+#include <cmath>
 #include <cstdint>
 #include <initializer_list>
 #include <sstream>
 #include <string>
+#include <type_traits>
 
 #include "seq_overlap.h"
 #include "xl_seq.h"
@@ -31,6 +33,11 @@ decltype(&xl_selective_scan) g_scan;
 decltype(&xl_selective_scan_workspace) g_scan_workspace;
 decltype(&xl_quantize_blocks) g_quantize;
 decltype(&xl_block_matmul) g_matmul;
+decltype(&xl_rms_norm) g_norm;
+decltype(&xl_add_adapters) g_adapters;
+decltype(&xl_add_adapters_workspace) g_adapters_workspace;
+decltype(&xl_gated_delta_rule) g_delta;
+decltype(&xl_gated_delta_rule_workspace) g_delta_workspace;
 decltype(&xl_seq_last_error) g_last_error;
 PyObject *g_error;
 
@@ -52,6 +59,12 @@ xls::Span rows_of(const at::Tensor &t)
 {
     const int64_t size = t.element_size();
     return {address(t), t.size(0), t.size(1), t.stride(0) * size, t.stride(1) * size, t.size(2) * size};
+}
+// rows of [batch, length, heads, width]; heads that lie apart as if what lies between them were theirs
+xls::Span heads_of(const at::Tensor &t)
+{
+    const int64_t size = t.element_size();
+    return {address(t), t.size(0), t.size(1), t.stride(0) * size, t.stride(1) * size, t.size(2) > 0 ? ((t.size(2) - 1) * t.stride(2) + t.size(3)) * size : 0};
 }
 xls::Span block_of(const at::Tensor *t) { return t ? xls::Span{address(*t), 1, 1, 0, 0, int64_t(t->nbytes())} : xls::Span{}; }
 xls::Span rows_of(const at::Tensor &t, int64_t width) { return {address(t), 1, t.size(0), 0, t.stride(0) * int64_t(t.element_size()), width}; }
@@ -119,6 +132,16 @@ struct Op {
         token = t.stride(1);
     }
 
+    // [batch, length, heads, width] with a contiguous last dimension: its steps between sequences, tokens and heads.
+    void heads(const char *what, const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape, long long &batch, long long &token, long long &head) const
+    {
+        check(what, t, type, shape);
+        if (t.stride(3) != 1 && shape[3] > 1) refuse(XL_E_SHAPE, name, ": the last dimension of ", what, " must be contiguous");
+        batch = t.stride(0);
+        token = t.stride(1);
+        head = t.stride(2);
+    }
+
     // A contiguous tensor, or none.
     void *dense(const char *what, const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape) const
     {
@@ -176,6 +199,12 @@ struct Args {
         return THPVariable_Unpack(args[i]);
     }
     const at::Tensor *optional(int i) const { return args[i] == Py_None ? nullptr : &tensor(i); }
+    double number(int i) const
+    {
+        const double v = PyFloat_AsDouble(args[i]);
+        if (v == -1. && PyErr_Occurred()) throw python_error();
+        return v;
+    }
     bool flag(int i) const
     {
         const int v = PyObject_IsTrue(args[i]);
@@ -183,6 +212,9 @@ struct Args {
         return v;
     }
 };
+
+// A result as it goes back: the object that was handed in, or a new one.
+PyObject *result(PyObject *given, const at::Tensor &t) { return given == Py_None ? THPVariable_Wrap(t) : Py_NewRef(given); }
 
 // (first, second) as a tuple; what was handed in goes back as the object it was.
 PyObject *pair(PyObject *given0, const at::Tensor &t0, PyObject *given1, const at::Tensor &t1)
@@ -435,6 +467,191 @@ PyObject *block_matmul(const Args &in)      // a, a_scales, b, b_scales, bias, d
     return result;
 }
 
+PyObject *rms_norm(const Args &in)          // name, x, weight, residual, new_residual, eps, out, scales
+{
+    const char *name = PyUnicode_AsUTF8(in.args[0]);
+    if (!name) throw python_error();
+    const bool quantized = name[8] != 0;        // rms_norm_quantized
+    const at::Tensor &x = in.tensor(1), &weight = in.tensor(2);
+    const at::Tensor *residual = in.optional(3), *kept = in.optional(4), *out = in.optional(6), *scales = in.optional(7);
+    if (x.dim() != 2) refuse(XL_E_SHAPE, name, ": x is [rows, k]");
+    const Op op(name, x);
+    const at::ScalarType type = x.scalar_type(), sum_type = residual ? residual->scalar_type() : kept ? kept->scalar_type() : type;
+    xl_rms_norm_args a = {};
+    a.dtype = type_code(name, "x", type);
+    a.residual_dtype = type_code(name, "residual", sum_type);
+    a.quantized = quantized;
+    a.rows = x.size(0);
+    a.k = x.size(1);
+    a.eps = in.number(5);
+    const int64_t blocks[] = {a.rows, (a.k + XL_SCALE_BLOCK - 1) / XL_SCALE_BLOCK}, wide = (a.k + 15) / 16 * 16;
+    const at::ScalarType out_type = quantized ? at::kFloat8_e4m3fn : type;
+    at::Tensor made, made_scales, made_kept;
+    if (!out) {
+        made = op.make({a.rows, quantized ? wide : a.k}, out_type);
+        if (quantized && wide != a.k) made.unsafeGetTensorImpl()->set_sizes_and_strides(x.sizes(), at::IntArrayRef{wide, 1});
+        out = &made;
+    }
+    if (quantized && !scales) {     // a column for each block, as the quantiser leaves them
+        const int64_t step[] = {1, a.rows};
+        scales = &(made_scales = op.make(blocks, step, at::kFloat));
+    }
+    if (residual && !kept) kept = &(made_kept = op.make(x.sizes(), sum_type));
+    op.check("x", x, type, x.sizes());
+    op.check("out", *out, out_type, x.sizes());
+    if (residual) op.check("residual", *residual, sum_type, x.sizes());
+    if (kept) op.check("new_residual", *kept, sum_type, x.sizes());
+    if (quantized) op.check("scales", *scales, at::kFloat, blocks);
+    if (a.k > 1 && (x.stride(1) != 1 || out->stride(1) != 1 || (residual && residual->stride(1) != 1) || (kept && kept->stride(1) != 1)))
+        refuse(XL_E_SHAPE, name, ": rows of x, out and the residuals must be contiguous");
+    if (quantized) {
+        check_readable(op, "out", *out);
+        a.scale_row = scales->stride(0);
+        a.scale_block = scales->stride(1);
+        a.scales = static_cast<float *>(scales->data_ptr());
+    }
+    a.x_row = x.stride(0);
+    a.y_row = out->stride(0);
+    a.x = x.data_ptr();
+    a.weight = op.dense_as<float>("weight", &weight, at::kFloat, {a.k});
+    a.y = out->data_ptr();
+    if (residual) {
+        a.residual_row = residual->stride(0);
+        a.residual = residual->data_ptr();
+    }
+    if (kept) {
+        a.new_residual_row = kept->stride(0);
+        a.new_residual = kept->data_ptr();
+    }
+    if (out != &made || (kept && kept != &made_kept) || (quantized && scales != &made_scales)) {
+        const auto span = [&](const at::Tensor *t) { return t ? rows_of(*t, a.k * int64_t(t->element_size())) : xls::Span{}; };
+        const Named factor = {"weight", block_of(&weight)}, sum = {"new_residual", span(kept)}, numbers = {"scales", quantized ? numbers_of(*scales) : xls::Span{}};
+        Named input = {"x (or is it, as a whole)", span(&x)}, old = {"residual (or is it, as a whole)", span(residual)};
+        if (quantized && scales != &made_scales) op.apart("scales", numbers.span, {input, old, sum, factor});
+        if (kept && kept != &made_kept) op.apart("new_residual", sum.span, {input, {old.what, old.span == sum.span ? xls::Span{} : old.span}, factor});
+        if (out != &made) {
+            const xls::Span y = quantized ? rows_of(*out, wide) : span(out);
+            if (!quantized && y == input.span) input.span = {};
+            op.apart("out", y, {input, {"residual", old.span}, sum, factor, numbers});
+        }
+    }
+    op.run(g_norm, a);
+    if (out != &made) written(*out);
+    if (quantized && scales != &made_scales) written(*scales);
+    if (kept && kept != &made_kept) written(*kept);
+    PyObject *parts[] = {result(in.args[6], *out), quantized ? result(in.args[7], *scales) : nullptr, kept ? result(in.args[4], *kept) : Py_NewRef(in.args[1])};
+    PyObject *all = !parts[0] || (quantized && !parts[1]) || !parts[2] ? nullptr : quantized ? PyTuple_Pack(3, parts[0], parts[1], parts[2]) : PyTuple_Pack(2, parts[0], parts[2]);
+    for (PyObject *p : parts) Py_XDECREF(p);
+    if (!all) throw python_error();
+    return all;
+}
+
+PyObject *add_adapters(const Args &in)      // y, x, down, up, index, scales, lengths, out
+{
+    const at::Tensor &y = in.tensor(0), &x = in.tensor(1), &down = in.tensor(2), &up = in.tensor(3), &index = in.tensor(4);
+    const at::Tensor *scales = in.optional(5), *lengths = in.optional(6), *out = in.optional(7);
+    if (y.dim() != 3 || x.dim() != 3 || down.dim() != 3) refuse(XL_E_SHAPE, "add_adapters: y is [batch, length, n], x [batch, length, k] and down [adapters, rank, k]");
+    const Op op("add_adapters", y);
+    const at::ScalarType type = y.scalar_type();
+    xl_adapters_args a = {};
+    a.dtype = type_code(op.name, "y", type);
+    a.batch = y.size(0);
+    a.length = y.size(1);
+    a.n = y.size(2);
+    a.k = x.size(2);
+    a.adapters = down.size(0);
+    a.rank = down.size(1);
+    at::Tensor made;
+    if (!out) out = &(made = op.make(y.sizes(), type));
+    int64_t b, t;
+    op.rows("y", y, type, y.sizes(), b, t);
+    a.y_batch = b, a.y_token = t;
+    op.rows("x", x, type, {a.batch, a.length, a.k}, b, t);
+    a.x_batch = b, a.x_token = t;
+    op.rows("out", *out, type, y.sizes(), b, t);
+    a.out_batch = b, a.out_token = t;
+    a.y = y.data_ptr();
+    a.x = x.data_ptr();
+    a.out = out->data_ptr();
+    a.down = op.dense("down", &down, type, {a.adapters, a.rank, a.k});
+    a.up = op.dense("up", &up, type, {a.adapters, a.n, a.rank});
+    a.index = op.dense_as<int>("index", &index, at::kInt, {a.batch});
+    a.scales = op.dense_as<float>("scales", scales, at::kFloat, {a.adapters});
+    a.lengths = op.dense_as<int>("lengths", lengths, at::kInt, {a.batch});
+    if (out != &made) {
+        const xls::Span to = rows_of(*out), from = rows_of(y);
+        op.apart("out", to, {{"y (or is it, as a whole)", from == to ? xls::Span{} : from}, {"x", rows_of(x)}, {"down", block_of(&down)}, {"up", block_of(&up)},
+                             {"index", block_of(&index)}, {"scales", block_of(scales)}, {"lengths", block_of(lengths)}});
+    }
+    at::Tensor workspace;
+    a.workspace_bytes = g_adapters_workspace(&a);
+    if (a.workspace_bytes > 0) a.workspace = (workspace = op.make({a.workspace_bytes}, at::kByte)).data_ptr();
+    op.run(g_adapters, a);
+    if (out != &made) written(*out);
+    PyObject *given = result(in.args[7], *out);
+    if (!given) throw python_error();
+    return given;
+}
+
+PyObject *gated_delta_rule(const Args &in)  // q, k, v, g, beta, scale, normalize, state, new_state, lengths, slots, out
+{
+    const at::Tensor &q = in.tensor(0), &k = in.tensor(1), &v = in.tensor(2), &g = in.tensor(3), &beta = in.tensor(4);
+    const at::Tensor *state = in.optional(7), *lengths = in.optional(9), *slots = in.optional(10), *given = in.optional(11);
+    if (q.dim() != 4 || v.dim() != 4) refuse(XL_E_SHAPE, "gated_delta_rule: q is [batch, length, key heads, dk] and v [batch, length, heads, dv]");
+    const Op op("gated_delta_rule", v);
+    const at::ScalarType type = v.scalar_type();
+    xl_delta_args a = {};
+    a.dtype = type_code(op.name, "v", type);
+    a.batch = v.size(0);
+    a.length = v.size(1);
+    a.heads = v.size(2);
+    a.dv = v.size(3);
+    a.key_heads = q.size(2);
+    a.dk = q.size(3);
+    a.normalize = in.flag(6);
+    const at::Tensor *kept = state_out(op, state, in.optional(8), slots);
+    a.nslots = slots && state->dim() ? state->size(0) : a.batch;
+    const int64_t shape[] = {a.nslots, a.heads, a.dk, a.dv}, keys[] = {a.batch, a.length, a.key_heads, a.dk}, tokens[] = {a.batch, a.length, a.heads};
+    at::Tensor made, made_state;
+    if (!given) given = &(made = op.make(v.sizes(), type));
+    if (!kept) kept = &(made_state = op.make(shape, at::kFloat));
+    int64_t b, t;
+    op.heads("q", q, type, keys, a.q_batch, a.q_token, a.q_head);
+    op.heads("k", k, type, keys, a.k_batch, a.k_token, a.k_head);
+    op.heads("v", v, type, v.sizes(), a.v_batch, a.v_token, a.v_head);
+    op.heads("out", *given, type, v.sizes(), a.y_batch, a.y_token, a.y_head);
+    if (a.heads > 1 && a.dv > 0 && a.y_head != a.dv) refuse(XL_E_SHAPE, "gated_delta_rule: the heads of out must lie next to each other");
+    op.rows("g", g, at::kFloat, tokens, b, t);
+    a.g_batch = b, a.g_token = t;
+    op.rows("beta", beta, at::kFloat, tokens, b, t);
+    a.beta_batch = b, a.beta_token = t;
+    a.scale = in.args[5] == Py_None ? 1. / std::sqrt(double(a.dk > 0 ? a.dk : 1)) : in.number(5);
+    a.q = q.data_ptr();
+    a.k = k.data_ptr();
+    a.v = v.data_ptr();
+    a.g = static_cast<const float *>(g.data_ptr());
+    a.beta = static_cast<const float *>(beta.data_ptr());
+    a.state = op.dense_as<float>("state", state, at::kFloat, shape);
+    a.new_state = op.dense_as<float>("new_state", kept, at::kFloat, shape);
+    a.lengths = op.dense_as<int>("lengths", lengths, at::kInt, {a.batch});
+    a.slots = op.dense_as<int>("slots", slots, at::kInt, {a.batch});
+    a.y = given->data_ptr();
+    if (given != &made || kept != &made_state) {
+        const Named old = {"state (or is it, as a whole)", a.state != a.new_state ? block_of(state) : xls::Span{}};
+        const Named in_q = {"q", heads_of(q)}, in_k = {"k", heads_of(k)}, in_v = {"v", heads_of(v)}, in_g = {"g", rows_of(g)}, in_beta = {"beta", rows_of(beta)},
+                    in_lengths = {"lengths", block_of(lengths)}, in_slots = {"slots", block_of(slots)};
+        if (given != &made) op.apart("out", heads_of(*given), {in_q, in_k, in_v, in_g, in_beta, old, {"new_state", block_of(kept)}, in_lengths, in_slots});
+        if (kept != &made_state) op.apart("new_state", block_of(kept), {in_q, in_k, in_v, in_g, in_beta, old, in_lengths, in_slots});
+    }
+    at::Tensor workspace;
+    a.workspace_bytes = g_delta_workspace(&a);
+    if (a.workspace_bytes > 0) a.workspace = (workspace = op.make({a.workspace_bytes}, at::kByte)).data_ptr();
+    op.run(g_delta, a);
+    if (given != &made) written(*given);
+    if (kept != &made_state) written(*kept);
+    return pair(in.args[11], *given, in.args[8] == Py_None && slots ? in.args[7] : in.args[8], *kept);
+}
+
 template <PyObject *(*F)(const Args &), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
@@ -450,18 +667,25 @@ template <PyObject *(*F)(const Args &), int N> PyObject *entry(PyObject *, PyObj
     END_HANDLE_TH_ERRORS
 }
 
-// bind(conv, scan, scan_workspace, quantize, matmul, last_error, exception): the addresses of the library's functions
+// bind(address ..., exception): the library's functions, in the order of seq.py's list
 PyObject *bind(PyObject *, PyObject *args)
 {
-    unsigned long long f[6];
+    unsigned long long f[11];
     PyObject *error;
-    if (!PyArg_ParseTuple(args, "KKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &error)) return nullptr;
-    g_conv = reinterpret_cast<decltype(g_conv)>(f[0]);
-    g_scan = reinterpret_cast<decltype(g_scan)>(f[1]);
-    g_scan_workspace = reinterpret_cast<decltype(g_scan_workspace)>(f[2]);
-    g_quantize = reinterpret_cast<decltype(g_quantize)>(f[3]);
-    g_matmul = reinterpret_cast<decltype(g_matmul)>(f[4]);
-    g_last_error = reinterpret_cast<decltype(g_last_error)>(f[5]);
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10], &error)) return nullptr;
+    int i = 0;
+    const auto set = [&](auto &function) { function = reinterpret_cast<std::decay_t<decltype(function)>>(f[i++]); };
+    set(g_conv);
+    set(g_scan);
+    set(g_scan_workspace);
+    set(g_quantize);
+    set(g_matmul);
+    set(g_norm);
+    set(g_adapters);
+    set(g_adapters_workspace);
+    set(g_delta);
+    set(g_delta_workspace);
+    set(g_last_error);
     Py_INCREF(error);
     Py_XSETREF(g_error, error);
     Py_RETURN_NONE;
@@ -473,7 +697,8 @@ template <PyObject *(*F)(const Args &), int N> PyMethodDef method(const char *na
 }
 
 PyMethodDef methods[] = {method<causal_conv, 9>("causal_conv"), method<selective_scan, 14>("selective_scan"), method<quantize, 5>("quantize"),
-                         method<block_matmul, 7>("block_matmul"), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         method<block_matmul, 7>("block_matmul"), method<rms_norm, 8>("rms_norm"), method<add_adapters, 8>("add_adapters"),
+                         method<gated_delta_rule, 12>("gated_delta_rule"), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_xl_seq", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,7 +1,7 @@
-"""Sequence operators on torch tensors: causal convolution, selective scan, block quantisation, block-scaled product.
+"""Sequence operators on torch tensors: causal convolution, selective scan, gated delta rule, norm, block quantisation, block-scaled product, adapters.
 
 The names and the meaning of every argument mirror include/xl_seq.h; the arithmetic runs in the HIP kernels of libxl_seq.so, and there is no
-CPU fallback.  Each call enqueues one kernel (a large product and a long scan of few channels two) on the current stream of its tensors' device and returns without waiting;
+CPU fallback.  Each call enqueues one kernel (a large product, a long scan of few channels and other calls with a workspace two) on the current stream of its tensors' device and returns without waiting;
 what does not fit raises `XlError` before anything is launched.  Inference only: tensors that ask for gradients are refused.
 """
 from __future__ import annotations
@@ -22,7 +22,8 @@ XL_F32, XL_F16, XL_BF16 = 0, 1, 2
 SCALE_BLOCK = 128
 
 # every symbol include/xl_seq.h declares
-EXPORTS = ["xl_causal_conv", "xl_selective_scan", "xl_selective_scan_workspace", "xl_quantize_blocks", "xl_block_matmul", "xl_seq_last_error"]
+EXPORTS = ["xl_causal_conv", "xl_selective_scan", "xl_selective_scan_workspace", "xl_quantize_blocks", "xl_block_matmul", "xl_rms_norm", "xl_add_adapters",
+           "xl_add_adapters_workspace", "xl_gated_delta_rule", "xl_gated_delta_rule_workspace", "xl_seq_last_error"]
 
 _lib = None
 _module = None
@@ -39,8 +40,11 @@ def lib() -> ctypes.CDLL:
             f = getattr(L, name)
             f.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
             f.restype = ctypes.c_int
-        L.xl_selective_scan_workspace.argtypes = [ctypes.c_char_p]
-        L.xl_selective_scan_workspace.restype = ctypes.c_longlong
+        for name in EXPORTS:
+            if name.endswith("_workspace"):
+                f = getattr(L, name)
+                f.argtypes = [ctypes.c_char_p]
+                f.restype = ctypes.c_longlong
         L.xl_seq_last_error.argtypes = []
         L.xl_seq_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -107,3 +111,40 @@ def block_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_sca
     With dtype torch.float32 all sums are fp32.  For 16-bit results the products of a block are added by the 8-bit matrix operation, twice as fast: 1e-5 to
     7e-5 of the result's norm off, less than the rounding to 16 bits."""
     return (_module or module()).block_matmul(a, a_scales, b, b_scales, bias, dtype, out)
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[torch.Tensor] = None, new_residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(x + residual) / sqrt(mean of its squares + eps) * weight for the rows of x [rows, k]; weight [k] is fp32, residual of x's type or fp32.
+
+    Returns the result, of x's type, and the sum, of the residual's type, which is the next layer's residual (without a residual: x itself).  `new_residual` receives
+    the sum if given (`residual` itself may be), `out` the result (x itself may be).  The norm is that of the sum before it is rounded to its type."""
+    return (_module or module()).rms_norm("rms_norm", x, weight, residual, new_residual, eps, out, None)
+
+
+def rms_norm_quantized(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[torch.Tensor] = None, new_residual: Optional[torch.Tensor] = None,
+                       eps: float = 1e-6, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """`rms_norm` with its fp32 result quantised as by `quantize_rows`, an operand of `block_matmul`: returns the e4m3 numbers, their scales and the sum."""
+    return (_module or module()).rms_norm("rms_norm_quantized", x, weight, residual, new_residual, eps, out, scales)
+
+
+def add_adapters(y: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor, index: torch.Tensor, *, scales: Optional[torch.Tensor] = None,
+                 lengths: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y[b] + scales[e] * x[b] down[e]^T up[e]^T with the adapter e = index[b] (int32) of each sequence; y[b] itself where there is no such adapter.
+
+    y [batch, length, n] is what the projection that all sequences share makes of x [batch, length, k]; down [adapters, rank, k], up [adapters, n, rank], all of one
+    type, rank at most 128; scales [adapters] are fp32.  Tokens past a sequence's own length (`lengths`, int32) come out as zeros.  `out` may be y itself."""
+    return (_module or module()).add_adapters(y, x, down, up, index, scales, lengths, out)
+
+
+def gated_delta_rule(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor, *, scale: Optional[float] = None,
+                     normalize: bool = False, state: Optional[torch.Tensor] = None, new_state: Optional[torch.Tensor] = None,
+                     lengths: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Recurrence of a matrix S [dk, dv] for each head: S <- exp(g) S, S <- S + beta k (v - S^T k)^T, and the result scale * S^T q (scale: dk^-0.5).
+
+    q, k [batch, length, key heads, dk] and v [batch, length, heads, dv] are of one type; neighbouring heads share a key head.  g (at most 0) and beta
+    [batch, length, heads] are fp32.  `normalize` divides each token's q and k by sqrt(sum of squares + 1e-6).  Returns the result and the states
+    [batch, heads, dk, dv] (fp32) for the next call; `state`, `new_state`, `slots` as for `causal_conv`.  One token or many: a call of length 1 is the step
+    of a generation.  `out` must not share memory with an input."""
+    return (_module or module()).gated_delta_rule(q, k, v, g, beta, scale, normalize, state, new_state, lengths, slots, out)
