@@ -31,7 +31,7 @@ SEQ_LIB = os.path.join(HERE, "libxl_seq.so")
 SEQ_SOURCES = [("seq_api.cpp", "seq_api", []), ("seq_conv.hip", "seq_conv", []), ("seq_scan.hip", "seq_scan", []),
                ("seq_quant.hip", "seq_quant", []), ("seq_matmul.hip", "seq_matmul", []), ("seq_mix_api.cpp", "seq_mix_api", []),
                ("seq_norm.hip", "seq_norm", []), ("seq_adapters.hip", "seq_adapters", []), ("seq_delta.hip", "seq_delta", [])]
-SEQ_HEADERS = [os.path.join(CSRC, "seq_internal.h"), os.path.join(CSRC, "seq_launch.h"), os.path.join(CSRC, "seq_checks.h"), os.path.join(CSRC, "seq_e4m3.h"),
+SEQ_HEADERS = [os.path.join(CSRC, "seq_internal.h"), os.path.join(CSRC, "seq_launch.h"), os.path.join(CSRC, "seq_checks.h"), os.path.join(CSRC, "seq_e4m3.h"), os.path.join(CSRC, "seq_parts.h"),
                os.path.join(ROOT, "include", "xl_seq.h"), os.path.join(ROOT, "include", "xl.h")]
 MODULE = os.path.join(HERE, "_xl_seq.so")
 
