@@ -3,7 +3,14 @@
 //   S <- e^g S,  S <- S + beta k (v - S^T k)^T,  y = scale S^T q
 //
 // Columns of S do not meet: each is a recurrence of its own, with the same keys, queries, decays and steps.
-#include "seq_internal.h"
+//
+// Single tokens and a few go one after the other.  Longer runs go in chunks of 64 tokens.  With G_i the sum of g up to token i of a chunk, and S0 the states before it, the corrections
+// d_i = beta_i (v_i - S_i^T k_i) of its tokens solve a triangular system:
+//   (I + A) D = diag(beta) (V - diag(e^G) K S0),     A[i,j] = beta_i (k_i.k_j) e^(G_i - G_j) for j < i
+//   Y = scale (diag(e^G) Q S0 + P D),                P[i,j] = (q_i.k_j) e^(G_i - G_j) for j <= i
+//   S = e^G_64 S0 + K^T diag(e^(G_64 - G)) D
+// A first kernel makes T = (I + A)^-1 and P of all chunks at once, a second one goes through the chunks of a sequence with the states in registers.
+#include "seq_parts.h"
 
 namespace xls {
 
@@ -101,8 +108,455 @@ __global__ __launch_bounds__(256) void token_kernel(const xl_delta_args a, int t
     }
 }
 
+// The chunks.  All products are operations of 16 x 16 x 32 on bf16 parts.  An operation's result has in a lane (col = lane % 16, quad = lane / 16) rows 4 quad ... 4 quad + 3 of column col, and its operands
+// eight numbers from 8 quad on of row (column) col.  If row m of the tiles 2 s and 2 s + 1 stands for number 32 s + 8 (m / 4) + m % 4 (+ 4 in the second), a lane has eight neighbours of
+// a column in the two results, which is an operand of the next product: results turn into operands without crossing lanes.
+static constexpr int CHUNK = 64;
+__device__ __forceinline__ int dealt(int tile, int m) { return tile / 2 * 32 + m / 4 * 8 + tile % 2 * 4 + m % 4; }
+
+// What the first kernel leaves of a chunk: operands as the second one's lanes read them, one after the other (T and P: tiles 0 and 1 have numbers for tokens 0 to 31, tiles 2 and 3 for all),
+// and for each token what its row is multiplied with.
+template <int DT, int DK> struct ChunkOf {
+    static constexpr int NP = parts_of<DT>(), NY = DT == XL_F32 ? 3 : 2;        // parts of inputs, and of what only y is made of
+    struct Rows {
+        float read[CHUNK], beta[CHUNK], write[CHUNK], query[CHUNK];     // e^G / |k|, beta, e^(G_64 - G) / |k|, scale e^G / |q|
+    };
+    bf16x8 T[6][3][64], P[6][NY][64], keys[DK / 16][2][NP][64];
+    Rows rows;
+    float decay[64];    // e^G_64
+};
+__device__ __forceinline__ int piece(int tile, int s) { return tile < 2 ? tile : 2 * tile - 2 + s; }
+
+struct Delta {
+    xl_delta_args a;
+    int first, chunks;          // of every sequence in this launch
+    bool full_keys;             // dk is DK
+    const float *carried;       // states between launches [batch, heads, dk, dv], or NULL
+    float *carry;
+};
+
+template <int DT, int DK> __device__ __forceinline__ void load_keys(const Delta &d, const typename Elem<DT>::T *row, int quad, Vec<typename Elem<DT>::T, 8> (&out)[DK / 32])
+{
+    typedef typename Elem<DT>::T T;
+    if (d.full_keys) {
+#pragma unroll
+        for (int s = 0; s < DK / 32; ++s) out[s] = load_vec<T, 8>(row + s * 32 + quad * 8);
+    } else {
+#pragma unroll
+        for (int s = 0; s < DK / 32; ++s) out[s] = load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
+    }
+}
+
+template <typename V> __device__ __forceinline__ float squares(V v)
+{
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)v[i], (float)v[i], s);
+    return s;
+}
+
+__device__ __forceinline__ f32x4 four(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
+
+// A chunk of a head.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
+// Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
+template <int DT, int DK>
+__global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
+{
+    typedef typename Elem<DT>::T T;
+    typedef ChunkOf<DT, DK> Chunk;
+    constexpr int KS = DK / 32, PITCH = CHUNK + 4;
+    __shared__ __align__(16) float A[CHUNK][PITCH];
+    __shared__ __align__(16) float X[CHUNK][PITCH];
+    __shared__ __align__(16) T keys[CHUNK][DK + 2];
+    __shared__ double G[CHUNK];
+    __shared__ float beta[CHUNK], inverse_k[CHUNK], inverse_q[CHUNK];
+    __shared__ int first_bad;
+    const xl_delta_args &a = d.a;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, H = (int)a.heads;
+    const long long units = a.batch * a.heads * d.chunks;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const int c = (int)(u % d.chunks), h = (int)(u / d.chunks % H), b = (int)(u / d.chunks / H), hk = h / (int)(a.heads / a.key_heads), t0 = (d.first + c) * CHUNK;
+        const int n = (slot_of(a.slots, a.nslots, b) < 0 ? 0 : length_of(a.lengths, b, (int)a.length)) - t0;        // tokens from here on
+        if (n <= 0) continue;
+        const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head + t0 * a.k_token, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head + t0 * a.q_token;
+        Chunk &out = static_cast<Chunk *>(a.workspace)[u];
+        __syncthreads();        // the unit before is done with
+        const int token = dealt(wave, col);
+        Vec<T, 8> mine[KS], query[KS];
+        load_keys<DT, DK>(d, k + min(token, n - 1) * a.k_token, quad, mine);
+        load_keys<DT, DK>(d, q + min(token, n - 1) * a.q_token, quad, query);
+        if (wave == 0) {
+            double g = lane < n ? (double)clamped(a.g[b * a.g_batch + (t0 + lane) * a.g_token + h]) : 0.;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const double more = __shfl_up(g, o);
+                g += lane >= o ? more : 0.;
+            }
+            G[lane] = g;
+            beta[lane] = lane < n ? a.beta[b * a.beta_batch + (t0 + lane) * a.beta_token + h] : 0.f;
+            if (lane == 0) first_bad = CHUNK;
+        }
+        float kk = 0.f, qq = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            kk += squares(mine[s]);
+            qq += squares(query[s]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) keys[token][s * 32 + quad * 8 + i] = mine[s][i];
+        }
+        kk += __shfl_xor(kk, 16);
+        qq += __shfl_xor(qq, 16);
+        kk += __shfl_xor(kk, 32);
+        qq += __shfl_xor(qq, 32);
+        if (quad == 0) {
+            inverse_k[token] = a.normalize ? __builtin_amdgcn_rsqf(kk + NORM_EPS) : 1.f;
+            inverse_q[token] = (a.normalize ? __builtin_amdgcn_rsqf(qq + NORM_EPS) : 1.f) * (float)a.scale;
+        }
+        // dot products of this tile's tokens with those of tile j
+        f32x4 with_k[4] = {}, with_q[4] = {};
+        Parts<Chunk::NP> mine_parts[KS], query_parts[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            mine_parts[s] = parts<DT>(mine[s]);
+            query_parts[s] = parts<DT>(query[s]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j > (wave | 1)) continue;
+            Vec<T, 8> other[KS];
+            load_keys<DT, DK>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const Parts<Chunk::NP> o = parts<DT>(other[s]);
+                with_k[j] = product(o, mine_parts[s], with_k[j]);
+                with_q[j] = product(o, query_parts[s], with_q[j]);
+            }
+        }
+        __syncthreads();
+        const double Gi = G[token];
+        const float ki = inverse_k[token] * beta[token], qi = inverse_q[token];
+        bool bad = false;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s > wave / 2) continue;
+            f32x8 p;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int j0 = s * 32 + quad * 8 + half * 4;
+                f32x4 row;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + i;
+                    const float e = exp_fast((float)(Gi - G[j])) * inverse_k[j], v = with_k[2 * s + half][i] * e * ki;
+                    bad |= j <= token && !finite(v);
+                    row[i] = j < token ? v : 0.f;
+                    p[half * 4 + i] = j <= token ? with_q[2 * s + half][i] * e * qi : 0.f;
+                }
+                *reinterpret_cast<f32x4 *>(&A[token][j0]) = row;
+            }
+            const Parts<Chunk::NY> split_p = split<Chunk::NY>(p);
+#pragma unroll
+            for (int i = 0; i < Chunk::NY; ++i) out.P[piece(wave, s)][i][lane] = split_p.p[i];
+        }
+        if (bad) atomicMin(&first_bad, token);
+        if (wave == 0) {
+            out.rows.read[lane] = exp_fast((float)G[lane]) * inverse_k[lane];
+            out.rows.beta[lane] = beta[lane];
+            out.rows.write[lane] = exp_fast((float)(G[CHUNK - 1] - G[lane])) * inverse_k[lane];
+            out.rows.query[lane] = exp_fast((float)G[lane]) * inverse_q[lane];
+            out.decay[lane] = exp_fast((float)G[CHUNK - 1]);
+        }
+        // the keys' columns, eight tokens a lane
+        for (int i = wave; i < DK / 16 * 2; i += 4) {
+            Vec<T, 8> v;
+            const int at = dealt(i / 2, col), t = i % 2 * 32 + quad * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = keys[t + e][at];
+            const Parts<Chunk::NP> kp = parts<DT>(v);
+#pragma unroll
+            for (int e = 0; e < Chunk::NP; ++e) out.keys[i / 2][i % 2][e][lane] = kp.p[e];
+        }
+        __syncthreads();
+        const int good = first_bad;
+        // T = (I + A)^-1 by blocks of 16 tokens.  On the diagonal: column col of block `wave`, one number after the other.
+        const int base = wave * 16;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == col ? 1.f : 0.f;
+#pragma unroll
+            for (int j = 0; j < i; j += 4) {
+                const f32x4 r = four(&A[base + i][base + j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < i) s = __builtin_fmaf(base + i < good ? -r[e] : 0.f, x[j + e], s);
+            }
+            x[i] = s;
+        }
+        f32x4 t[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            t[0][e] = quad == 0 ? x[e] : quad == 1 ? x[4 + e] : quad == 2 ? x[8 + e] : x[12 + e];
+            X[base + quad * 4 + e][base + col] = t[0][e];
+        }
+        __syncthreads();
+        // Below it, column of blocks `wave`: T_ij = -T_ii sum over m of A_im T_mj
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            const int row = (wave + i) * 16;
+            if (row >= CHUNK) break;
+            f32x4 sum = {};
+#pragma unroll
+            for (int m = 0; m < i; ++m) {
+                f32x4 r = four(&A[row + col][(wave + m) * 16 + quad * 4]);
+                if (row + col >= good) r = f32x4{};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(r[e], t[m][e], sum, 0, 0, 0);
+            }
+            const f32x4 diagonal = four(&X[row + col][row + quad * 4]);
+            t[i] = f32x4{};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(-diagonal[e], sum[e], t[i], 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) X[row + quad * 4 + e][base + col] = t[i][e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s > wave / 2) continue;
+            const int j0 = s * 32 + quad * 8;
+            const f32x4 lo = four(&X[token][j0]), hi = four(&X[token][j0 + 4]);
+            f32x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = j0 + e <= token ? v[e] : 0.f;        // blocks above the diagonal were never written
+                if (token >= good && j0 + e == token) v[e] = __builtin_nanf("");
+            }
+            const Parts<3> p = split<3>(v);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) out.T[piece(wave, s)][e][lane] = p.p[e];
+        }
+    }
+}
+
+// 16 columns of a head's states through the chunks of a sequence, four waves: wave w has the states' rows w DK / 4 ... in its registers, and makes the rows of its token tile w in between.  What the waves
+// need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
+// Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
+template <int DT, int DK>
+__global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
+{
+    typedef typename Elem<DT>::T T;
+    typedef ChunkOf<DT, DK> Chunk;
+    constexpr int KS = DK / 32, TW = DK / 64, NP = Chunk::NP, NY = Chunk::NY;
+    __shared__ bf16x8 states[KS][3][64], right[2][3][64], read[2][NY][64], wrote[2][3][64];
+    __shared__ int first_bad[2][16];
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const xl_delta_args &a = d.a;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, length = (int)a.length;
+    const int u = neighbours_together(blockIdx.x, gridDim.x), tile = u % tiles, h = u / tiles % H, b = u / tiles / H, hk = h / (int)(a.heads / a.key_heads);
+    const int j = tile * 16 + col, at_column = min(j, DV - 1);
+    const long long slot = slot_of(a.slots, a.nslots, b);
+    const int n = slot < 0 ? 0 : length_of(a.lengths, b, length), end = min((n + CHUNK - 1) / CHUNK, d.first + d.chunks);
+    T *y = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + j;
+    if (d.first == 0 && j < DV)
+        for (int t = n + threadIdx.x / 16; t < length; t += 16) y[t * a.y_token] = (T)0.f;
+    if (slot < 0) return;
+    const long long here = ((long long)b * H + h) * a.dk * DV + at_column, there = (slot * H + h) * a.dk * DV + at_column;
+    const float *from = d.first > 0 ? d.carried + here : a.state ? a.state + there : nullptr;
+    float *to = d.carry ? d.carry + here : a.new_state ? a.new_state + there : nullptr;
+    f32x4 S[TW];
+#pragma unroll
+    for (int i = 0; i < TW; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = dealt(wave * TW + i, quad * 4 + e);
+            S[i][e] = from && row < a.dk ? from[(long long)row * DV] : 0.f;
+        }
+    if (threadIdx.x < 32) first_bad[threadIdx.x / 16][col] = CHUNK;
+    const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head;
+    const T *v = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + at_column;
+    const Chunk *chunk = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks;
+    const int token = dealt(wave, col), rows = dealt(wave, quad * 4);       // of operands and of results
+    for (int c = d.first; c < end; ++c, ++chunk) {
+        const int t0 = c * CHUNK, odd = c % 2;
+        Vec<T, 8> key[KS], query[KS];
+        load_keys<DT, DK>(d, k + min(t0 + token, n - 1) * a.k_token, quad, key);
+        load_keys<DT, DK>(d, q + min(t0 + token, n - 1) * a.q_token, quad, query);
+        float value[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) value[e] = (float)v[min(t0 + rows + e, n - 1) * a.v_token];
+#pragma unroll
+        for (int i = 0; i < TW; ++i) {
+            const int r = wave * TW + i;
+            f32x4 rest = S[i];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const bf16x4 w = __builtin_convertvector(rest, bf16x4);
+                reinterpret_cast<bf16x4 *>(&states[r / 2][p][lane])[r % 2] = w;
+                rest -= __builtin_convertvector(w, f32x4);
+            }
+        }
+        __syncthreads();
+        f32x4 known = {}, y_states = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            Parts<3> S0;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) S0.p[p] = states[s][p][lane];
+            known = product(parts<DT>(key[s]), S0, known);
+            Parts<NY> less;
+#pragma unroll
+            for (int p = 0; p < NY; ++p) less.p[p] = S0.p[p];
+            y_states = product(parts<DT>(query[s]), less, y_states);
+        }
+        const f32x4 read_factor = four(chunk->rows.read + rows), beta = four(chunk->rows.beta + rows);
+        f32x4 side;
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            side[e] = beta[e] * (value[e] - read_factor[e] * known[e]);
+            bad |= !finite(side[e]);
+        }
+        if (threadIdx.x < 16) first_bad[!odd][col] = CHUNK;
+        if (__any(bad)) {
+#pragma unroll
+            for (int e = 3; e >= 0; --e)
+                if (!finite(side[e])) {
+                    atomicMin(&first_bad[odd][col], rows + e);
+                    side[e] = 0.f;
+                }
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const bf16x4 w = __builtin_convertvector(side, bf16x4);
+            reinterpret_cast<bf16x4 *>(&right[wave / 2][p][lane])[wave % 2] = w;
+            side -= __builtin_convertvector(w, f32x4);
+        }
+        __syncthreads();
+        f32x4 D = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s > wave / 2) continue;
+            Parts<3> t, r;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                t.p[p] = chunk->T[piece(wave, s)][p][lane];
+                r.p[p] = right[s][p][lane];
+            }
+            D = product(t, r, D);
+        }
+        bad = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= !finite(D[e]);
+        if (__any(bad)) {
+#pragma unroll
+            for (int e = 3; e >= 0; --e)
+                if (!finite(D[e])) {
+                    atomicMin(&first_bad[odd][col], rows + e);
+                    D[e] = 0.f;
+                }
+        }
+        f32x4 put = four(chunk->rows.write + rows);
+        put *= D;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            if (p < NY) {
+                const bf16x4 w = __builtin_convertvector(D, bf16x4);
+                reinterpret_cast<bf16x4 *>(&read[wave / 2][p][lane])[wave % 2] = w;
+                D -= __builtin_convertvector(w, f32x4);
+            }
+            const bf16x4 w = __builtin_convertvector(put, bf16x4);
+            reinterpret_cast<bf16x4 *>(&wrote[wave / 2][p][lane])[wave % 2] = w;
+            put -= __builtin_convertvector(w, f32x4);
+        }
+        __syncthreads();
+        const int lost = first_bad[odd][col];
+        f32x4 y_tokens = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            Parts<3> w;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) w.p[p] = wrote[s][p][lane];
+            if (s <= wave / 2) {
+                Parts<NY> p, r;
+#pragma unroll
+                for (int i = 0; i < NY; ++i) {
+                    p.p[i] = chunk->P[piece(wave, s)][i][lane];
+                    r.p[i] = read[s][i][lane];
+                }
+                y_tokens = product(p, r, y_tokens);
+            }
+            if (s == 0) {
+                const float decay = chunk->decay[lane];
+#pragma unroll
+                for (int i = 0; i < TW; ++i) S[i] *= decay;
+            }
+#pragma unroll
+            for (int i = 0; i < TW; ++i) {
+                Parts<NP> kp;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) kp.p[p] = chunk->keys[wave * TW + i][s][p][lane];
+                S[i] = product(kp, w, S[i]);
+            }
+        }
+        if (lost < CHUNK)
+#pragma unroll
+            for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        const f32x4 query_factor = four(chunk->rows.query + rows);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float out = rows + e < lost ? __builtin_fmaf(query_factor[e], y_states[e], y_tokens[e]) : __builtin_nanf("");
+            if (t0 + rows + e < n && j < DV) y[(t0 + rows + e) * a.y_token] = (T)out;
+        }
+    }
+    if (to && j < DV)
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = dealt(wave * TW + i, quad * 4 + e);
+                if (row < a.dk) to[(long long)row * DV] = S[i][e];
+            }
+}
+
+static constexpr int FEW_TOKENS = 16;
+static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
+
+template <int DT, int DK> struct ChunkPlan {
+    long long chunks, at_once, carried, bytes;      // of a sequence, in one launch, states carried between launches
+    explicit ChunkPlan(const xl_delta_args &a)
+    {
+        const long long heads = a.batch * a.heads, each = heads * (long long)sizeof(ChunkOf<DT, DK>);
+        chunks = (a.length + CHUNK - 1) / CHUNK;
+        at_once = MOST_BYTES / each;
+        at_once = at_once < 1 ? 1 : at_once > chunks ? chunks : at_once;
+        carried = at_once < chunks ? heads * a.dk * a.dv * 4 : 0;
+        bytes = at_once * each + (carried + 15) / 16 * 16;
+    }
+};
+
+template <int DT, int DK> static hipError_t launch_chunks(const xl_delta_args &a, hipStream_t s)
+{
+    const ChunkPlan<DT, DK> plan(a);
+    const int tiles = (int)((a.dv + 15) / 16);
+    float *carried = plan.carried ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + plan.at_once * a.batch * a.heads * (long long)sizeof(ChunkOf<DT, DK>)) : nullptr;
+    for (long long first = 0; first < plan.chunks; first += plan.at_once) {
+        const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
+        const Delta d = {a, (int)first, (int)some, a.dk == DK, carried, first + some < plan.chunks ? carried : nullptr};
+        hipError_t e = launch_kernel(prepare_kernel<DT, DK>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
+        if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 256, s, d, tiles);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
+static bool in_chunks(const xl_delta_args &a) { return a.length > FEW_TOKENS && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 23; }
+
 template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStream_t s)
 {
+    if (in_chunks(a)) return a.dk <= 64 ? launch_chunks<DT, 64>(a, s) : a.dk <= 128 ? launch_chunks<DT, 128>(a, s) : launch_chunks<DT, 256>(a, s);
     const int tiles = (int)((a.dv + COLS - 1) / COLS);
     const long long groups = (a.batch * a.heads * tiles + 3) / 4;
     const dim3 grid((unsigned)(groups < 1 << 20 ? groups : 1 << 20));
@@ -110,7 +564,14 @@ template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStrea
          : a.dk <= 128 ? launch_kernel(token_kernel<DT, 16>, grid, 256, s, a, tiles) : launch_kernel(token_kernel<DT, 32>, grid, 256, s, a, tiles);
 }
 
-long long delta_workspace(const xl_delta_args &) { return 0; }
+template <int DT> static long long workspace_of(const xl_delta_args &a)
+{
+    return a.dk <= 64 ? ChunkPlan<DT, 64>(a).bytes : a.dk <= 128 ? ChunkPlan<DT, 128>(a).bytes : ChunkPlan<DT, 256>(a).bytes;
+}
+long long delta_workspace(const xl_delta_args &a)
+{
+    return !in_chunks(a) ? 0 : a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
+}
 
 hipError_t launch_gated_delta_rule(const xl_delta_args &a, hipStream_t s)
 {
