@@ -116,7 +116,9 @@ __device__ __forceinline__ int dealt(int tile, int m) { return tile / 2 * 32 + m
 
 // What the first kernel leaves of a chunk: operands as the second one's lanes read them, one after the other (T and P: tiles 0 and 1 have numbers for tokens 0 to 31, tiles 2 and 3 for all),
 // and for each token what its row is multiplied with.
-template <int DT, int DK> struct ChunkOf {
+// FULL: dk is DK.  Shorter keys are laid out with the zeros that fill them up; others the second kernel reads where they lie.
+template <int DT, int DK, bool FULL> struct ChunkOf {
+    typedef Vec<typename Elem<DT>::T, 8> Run;
     static constexpr int NP = parts_of<DT>(), NY = DT == XL_F32 ? 3 : 2;        // parts of inputs, and of what only y is made of
     struct Rows {
         float read[CHUNK], beta[CHUNK], write[CHUNK], query[CHUNK];     // e^G / |k|, beta, e^(G_64 - G) / |k|, scale e^G / |q|
@@ -124,27 +126,22 @@ template <int DT, int DK> struct ChunkOf {
     bf16x8 T[6][3][64], P[6][NY][64], keys[DK / 16][2][NP][64];
     Rows rows;
     float decay[64];    // e^G_64
+    Run padded[FULL ? 0 : 2][4][DK / 32][64];       // rows of keys and queries
 };
 __device__ __forceinline__ int piece(int tile, int s) { return tile < 2 ? tile : 2 * tile - 2 + s; }
 
 struct Delta {
     xl_delta_args a;
     int first, chunks;          // of every sequence in this launch
-    bool full_keys;             // dk is DK
     const float *carried;       // states between launches [batch, heads, dk, dv], or NULL
     float *carry;
 };
 
-template <int DT, int DK> __device__ __forceinline__ void load_keys(const Delta &d, const typename Elem<DT>::T *row, int quad, Vec<typename Elem<DT>::T, 8> (&out)[DK / 32])
+template <int DK, bool FULL, typename T> __device__ __forceinline__ void load_keys(const Delta &d, const T *row, int quad, Vec<T, 8> (&out)[DK / 32])
 {
-    typedef typename Elem<DT>::T T;
-    if (d.full_keys) {
 #pragma unroll
-        for (int s = 0; s < DK / 32; ++s) out[s] = load_vec<T, 8>(row + s * 32 + quad * 8);
-    } else {
-#pragma unroll
-        for (int s = 0; s < DK / 32; ++s) out[s] = load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
-    }
+    for (int s = 0; s < DK / 32; ++s)
+        out[s] = FULL ? load_vec<T, 8>(row + s * 32 + quad * 8) : load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
 }
 
 template <typename V> __device__ __forceinline__ float squares(V v)
@@ -160,11 +157,11 @@ __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_in
 
 // A chunk of a head.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
 // Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
-template <int DT, int DK>
+template <int DT, int DK, bool FULL>
 __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
 {
     typedef typename Elem<DT>::T T;
-    typedef ChunkOf<DT, DK> Chunk;
+    typedef ChunkOf<DT, DK, FULL> Chunk;
     constexpr int KS = DK / 32, PITCH = CHUNK + 4;
     __shared__ __align__(16) float A[CHUNK][PITCH];
     __shared__ __align__(16) float X[CHUNK][PITCH];
@@ -184,8 +181,8 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         __syncthreads();        // the unit before is done with
         const int token = dealt(wave, col);
         Vec<T, 8> mine[KS], query[KS];
-        load_keys<DT, DK>(d, k + min(token, n - 1) * a.k_token, quad, mine);
-        load_keys<DT, DK>(d, q + min(token, n - 1) * a.q_token, quad, query);
+        load_keys<DK, FULL>(d, k + min(token, n - 1) * a.k_token, quad, mine);
+        load_keys<DK, FULL>(d, q + min(token, n - 1) * a.q_token, quad, query);
         if (wave == 0) {
             double g = lane < n ? (double)clamped(a.g[b * a.g_batch + (t0 + lane) * a.g_token + h]) : 0.;
 #pragma unroll
@@ -200,6 +197,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         float kk = 0.f, qq = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
+            if constexpr (!FULL) {
+                out.padded[0][wave][s][lane] = mine[s];
+                out.padded[1][wave][s][lane] = query[s];
+            }
             kk += squares(mine[s]);
             qq += squares(query[s]);
 #pragma unroll
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         for (int j = 0; j < 4; ++j) {
             if (j > (wave | 1)) continue;
             Vec<T, 8> other[KS];
-            load_keys<DT, DK>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
+            load_keys<DK, FULL>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const Parts<Chunk::NP> o = parts<DT>(other[s]);
@@ -340,14 +341,23 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
     }
 }
 
+// What is written before this is done before what is written after it: loads from LDS all at once ahead of the products, not each in front of its own.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// v is there now: what it was made of may be loaded anew into the same registers.
+__device__ __forceinline__ void settle(f32x4 &v)
+{
+    asm volatile("" : "+v"(v));
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // 16 columns of a head's states through the chunks of a sequence, four waves: wave w has the states' rows w DK / 4 ... in its registers, and makes the rows of its token tile w in between.  What the waves
 // need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
-template <int DT, int DK>
+template <int DT, int DK, bool FULL>
 __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
 {
     typedef typename Elem<DT>::T T;
-    typedef ChunkOf<DT, DK> Chunk;
+    typedef ChunkOf<DT, DK, FULL> Chunk;
     constexpr int KS = DK / 32, TW = DK / 64, NP = Chunk::NP, NY = Chunk::NY;
     __shared__ bf16x8 states[KS][3][64], right[2][3][64], read[2][NY][64], wrote[2][3][64];
     __shared__ int first_bad[2][16];
@@ -376,16 +386,62 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
     if (threadIdx.x < 32) first_bad[threadIdx.x / 16][col] = CHUNK;
     const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head;
     const T *v = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + at_column;
-    const Chunk *chunk = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks;
+    const Chunk *chunks = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks;
     const int token = dealt(wave, col), rows = dealt(wave, quad * 4);       // of operands and of results
-    for (int c = d.first; c < end; ++c, ++chunk) {
-        const int t0 = c * CHUNK, odd = c % 2;
-        Vec<T, 8> key[KS], query[KS];
-        load_keys<DT, DK>(d, k + min(t0 + token, n - 1) * a.k_token, quad, key);
-        load_keys<DT, DK>(d, q + min(t0 + token, n - 1) * a.q_token, quad, query);
-        float value[4];
+    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead.
+    Vec<T, 8> key[KS], query[KS];
+    T value[4];
+    f32x4 read_factor, beta, write_factor, query_factor;
+    float decay;
+    Parts<3> solve[2];
+    Parts<NY> causal[2];
+    Parts<NP> keys[TW][2];
+    const auto ask_first = [&](int c) {
+        const int t0 = c * CHUNK;
+        if constexpr (FULL) {
+            load_keys<DK, true>(d, k + min(t0 + token, n - 1) * a.k_token, quad, key);
+            load_keys<DK, true>(d, q + min(t0 + token, n - 1) * a.q_token, quad, query);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) value[e] = (float)v[min(t0 + rows + e, n - 1) * a.v_token];
+            for (int s = 0; s < KS; ++s) {
+                key[s] = chunks[c - d.first].padded[0][wave][s][lane];
+                query[s] = chunks[c - d.first].padded[1][wave][s][lane];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) value[e] = v[min(t0 + rows + e, n - 1) * a.v_token];
+        read_factor = four(chunks[c - d.first].rows.read + rows);
+        beta = four(chunks[c - d.first].rows.beta + rows);
+    };
+    const auto ask_second = [&](int c) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s <= wave / 2)
+#pragma unroll
+                for (int p = 0; p < 3; ++p) solve[s].p[p] = chunks[c - d.first].T[piece(wave, s)][p][lane];
+        write_factor = four(chunks[c - d.first].rows.write + rows);
+    };
+    const auto ask_third = [&](int c) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s <= wave / 2)
+#pragma unroll
+                for (int p = 0; p < NY; ++p) causal[s].p[p] = chunks[c - d.first].P[piece(wave, s)][p][lane];
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c - d.first].keys[wave * TW + i][s][p][lane];
+        }
+        decay = chunks[c - d.first].decay[lane];
+        query_factor = four(chunks[c - d.first].rows.query + rows);
+    };
+    if (d.first < end) {
+        ask_first(d.first);
+        ask_second(d.first);
+        ask_third(d.first);
+    }
+    for (int c = d.first; c < end; ++c) {
+        const int t0 = c * CHUNK, odd = c % 2, next = min(c + 1, end - 1);
 #pragma unroll
         for (int i = 0; i < TW; ++i) {
             const int r = wave * TW + i;
@@ -399,25 +455,30 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
         }
         __syncthreads();
         f32x4 known = {}, y_states = {};
+        Parts<3> S0[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) S0[s].p[p] = states[s][p][lane];
+        in_order();
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            Parts<3> S0;
-#pragma unroll
-            for (int p = 0; p < 3; ++p) S0.p[p] = states[s][p][lane];
-            known = product(parts<DT>(key[s]), S0, known);
+            known = product(parts<DT>(key[s]), S0[s], known);
             Parts<NY> less;
 #pragma unroll
-            for (int p = 0; p < NY; ++p) less.p[p] = S0.p[p];
+            for (int p = 0; p < NY; ++p) less.p[p] = S0[s].p[p];
             y_states = product(parts<DT>(query[s]), less, y_states);
         }
-        const f32x4 read_factor = four(chunk->rows.read + rows), beta = four(chunk->rows.beta + rows);
         f32x4 side;
         bool bad = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            side[e] = beta[e] * (value[e] - read_factor[e] * known[e]);
+            side[e] = beta[e] * ((float)value[e] - read_factor[e] * known[e]);
             bad |= !finite(side[e]);
         }
+        settle(side);
+        settle(y_states);
+        ask_first(next);
         if (threadIdx.x < 16) first_bad[!odd][col] = CHUNK;
         if (__any(bad)) {
 #pragma unroll
@@ -435,17 +496,14 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
         }
         __syncthreads();
         f32x4 D = {};
+        Parts<3> r[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s > wave / 2) continue;
-            Parts<3> t, r;
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                t.p[p] = chunk->T[piece(wave, s)][p][lane];
-                r.p[p] = right[s][p][lane];
-            }
-            D = product(t, r, D);
-        }
+            for (int p = 0; p < 3; ++p) r[s].p[p] = right[s][p][lane];
+        in_order();
+        D = product(solve[0], r[0], D);
+        if (wave >= 2) D = product(solve[1], r[1], D);
         bad = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) bad |= !finite(D[e]);
@@ -457,8 +515,9 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
                     D[e] = 0.f;
                 }
         }
-        f32x4 put = four(chunk->rows.write + rows);
-        put *= D;
+        f32x4 put = write_factor * D;
+        settle(put);
+        ask_second(next);
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
             if (p < NY) {
@@ -472,43 +531,36 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
         }
         __syncthreads();
         const int lost = first_bad[odd][col];
+#pragma unroll
+        for (int i = 0; i < TW; ++i) S[i] *= decay;
         f32x4 y_tokens = {};
+        Parts<3> w[2];
+        Parts<NY> now[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            Parts<3> w;
 #pragma unroll
-            for (int p = 0; p < 3; ++p) w.p[p] = wrote[s][p][lane];
-            if (s <= wave / 2) {
-                Parts<NY> p, r;
+            for (int p = 0; p < 3; ++p) w[s].p[p] = wrote[s][p][lane];
 #pragma unroll
-                for (int i = 0; i < NY; ++i) {
-                    p.p[i] = chunk->P[piece(wave, s)][i][lane];
-                    r.p[i] = read[s][i][lane];
-                }
-                y_tokens = product(p, r, y_tokens);
-            }
-            if (s == 0) {
-                const float decay = chunk->decay[lane];
-#pragma unroll
-                for (int i = 0; i < TW; ++i) S[i] *= decay;
-            }
-#pragma unroll
-            for (int i = 0; i < TW; ++i) {
-                Parts<NP> kp;
-#pragma unroll
-                for (int p = 0; p < NP; ++p) kp.p[p] = chunk->keys[wave * TW + i][s][p][lane];
-                S[i] = product(kp, w, S[i]);
-            }
+            for (int p = 0; p < NY; ++p) now[s].p[p] = read[s][p][lane];
         }
+        in_order();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < TW; ++i) S[i] = product(keys[i][s], w[s], S[i]);
+        y_tokens = product(causal[0], now[0], y_tokens);
+        if (wave >= 2) y_tokens = product(causal[1], now[1], y_tokens);
         if (lost < CHUNK)
 #pragma unroll
             for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-        const f32x4 query_factor = four(chunk->rows.query + rows);
+        f32x4 out;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float out = rows + e < lost ? __builtin_fmaf(query_factor[e], y_states[e], y_tokens[e]) : __builtin_nanf("");
-            if (t0 + rows + e < n && j < DV) y[(t0 + rows + e) * a.y_token] = (T)out;
-        }
+        for (int e = 0; e < 4; ++e) out[e] = rows + e < lost ? __builtin_fmaf(query_factor[e], y_states[e], y_tokens[e]) : __builtin_nanf("");
+        settle(out);
+        ask_third(next);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t0 + rows + e < n && j < DV) y[(t0 + rows + e) * a.y_token] = (T)out[e];
     }
     if (to && j < DV)
 #pragma unroll
@@ -523,32 +575,46 @@ __global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
 static constexpr int FEW_TOKENS = 16;
 static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
 
-template <int DT, int DK> struct ChunkPlan {
-    long long chunks, at_once, carried, bytes;      // of a sequence, in one launch, states carried between launches
-    explicit ChunkPlan(const xl_delta_args &a)
+template <int DT, int DK, bool FULL> struct Chunked {
+    static constexpr long long EACH = sizeof(ChunkOf<DT, DK, FULL>);
+    long long chunks, at_once, carried;     // of a sequence, in one launch, bytes of states between launches
+    Chunked() {}
+    explicit Chunked(const xl_delta_args &a)
     {
-        const long long heads = a.batch * a.heads, each = heads * (long long)sizeof(ChunkOf<DT, DK>);
+        const long long heads = a.batch * a.heads;
         chunks = (a.length + CHUNK - 1) / CHUNK;
-        at_once = MOST_BYTES / each;
+        at_once = MOST_BYTES / (heads * EACH);
         at_once = at_once < 1 ? 1 : at_once > chunks ? chunks : at_once;
         carried = at_once < chunks ? heads * a.dk * a.dv * 4 : 0;
-        bytes = at_once * each + (carried + 15) / 16 * 16;
+    }
+    static long long bytes(const xl_delta_args &a)
+    {
+        const Chunked plan(a);
+        return plan.at_once * a.batch * a.heads * EACH + (plan.carried + 15) / 16 * 16;
+    }
+    static hipError_t launch(const xl_delta_args &a, hipStream_t s)
+    {
+        const Chunked plan(a);
+        const int tiles = (int)((a.dv + 15) / 16);
+        float *carried = plan.carried ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + plan.at_once * a.batch * a.heads * EACH) : nullptr;
+        for (long long first = 0; first < plan.chunks; first += plan.at_once) {
+            const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
+            const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr};
+            hipError_t e = launch_kernel(prepare_kernel<DT, DK, FULL>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
+            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK, FULL>, dim3((unsigned)(a.batch * a.heads * tiles)), 256, s, d, tiles);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     }
 };
 
-template <int DT, int DK> static hipError_t launch_chunks(const xl_delta_args &a, hipStream_t s)
+// f with the chunks of these arguments
+template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
 {
-    const ChunkPlan<DT, DK> plan(a);
-    const int tiles = (int)((a.dv + 15) / 16);
-    float *carried = plan.carried ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + plan.at_once * a.batch * a.heads * (long long)sizeof(ChunkOf<DT, DK>)) : nullptr;
-    for (long long first = 0; first < plan.chunks; first += plan.at_once) {
-        const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
-        const Delta d = {a, (int)first, (int)some, a.dk == DK, carried, first + some < plan.chunks ? carried : nullptr};
-        hipError_t e = launch_kernel(prepare_kernel<DT, DK>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
-        if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 256, s, d, tiles);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    if (a.dk == 64) return f(Chunked<DT, 64, true>());
+    if (a.dk == 128) return f(Chunked<DT, 128, true>());
+    if (a.dk == 256) return f(Chunked<DT, 256, true>());
+    return a.dk < 64 ? f(Chunked<DT, 64, false>()) : a.dk < 128 ? f(Chunked<DT, 128, false>()) : f(Chunked<DT, 256, false>());
 }
 
 // Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
@@ -556,7 +622,7 @@ static bool in_chunks(const xl_delta_args &a) { return a.length > FEW_TOKENS && 
 
 template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStream_t s)
 {
-    if (in_chunks(a)) return a.dk <= 64 ? launch_chunks<DT, 64>(a, s) : a.dk <= 128 ? launch_chunks<DT, 128>(a, s) : launch_chunks<DT, 256>(a, s);
+    if (in_chunks(a)) return with_keys<DT>(a, [&](auto chunked) { return chunked.launch(a, s); });
     const int tiles = (int)((a.dv + COLS - 1) / COLS);
     const long long groups = (a.batch * a.heads * tiles + 3) / 4;
     const dim3 grid((unsigned)(groups < 1 << 20 ? groups : 1 << 20));
@@ -566,7 +632,7 @@ template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStrea
 
 template <int DT> static long long workspace_of(const xl_delta_args &a)
 {
-    return a.dk <= 64 ? ChunkPlan<DT, 64>(a).bytes : a.dk <= 128 ? ChunkPlan<DT, 128>(a).bytes : ChunkPlan<DT, 256>(a).bytes;
+    return with_keys<DT>(a, [&](auto chunked) { return chunked.bytes(a); });
 }
 long long delta_workspace(const xl_delta_args &a)
 {
