@@ -350,226 +350,275 @@ __device__ __forceinline__ void settle(f32x4 &v)
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// 16 columns of a head's states through the chunks of a sequence, four waves: wave w has the states' rows w DK / 4 ... in its registers, and makes the rows of its token tile w in between.  What the waves
-// need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
+// The rows of a chunk that exist, as a buffer: what lies past the last one comes out as zeros and is not written.
+struct Tokens {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Tokens(const void *base, long long first, int rows, long long step, int width)      // in bytes
+    {
+        const unsigned long long p = (unsigned long long)base + first * step;
+        const int lo = __builtin_amdgcn_readfirstlane((int)p), hi = __builtin_amdgcn_readfirstlane((int)(p >> 32));
+        const int bytes = (int)(min(rows, CHUNK) - 1) * (int)step + width;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo), (short)0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+    }
+    template <typename T> __device__ __forceinline__ T load(int at) const
+    {
+        if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
+        else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
+    }
+    template <typename T> __device__ __forceinline__ Vec<T, 8> load8(int at) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            return __builtin_bit_cast(Vec<T, 8>, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+        } else {
+            const f32x4 lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0)), hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 16, 0));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void store(int at, T v) const
+    {
+        if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), rsrc, at, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rsrc, at, 0, 0);
+    }
+};
+static constexpr int NOWHERE = (int)0x80000000u;        // past the end of every such buffer
+
+template <int DT, int DK, bool FULL> struct Meeting {
+    bf16x8 states[DK / 32][3][64], right[2][3][64], read[2][ChunkOf<DT, DK, FULL>::NY][64], wrote[2][3][64];
+    int first_bad[2][16];
+    // A wave's result as half of an operand of the next product.
+    template <int N> static __device__ __forceinline__ void put(bf16x8 (*to)[64], int half, int lane, f32x4 v)
+    {
+        const Parts4<N> parts = split4<N>(v);
+#pragma unroll
+        for (int p = 0; p < N; ++p) reinterpret_cast<u32x2 *>(&to[p][lane])[half] = parts.p[p];
+    }
+};
+
+// 16 columns of a head's states through the chunks of a sequence: eight waves, each with a part of the states' rows in its registers.  Four of them (SOLVES) solve for D, wave w the rows of token tile w; the
+// other four make y in between.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
-template <int DT, int DK, bool FULL>
-__global__ __launch_bounds__(256) void chunks_kernel(const Delta d, int tiles)
+template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ void go_through(const Delta &d, Meeting<DT, DK, FULL> &m, int tile, int b, int h, int wave)
 {
     typedef typename Elem<DT>::T T;
     typedef ChunkOf<DT, DK, FULL> Chunk;
-    constexpr int KS = DK / 32, TW = DK / 64, NP = Chunk::NP, NY = Chunk::NY;
-    __shared__ bf16x8 states[KS][3][64], right[2][3][64], read[2][NY][64], wrote[2][3][64];
-    __shared__ int first_bad[2][16];
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef Meeting<DT, DK, FULL> Meet;
+    constexpr bool HOLDS = DK > 64 || !SOLVES;      // a tile of 16 rows of the states
+    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = Chunk::NP, NY = Chunk::NY, SIZE = sizeof(T), NS = SOLVES ? 3 : NY;
     const xl_delta_args &a = d.a;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, length = (int)a.length;
-    const int u = neighbours_together(blockIdx.x, gridDim.x), tile = u % tiles, h = u / tiles % H, b = u / tiles / H, hk = h / (int)(a.heads / a.key_heads);
-    const int j = tile * 16 + col, at_column = min(j, DV - 1);
+    const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, hk = h / (int)(a.heads / a.key_heads);
+    const int j = tile * 16 + col, at_column = min(j, DV - 1), w4 = wave % 4, held = DK > 64 ? wave * TW : w4;
     const long long slot = slot_of(a.slots, a.nslots, b);
-    const int n = slot < 0 ? 0 : length_of(a.lengths, b, length), end = min((n + CHUNK - 1) / CHUNK, d.first + d.chunks);
-    T *y = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + j;
-    if (d.first == 0 && j < DV)
-        for (int t = n + threadIdx.x / 16; t < length; t += 16) y[t * a.y_token] = (T)0.f;
-    if (slot < 0) return;
+    const int n = length_of(a.lengths, b, (int)a.length), end = min((n + CHUNK - 1) / CHUNK, d.first + d.chunks);
     const long long here = ((long long)b * H + h) * a.dk * DV + at_column, there = (slot * H + h) * a.dk * DV + at_column;
     const float *from = d.first > 0 ? d.carried + here : a.state ? a.state + there : nullptr;
     float *to = d.carry ? d.carry + here : a.new_state ? a.new_state + there : nullptr;
-    f32x4 S[TW];
+    f32x4 S[TW] = {};
+    if constexpr (HOLDS) {
 #pragma unroll
-    for (int i = 0; i < TW; ++i)
+        for (int i = 0; i < TW; ++i) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = dealt(wave * TW + i, quad * 4 + e);
-            S[i][e] = from && row < a.dk ? from[(long long)row * DV] : 0.f;
-        }
-    if (threadIdx.x < 32) first_bad[threadIdx.x / 16][col] = CHUNK;
-    const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head;
-    const T *v = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + at_column;
-    const Chunk *chunks = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks;
-    const int token = dealt(wave, col), rows = dealt(wave, quad * 4);       // of operands and of results
-    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead.
-    Vec<T, 8> key[KS], query[KS];
-    T value[4];
-    f32x4 read_factor, beta, write_factor, query_factor;
-    float decay;
-    Parts<3> solve[2];
-    Parts<NY> causal[2];
-    Parts<NP> keys[TW][2];
-    const auto ask_first = [&](int c) {
-        const int t0 = c * CHUNK;
-        if constexpr (FULL) {
-            load_keys<DK, true>(d, k + min(t0 + token, n - 1) * a.k_token, quad, key);
-            load_keys<DK, true>(d, q + min(t0 + token, n - 1) * a.q_token, quad, query);
-        } else {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                key[s] = chunks[c - d.first].padded[0][wave][s][lane];
-                query[s] = chunks[c - d.first].padded[1][wave][s][lane];
+            for (int e = 0; e < 4; ++e) {
+                const int row = dealt(held + i, quad * 4 + e);
+                if (from && row < a.dk) S[i][e] = from[(long long)row * DV];
             }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) value[e] = v[min(t0 + rows + e, n - 1) * a.v_token];
-        read_factor = four(chunks[c - d.first].rows.read + rows);
-        beta = four(chunks[c - d.first].rows.beta + rows);
+        for (int i = 0; i < TW; ++i) settle(S[i]);
+    }
+    const T *row_base = SOLVES ? static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head : static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head;
+    const T *v_base = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head;
+    T *y_base = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head;
+    const long long row_step = (SOLVES ? a.k_token : a.q_token) * SIZE, v_step = a.v_token * SIZE, y_step = a.y_token * SIZE;
+    const Chunk *chunks = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks - d.first;
+    const int token = dealt(w4, col), rows = dealt(w4, quad * 4);       // of operands and of results
+    const int row_at = token * (int)row_step + quad * 8 * SIZE;
+    int at[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) at[e] = SOLVES ? (rows + e) * (int)v_step + at_column * SIZE : j < DV ? (rows + e) * (int)y_step + j * SIZE : NOWHERE;
+    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead.
+    Vec<T, 8> row[KS];          // of keys, or of queries
+    T value[4];
+    f32x4 row_factor, beta, write_factor;
+    float decay;
+    Parts<NS> triangle[2];      // T, or P
+    Parts<NP> keys[TW][2];
+    const auto ask_rows = [&](int c) {
+        if constexpr (FULL) {
+            const Tokens tokens(row_base, (long long)c * CHUNK, n - c * CHUNK, row_step, DK * SIZE);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) row[s] = tokens.template load8<T>(row_at + s * 32 * SIZE);
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) row[s] = chunks[c].padded[!SOLVES][w4][s][lane];
+        }
+        row_factor = four((SOLVES ? chunks[c].rows.read : chunks[c].rows.query) + rows);
+        if constexpr (SOLVES) {
+            const Tokens tokens(v_base, (long long)c * CHUNK, n - c * CHUNK, v_step, DV * SIZE);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(at[e]);
+            beta = four(chunks[c].rows.beta + rows);
+        }
     };
-    const auto ask_second = [&](int c) {
+    const auto ask_triangle = [&](int c) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-            if (s <= wave / 2)
+            if (s <= w4 / 2) {
 #pragma unroll
-                for (int p = 0; p < 3; ++p) solve[s].p[p] = chunks[c - d.first].T[piece(wave, s)][p][lane];
-        write_factor = four(chunks[c - d.first].rows.write + rows);
+                for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? chunks[c].T[piece(w4, s)][p][lane] : chunks[c].P[piece(w4, s)][p][lane];
+            }
+        if constexpr (SOLVES) write_factor = four(chunks[c].rows.write + rows);
     };
-    const auto ask_third = [&](int c) {
+    const auto ask_keys = [&](int c) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s <= wave / 2)
-#pragma unroll
-                for (int p = 0; p < NY; ++p) causal[s].p[p] = chunks[c - d.first].P[piece(wave, s)][p][lane];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int i = 0; i < TW; ++i)
 #pragma unroll
-                for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c - d.first].keys[wave * TW + i][s][p][lane];
-        }
-        decay = chunks[c - d.first].decay[lane];
-        query_factor = four(chunks[c - d.first].rows.query + rows);
+                for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c].keys[held + i][s][p][lane];
+        decay = chunks[c].decay[lane];
     };
     if (d.first < end) {
-        ask_first(d.first);
-        ask_second(d.first);
-        ask_third(d.first);
+        ask_rows(d.first);
+        ask_triangle(d.first);
+        if constexpr (HOLDS) ask_keys(d.first);
     }
     for (int c = d.first; c < end; ++c) {
-        const int t0 = c * CHUNK, odd = c % 2, next = min(c + 1, end - 1);
+        const int odd = c % 2, next = min(c + 1, end - 1);
+        // a wave's numbers that are not finite: noted for their column, and zero from here on
+        const auto clean = [&](f32x4 &v) {
+            bool bad = false;
 #pragma unroll
-        for (int i = 0; i < TW; ++i) {
-            const int r = wave * TW + i;
-            f32x4 rest = S[i];
+            for (int e = 0; e < 4; ++e) bad |= !finite(v[e]);
+            if (__any(bad)) {
 #pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                const bf16x4 w = __builtin_convertvector(rest, bf16x4);
-                reinterpret_cast<bf16x4 *>(&states[r / 2][p][lane])[r % 2] = w;
-                rest -= __builtin_convertvector(w, f32x4);
+                for (int e = 3; e >= 0; --e)
+                    if (!finite(v[e])) {
+                        atomicMin(&m.first_bad[odd][col], rows + e);
+                        v[e] = 0.f;
+                    }
+            }
+        };
+        if constexpr (HOLDS) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i) Meet::template put<3>(m.states[(held + i) / 2], (held + i) % 2, lane, S[i]);
+        }
+        __syncthreads();
+        f32x4 acc = {};         // K S0, or Q S0
+        {
+            constexpr int AT_ONCE = KS < 4 ? KS : 4;
+#pragma unroll
+            for (int s0 = 0; s0 < KS; s0 += AT_ONCE) {
+                Parts<NS> S0[AT_ONCE];
+#pragma unroll
+                for (int s = 0; s < AT_ONCE; ++s)
+#pragma unroll
+                    for (int p = 0; p < NS; ++p) S0[s].p[p] = m.states[s0 + s][p][lane];
+                in_order();
+#pragma unroll
+                for (int s = 0; s < AT_ONCE; ++s) acc = product(parts<DT>(row[s0 + s]), S0[s], acc);
             }
         }
-        __syncthreads();
-        f32x4 known = {}, y_states = {};
-        Parts<3> S0[KS];
+        acc *= row_factor;
+        if constexpr (SOLVES) {
+            f32x4 side;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int p = 0; p < 3; ++p) S0[s].p[p] = states[s][p][lane];
-        in_order();
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            known = product(parts<DT>(key[s]), S0[s], known);
-            Parts<NY> less;
-#pragma unroll
-            for (int p = 0; p < NY; ++p) less.p[p] = S0[s].p[p];
-            y_states = product(parts<DT>(query[s]), less, y_states);
-        }
-        f32x4 side;
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            side[e] = beta[e] * ((float)value[e] - read_factor[e] * known[e]);
-            bad |= !finite(side[e]);
-        }
-        settle(side);
-        settle(y_states);
-        ask_first(next);
-        if (threadIdx.x < 16) first_bad[!odd][col] = CHUNK;
-        if (__any(bad)) {
-#pragma unroll
-            for (int e = 3; e >= 0; --e)
-                if (!finite(side[e])) {
-                    atomicMin(&first_bad[odd][col], rows + e);
-                    side[e] = 0.f;
-                }
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            const bf16x4 w = __builtin_convertvector(side, bf16x4);
-            reinterpret_cast<bf16x4 *>(&right[wave / 2][p][lane])[wave % 2] = w;
-            side -= __builtin_convertvector(w, f32x4);
+            for (int e = 0; e < 4; ++e) side[e] = beta[e] * ((float)value[e] - acc[e]);
+            settle(side);
+            ask_rows(next);
+            if (threadIdx.x < 16) m.first_bad[!odd][col] = CHUNK;
+            clean(side);
+            Meet::template put<3>(m.right[w4 / 2], w4 % 2, lane, side);
+        } else {
+            settle(acc);
+            ask_rows(next);
         }
         __syncthreads();
-        f32x4 D = {};
-        Parts<3> r[2];
+        if constexpr (SOLVES) {
+            Parts<3> right[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int p = 0; p < 3; ++p) r[s].p[p] = right[s][p][lane];
-        in_order();
-        D = product(solve[0], r[0], D);
-        if (wave >= 2) D = product(solve[1], r[1], D);
-        bad = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= !finite(D[e]);
-        if (__any(bad)) {
-#pragma unroll
-            for (int e = 3; e >= 0; --e)
-                if (!finite(D[e])) {
-                    atomicMin(&first_bad[odd][col], rows + e);
-                    D[e] = 0.f;
-                }
-        }
-        f32x4 put = write_factor * D;
-        settle(put);
-        ask_second(next);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            if (p < NY) {
-                const bf16x4 w = __builtin_convertvector(D, bf16x4);
-                reinterpret_cast<bf16x4 *>(&read[wave / 2][p][lane])[wave % 2] = w;
-                D -= __builtin_convertvector(w, f32x4);
-            }
-            const bf16x4 w = __builtin_convertvector(put, bf16x4);
-            reinterpret_cast<bf16x4 *>(&wrote[wave / 2][p][lane])[wave % 2] = w;
-            put -= __builtin_convertvector(w, f32x4);
+                for (int p = 0; p < 3; ++p) right[s].p[p] = m.right[s][p][lane];
+            in_order();
+            f32x4 D = product(triangle[0], right[0], f32x4{});
+            if (w4 >= 2) D = product(triangle[1], right[1], D);
+            clean(D);
+            f32x4 weighted = write_factor * D;
+            settle(weighted);
+            ask_triangle(next);
+            Meet::template put<3>(m.wrote[w4 / 2], w4 % 2, lane, weighted);
+            Meet::template put<NY>(m.read[w4 / 2], w4 % 2, lane, D);
         }
         __syncthreads();
-        const int lost = first_bad[odd][col];
-#pragma unroll
-        for (int i = 0; i < TW; ++i) S[i] *= decay;
-        f32x4 y_tokens = {};
-        Parts<3> w[2];
-        Parts<NY> now[2];
+        const int lost = m.first_bad[odd][col];
+        Parts<3> wrote[2];
+        Parts<NY> read[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+            if constexpr (HOLDS) {
 #pragma unroll
-            for (int p = 0; p < 3; ++p) w[s].p[p] = wrote[s][p][lane];
-#pragma unroll
-            for (int p = 0; p < NY; ++p) now[s].p[p] = read[s][p][lane];
-        }
-        in_order();
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < TW; ++i) S[i] = product(keys[i][s], w[s], S[i]);
-        y_tokens = product(causal[0], now[0], y_tokens);
-        if (wave >= 2) y_tokens = product(causal[1], now[1], y_tokens);
-        if (lost < CHUNK)
-#pragma unroll
-            for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-        f32x4 out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = rows + e < lost ? __builtin_fmaf(query_factor[e], y_states[e], y_tokens[e]) : __builtin_nanf("");
-        settle(out);
-        ask_third(next);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (t0 + rows + e < n && j < DV) y[(t0 + rows + e) * a.y_token] = (T)out[e];
-    }
-    if (to && j < DV)
-#pragma unroll
-        for (int i = 0; i < TW; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = dealt(wave * TW + i, quad * 4 + e);
-                if (row < a.dk) to[(long long)row * DV] = S[i][e];
+                for (int p = 0; p < 3; ++p) wrote[s].p[p] = m.wrote[s][p][lane];
             }
+            if constexpr (!SOLVES) {
+#pragma unroll
+                for (int p = 0; p < NY; ++p) read[s].p[p] = m.read[s][p][lane];
+            }
+        }
+        if constexpr (HOLDS) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i) S[i] *= decay;
+            in_order();
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < TW; ++i) S[i] = product(keys[i][s], wrote[s], S[i]);
+            if (lost < CHUNK) {
+#pragma unroll
+                for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+            }
+#pragma unroll
+            for (int i = 0; i < TW; ++i) settle(S[i]);
+            ask_keys(next);
+        }
+        if constexpr (!SOLVES) {
+            f32x4 out = product(triangle[0], read[0], acc);
+            if (w4 >= 2) out = product(triangle[1], read[1], out);
+            settle(out);
+            ask_triangle(next);
+            const Tokens tokens(y_base, (long long)c * CHUNK, n - c * CHUNK, y_step, DV * SIZE);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tokens.store(at[e], (T)(rows + e < lost ? out[e] : __builtin_nanf("")));
+        }
+    }
+    if constexpr (HOLDS) {
+        if (to && j < DV) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = dealt(held + i, quad * 4 + e);
+                    if (row < a.dk) to[(long long)row * DV] = S[i][e];
+                }
+        }
+    }
+}
+
+template <int DT, int DK, bool FULL>
+__global__ __launch_bounds__(512) void chunks_kernel(const Delta d, int tiles)
+{
+    typedef typename Elem<DT>::T T;
+    __shared__ Meeting<DT, DK, FULL> m;
+    const xl_delta_args &a = d.a;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = (int)a.heads, length = (int)a.length;
+    const int u = neighbours_together(blockIdx.x, gridDim.x), tile = u % tiles, h = u / tiles % H, b = u / tiles / H, j = tile * 16 + threadIdx.x % 16;
+    const bool absent = slot_of(a.slots, a.nslots, b) < 0;
+    if (d.first == 0 && j < a.dv)
+        for (int t = (absent ? 0 : length_of(a.lengths, b, length)) + threadIdx.x / 16; t < length; t += 32) static_cast<T *>(a.y)[b * a.y_batch + t * a.y_token + h * a.y_head + j] = (T)0.f;
+    if (absent) return;
+    if (threadIdx.x < 32) m.first_bad[threadIdx.x / 16][threadIdx.x % 16] = CHUNK;
+    // the two halves of the waves meet at the same three barriers a chunk, each from a loop of its own: registers and loads on their way are its own too
+    if (wave < 4) go_through<DT, DK, FULL, true>(d, m, tile, b, h, wave);
+    else go_through<DT, DK, FULL, false>(d, m, tile, b, h, wave);
 }
 
 static constexpr int FEW_TOKENS = 16;
@@ -601,24 +650,35 @@ template <int DT, int DK, bool FULL> struct Chunked {
             const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
             const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr};
             hipError_t e = launch_kernel(prepare_kernel<DT, DK, FULL>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
-            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK, FULL>, dim3((unsigned)(a.batch * a.heads * tiles)), 256, s, d, tiles);
+            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK, FULL>, dim3((unsigned)(a.batch * a.heads * tiles)), 512, s, d, tiles);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;
     }
 };
 
-// f with the chunks of these arguments
+// Rows of a chunk lie within 2 GB of each other.
+static constexpr long long FURTHEST = 1ll << 22;
+
+// f with the chunks of these arguments.  Keys that do not fill their place, lie at odd addresses or far apart are laid out anew.
 template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
 {
-    if (a.dk == 64) return f(Chunked<DT, 64, true>());
-    if (a.dk == 128) return f(Chunked<DT, 128, true>());
-    if (a.dk == 256) return f(Chunked<DT, 256, true>());
-    return a.dk < 64 ? f(Chunked<DT, 64, false>()) : a.dk < 128 ? f(Chunked<DT, 128, false>()) : f(Chunked<DT, 256, false>());
+    const int size = sizeof(typename Elem<DT>::T);
+    const auto readable = [&](const void *p, long long batch, long long token, long long head) {
+        return (reinterpret_cast<uintptr_t>(p) | batch * size | token * size | head * size) % 4 == 0 && token <= FURTHEST;
+    };
+    const bool direct = readable(a.k, a.k_batch, a.k_token, a.k_head) && readable(a.q, a.q_batch, a.q_token, a.q_head);
+    if (a.dk == 64 && direct) return f(Chunked<DT, 64, true>());
+    if (a.dk == 128 && direct) return f(Chunked<DT, 128, true>());
+    if (a.dk == 256 && direct) return f(Chunked<DT, 256, true>());
+    return a.dk <= 64 ? f(Chunked<DT, 64, false>()) : a.dk <= 128 ? f(Chunked<DT, 128, false>()) : f(Chunked<DT, 256, false>());
 }
 
 // Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
-static bool in_chunks(const xl_delta_args &a) { return a.length > FEW_TOKENS && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 23; }
+static bool in_chunks(const xl_delta_args &a)
+{
+    return a.length > FEW_TOKENS && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 22 && a.v_token <= FURTHEST && a.y_token <= FURTHEST && a.dv <= FURTHEST;
+}
 
 template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStream_t s)
 {
