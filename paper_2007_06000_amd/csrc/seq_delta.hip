@@ -382,6 +382,14 @@ struct Tokens {
 };
 static constexpr int NOWHERE = (int)0x80000000u;        // past the end of every such buffer
 
+// A quad's four tokens' numbers, of which each lane has loaded that of token col % 4.
+__device__ __forceinline__ f32x4 of_tokens(float v)
+{
+    const int one = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(f32x4, u32x4{(unsigned)__builtin_amdgcn_mov_dpp(one, 0x00, 0xf, 0xf, true), (unsigned)__builtin_amdgcn_mov_dpp(one, 0x55, 0xf, 0xf, true),
+                                           (unsigned)__builtin_amdgcn_mov_dpp(one, 0xaa, 0xf, 0xf, true), (unsigned)__builtin_amdgcn_mov_dpp(one, 0xff, 0xf, 0xf, true)});
+}
+
 template <int DT, int DK, bool FULL> struct Meeting {
     bf16x8 states[DK / 32][3][64], right[2][3][64], read[2][ChunkOf<DT, DK, FULL>::NY][64], wrote[2][3][64];
     int first_bad[2][16];
@@ -435,55 +443,53 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
     int at[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) at[e] = SOLVES ? (rows + e) * (int)v_step + at_column * SIZE : j < DV ? (rows + e) * (int)y_step + j * SIZE : NOWHERE;
-    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead.
+    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead, and each part behind the product that has used it: all at once
+    // the loads would hold up the wave that issues them (a compute unit's address unit takes 16 cycles for 16 bytes a lane).
     Vec<T, 8> row[KS];          // of keys, or of queries
     T value[4];
-    f32x4 row_factor, beta, write_factor;
-    float decay;
+    float row_factor, beta, write_factor, decay;        // of one of the quad's four tokens
     Parts<NS> triangle[2];      // T, or P
     Parts<NP> keys[TW][2];
-    const auto ask_rows = [&](int c) {
-        if constexpr (FULL) {
-            const Tokens tokens(row_base, (long long)c * CHUNK, n - c * CHUNK, row_step, DK * SIZE);
-#pragma unroll
-            for (int s = 0; s < KS; ++s) row[s] = tokens.template load8<T>(row_at + s * 32 * SIZE);
-        } else {
-#pragma unroll
-            for (int s = 0; s < KS; ++s) row[s] = chunks[c].padded[!SOLVES][w4][s][lane];
-        }
-        row_factor = four((SOLVES ? chunks[c].rows.read : chunks[c].rows.query) + rows);
+    const auto tokens_of = [&](const T *base, int c, long long step, int width) { return Tokens(base, (long long)c * CHUNK, n - c * CHUNK, step, width * SIZE); };
+    const auto ask_row = [&](const Tokens &tokens, int c, int s) { row[s] = FULL ? tokens.template load8<T>(row_at + s * 32 * SIZE) : chunks[c].padded[FULL ? 0 : !SOLVES][w4][s][lane]; };
+    const auto ask_factors = [&](int c) {
+        row_factor = (SOLVES ? chunks[c].rows.read : chunks[c].rows.query)[rows + col % 4];
         if constexpr (SOLVES) {
-            const Tokens tokens(v_base, (long long)c * CHUNK, n - c * CHUNK, v_step, DV * SIZE);
+            const Tokens tokens = tokens_of(v_base, c, v_step, DV);
 #pragma unroll
             for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(at[e]);
-            beta = four(chunks[c].rows.beta + rows);
+            beta = chunks[c].rows.beta[rows + col % 4];
+            write_factor = chunks[c].rows.write[rows + col % 4];
         }
     };
-    const auto ask_triangle = [&](int c) {
+    const auto ask_triangle = [&](int c, int s) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (s <= w4 / 2) {
-#pragma unroll
-                for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? chunks[c].T[piece(w4, s)][p][lane] : chunks[c].P[piece(w4, s)][p][lane];
-            }
-        if constexpr (SOLVES) write_factor = four(chunks[c].rows.write + rows);
+        for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? chunks[c].T[piece(w4, s)][p][lane] : chunks[c].P[piece(w4, s)][p][lane];
     };
-    const auto ask_keys = [&](int c) {
+    const auto ask_keys = [&](int c, int i, int s) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < TW; ++i)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c].keys[held + i][s][p][lane];
-        decay = chunks[c].decay[lane];
+        for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c].keys[held + i][s][p][lane];
     };
     if (d.first < end) {
-        ask_rows(d.first);
-        ask_triangle(d.first);
-        if constexpr (HOLDS) ask_keys(d.first);
+        const Tokens tokens = tokens_of(row_base, d.first, row_step, DK);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) ask_row(tokens, d.first, s);
+        ask_factors(d.first);
+        ask_triangle(d.first, 0);
+        if (w4 >= 2) ask_triangle(d.first, 1);
+        if constexpr (HOLDS) {
+#pragma unroll
+            for (int i = 0; i < TW; ++i) {
+                ask_keys(d.first, i, 0);
+                ask_keys(d.first, i, 1);
+            }
+            decay = chunks[d.first].decay[lane];
+        }
     }
     for (int c = d.first; c < end; ++c) {
         const int odd = c % 2, next = min(c + 1, end - 1);
+        const Tokens next_rows = tokens_of(row_base, next, row_step, DK);
+        f32x4 weight = {};
         // a wave's numbers that are not finite: noted for their column, and zero from here on
         const auto clean = [&](f32x4 &v) {
             bool bad = false;
@@ -515,22 +521,27 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
                     for (int p = 0; p < NS; ++p) S0[s].p[p] = m.states[s0 + s][p][lane];
                 in_order();
 #pragma unroll
-                for (int s = 0; s < AT_ONCE; ++s) acc = product(parts<DT>(row[s0 + s]), S0[s], acc);
+                for (int s = 0; s < AT_ONCE; ++s) {
+                    acc = product(parts<DT>(row[s0 + s]), S0[s], acc);
+                    in_order();
+                    ask_row(next_rows, next, s0 + s);
+                    in_order();
+                }
             }
         }
-        acc *= row_factor;
+        acc *= of_tokens(row_factor);
         if constexpr (SOLVES) {
-            f32x4 side;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) side[e] = beta[e] * ((float)value[e] - acc[e]);
+            f32x4 side = of_tokens(beta) * (f32x4{(float)value[0], (float)value[1], (float)value[2], (float)value[3]} - acc);
             settle(side);
-            ask_rows(next);
+            weight = of_tokens(write_factor);
+            settle(weight);
+            ask_factors(next);
             if (threadIdx.x < 16) m.first_bad[!odd][col] = CHUNK;
             clean(side);
             Meet::template put<3>(m.right[w4 / 2], w4 % 2, lane, side);
         } else {
             settle(acc);
-            ask_rows(next);
+            ask_factors(next);
         }
         __syncthreads();
         if constexpr (SOLVES) {
@@ -541,11 +552,15 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
                 for (int p = 0; p < 3; ++p) right[s].p[p] = m.right[s][p][lane];
             in_order();
             f32x4 D = product(triangle[0], right[0], f32x4{});
-            if (w4 >= 2) D = product(triangle[1], right[1], D);
+            in_order();
+            ask_triangle(next, 0);
+            if (w4 >= 2) {
+                D = product(triangle[1], right[1], D);
+                in_order();
+                ask_triangle(next, 1);
+            }
             clean(D);
-            f32x4 weighted = write_factor * D;
-            settle(weighted);
-            ask_triangle(next);
+            const f32x4 weighted = weight * D;
             Meet::template put<3>(m.wrote[w4 / 2], w4 % 2, lane, weighted);
             Meet::template put<NY>(m.read[w4 / 2], w4 % 2, lane, D);
         }
@@ -571,20 +586,30 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int i = 0; i < TW; ++i) S[i] = product(keys[i][s], wrote[s], S[i]);
+                for (int i = 0; i < TW; ++i) {
+                    S[i] = product(keys[i][s], wrote[s], S[i]);
+                    in_order();
+                    ask_keys(next, i, s);
+                    in_order();
+                }
+            decay = chunks[next].decay[lane];
             if (lost < CHUNK) {
 #pragma unroll
                 for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
             }
 #pragma unroll
             for (int i = 0; i < TW; ++i) settle(S[i]);
-            ask_keys(next);
         }
         if constexpr (!SOLVES) {
             f32x4 out = product(triangle[0], read[0], acc);
-            if (w4 >= 2) out = product(triangle[1], read[1], out);
+            in_order();
+            ask_triangle(next, 0);
+            if (w4 >= 2) {
+                out = product(triangle[1], read[1], out);
+                in_order();
+                ask_triangle(next, 1);
+            }
             settle(out);
-            ask_triangle(next);
             const Tokens tokens(y_base, (long long)c * CHUNK, n - c * CHUNK, y_step, DV * SIZE);
 #pragma unroll
             for (int e = 0; e < 4; ++e) tokens.store(at[e], (T)(rows + e < lost ? out[e] : __builtin_nanf("")));
