@@ -114,19 +114,17 @@ __global__ __launch_bounds__(256) void token_kernel(const xl_delta_args a, int t
 static constexpr int CHUNK = 64;
 __device__ __forceinline__ int dealt(int tile, int m) { return tile / 2 * 32 + m / 4 * 8 + tile % 2 * 4 + m % 4; }
 
-// What the first kernel leaves of a chunk: operands as the second one's lanes read them, one after the other (T and P: tiles 0 and 1 have numbers for tokens 0 to 31, tiles 2 and 3 for all),
-// and for each token what its row is multiplied with.
-// FULL: dk is DK.  Shorter keys are laid out with the zeros that fill them up; others the second kernel reads where they lie.
-template <int DT, int DK, bool FULL> struct ChunkOf {
-    typedef Vec<typename Elem<DT>::T, 8> Run;
-    static constexpr int NP = parts_of<DT>(), NY = DT == XL_F32 ? 3 : 2;        // parts of inputs, and of what only y is made of
-    struct Rows {
-        float read[CHUNK], beta[CHUNK], write[CHUNK], query[CHUNK];     // e^G / |k|, beta, e^(G_64 - G) / |k|, scale e^G / |q|
-    };
-    bf16x8 T[6][3][64], P[6][NY][64], keys[DK / 16][2][NP][64];
-    Rows rows;
-    float decay[64];    // e^G_64
-    Run padded[FULL ? 0 : 2][4][DK / 32][64];       // rows of keys and queries
+// What the first kernel leaves of a chunk: operands as the second one's lanes read them, one after the other, so that each load is one run of memory (read where they lie, sixteen rows at a time, the
+// second kernel took 433 us of 2 x 12321 tokens and 16 heads instead of 368).  Keys and queries are filled up with zeros to DK, and as they came: heads that share a key head share them.
+template <int DT, int DK> struct KeyChunk {
+    Vec<typename Elem<DT>::T, 8> rows[2][4][DK / 32][64];               // keys and queries, by token tiles
+    bf16x8 columns[DK / 16][2][parts_of<DT>()][64];                     // keys, by tiles of their numbers
+};
+// T and P: tiles 0 and 1 have numbers for tokens 0 to 31, tiles 2 and 3 for all.
+template <int DT> struct HeadChunk {
+    static constexpr int NY = DT == XL_F32 ? 3 : 2;                     // parts of what only y is made of
+    bf16x8 T[6][3][64], P[6][NY][64];
+    float factors[5][64];       // of each token: e^G / |k|, beta, e^(G_64 - G) / |k|, scale e^G / |q|; and e^G_64
 };
 __device__ __forceinline__ int piece(int tile, int s) { return tile < 2 ? tile : 2 * tile - 2 + s; }
 
@@ -135,13 +133,13 @@ struct Delta {
     int first, chunks;          // of every sequence in this launch
     const float *carried;       // states between launches [batch, heads, dk, dv], or NULL
     float *carry;
+    void *keys, *heads;         // chunks [batch, key heads, chunks] and [batch, heads, chunks]
 };
 
-template <int DK, bool FULL, typename T> __device__ __forceinline__ void load_keys(const Delta &d, const T *row, int quad, Vec<T, 8> (&out)[DK / 32])
+template <int DK, typename T> __device__ __forceinline__ void load_keys(const Delta &d, const T *row, int quad, Vec<T, 8> (&out)[DK / 32])
 {
 #pragma unroll
-    for (int s = 0; s < DK / 32; ++s)
-        out[s] = FULL ? load_vec<T, 8>(row + s * 32 + quad * 8) : load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
+    for (int s = 0; s < DK / 32; ++s) out[s] = load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
 }
 
 template <typename V> __device__ __forceinline__ float squares(V v)
@@ -157,12 +155,12 @@ __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_in
 
 // A chunk of a head.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
 // Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
-template <int DT, int DK, bool FULL>
+template <int DT, int DK>
 __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
 {
     typedef typename Elem<DT>::T T;
-    typedef ChunkOf<DT, DK, FULL> Chunk;
-    constexpr int KS = DK / 32, PITCH = CHUNK + 4;
+    typedef HeadChunk<DT> Chunk;
+    constexpr int KS = DK / 32, PITCH = CHUNK + 4, NP = parts_of<DT>();
     __shared__ __align__(16) float A[CHUNK][PITCH];
     __shared__ __align__(16) float X[CHUNK][PITCH];
     __shared__ __align__(16) T keys[CHUNK][DK + 2];
@@ -177,12 +175,14 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         const int n = (slot_of(a.slots, a.nslots, b) < 0 ? 0 : length_of(a.lengths, b, (int)a.length)) - t0;        // tokens from here on
         if (n <= 0) continue;
         const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head + t0 * a.k_token, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head + t0 * a.q_token;
-        Chunk &out = static_cast<Chunk *>(a.workspace)[u];
+        Chunk &out = static_cast<Chunk *>(d.heads)[u];
+        const int group = (int)(a.heads / a.key_heads);
+        KeyChunk<DT, DK> &shared = static_cast<KeyChunk<DT, DK> *>(d.keys)[((long long)b * a.key_heads + hk) * d.chunks + c];       // by the first of the heads that share them
         __syncthreads();        // the unit before is done with
         const int token = dealt(wave, col);
         Vec<T, 8> mine[KS], query[KS];
-        load_keys<DK, FULL>(d, k + min(token, n - 1) * a.k_token, quad, mine);
-        load_keys<DK, FULL>(d, q + min(token, n - 1) * a.q_token, quad, query);
+        load_keys<DK>(d, k + min(token, n - 1) * a.k_token, quad, mine);
+        load_keys<DK>(d, q + min(token, n - 1) * a.q_token, quad, query);
         if (wave == 0) {
             double g = lane < n ? (double)clamped(a.g[b * a.g_batch + (t0 + lane) * a.g_token + h]) : 0.;
 #pragma unroll
@@ -197,9 +197,9 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         float kk = 0.f, qq = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            if constexpr (!FULL) {
-                out.padded[0][wave][s][lane] = mine[s];
-                out.padded[1][wave][s][lane] = query[s];
+            if (h % group == 0) {
+                shared.rows[0][wave][s][lane] = mine[s];
+                shared.rows[1][wave][s][lane] = query[s];
             }
             kk += squares(mine[s]);
             qq += squares(query[s]);
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         }
         // dot products of this tile's tokens with those of tile j
         f32x4 with_k[4] = {}, with_q[4] = {};
-        Parts<Chunk::NP> mine_parts[KS], query_parts[KS];
+        Parts<NP> mine_parts[KS], query_parts[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             mine_parts[s] = parts<DT>(mine[s]);
@@ -226,10 +226,10 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         for (int j = 0; j < 4; ++j) {
             if (j > (wave | 1)) continue;
             Vec<T, 8> other[KS];
-            load_keys<DK, FULL>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
+            load_keys<DK>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const Parts<Chunk::NP> o = parts<DT>(other[s]);
+                const Parts<NP> o = parts<DT>(other[s]);
                 with_k[j] = product(o, mine_parts[s], with_k[j]);
                 with_q[j] = product(o, query_parts[s], with_q[j]);
             }
@@ -262,21 +262,21 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         }
         if (bad) atomicMin(&first_bad, token);
         if (wave == 0) {
-            out.rows.read[lane] = exp_fast((float)G[lane]) * inverse_k[lane];
-            out.rows.beta[lane] = beta[lane];
-            out.rows.write[lane] = exp_fast((float)(G[CHUNK - 1] - G[lane])) * inverse_k[lane];
-            out.rows.query[lane] = exp_fast((float)G[lane]) * inverse_q[lane];
-            out.decay[lane] = exp_fast((float)G[CHUNK - 1]);
+            out.factors[0][lane] = exp_fast((float)G[lane]) * inverse_k[lane];
+            out.factors[1][lane] = beta[lane];
+            out.factors[2][lane] = exp_fast((float)(G[CHUNK - 1] - G[lane])) * inverse_k[lane];
+            out.factors[3][lane] = exp_fast((float)G[lane]) * inverse_q[lane];
+            out.factors[4][lane] = exp_fast((float)G[CHUNK - 1]);
         }
         // the keys' columns, eight tokens a lane
-        for (int i = wave; i < DK / 16 * 2; i += 4) {
+        for (int i = wave; i < (h % group == 0 ? DK / 16 * 2 : 0); i += 4) {
             Vec<T, 8> v;
             const int at = dealt(i / 2, col), t = i % 2 * 32 + quad * 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = keys[t + e][at];
-            const Parts<Chunk::NP> kp = parts<DT>(v);
+            const Parts<NP> kp = parts<DT>(v);
 #pragma unroll
-            for (int e = 0; e < Chunk::NP; ++e) out.keys[i / 2][i % 2][e][lane] = kp.p[e];
+            for (int e = 0; e < NP; ++e) shared.columns[i / 2][i % 2][e][lane] = kp.p[e];
         }
         __syncthreads();
         const int good = first_bad;
@@ -360,58 +360,50 @@ struct Tokens {
         const int bytes = (int)(min(rows, CHUNK) - 1) * (int)step + width;
         rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo), (short)0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
     }
-    template <typename T> __device__ __forceinline__ T load(int at) const
+    template <typename V> __device__ __forceinline__ V load(int at) const
     {
-        if constexpr (sizeof(T) == 2) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
-        else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
+        if constexpr (sizeof(V) == 2) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0));
+        else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0));
+        else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0));
+        else return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
     }
-    template <typename T> __device__ __forceinline__ Vec<T, 8> load8(int at) const
+    template <typename V> __device__ __forceinline__ void store(int at, V v) const
     {
-        if constexpr (sizeof(T) == 2) {
-            return __builtin_bit_cast(Vec<T, 8>, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
-        } else {
-            const f32x4 lo = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0)), hi = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 16, 0));
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-    }
-    template <typename T> __device__ __forceinline__ void store(int at, T v) const
-    {
-        if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), rsrc, at, 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rsrc, at, 0, 0);
+        if constexpr (sizeof(V) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), rsrc, at, 0, 0);
+        else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rsrc, at, 0, 0);
+        else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), rsrc, at, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rsrc, at, 0, 0);
     }
 };
 static constexpr int NOWHERE = (int)0x80000000u;        // past the end of every such buffer
 
-// A quad's four tokens' numbers, of which each lane has loaded that of token col % 4.
-__device__ __forceinline__ f32x4 of_tokens(float v)
-{
-    const int one = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(f32x4, u32x4{(unsigned)__builtin_amdgcn_mov_dpp(one, 0x00, 0xf, 0xf, true), (unsigned)__builtin_amdgcn_mov_dpp(one, 0x55, 0xf, 0xf, true),
-                                           (unsigned)__builtin_amdgcn_mov_dpp(one, 0xaa, 0xf, 0xf, true), (unsigned)__builtin_amdgcn_mov_dpp(one, 0xff, 0xf, 0xf, true)});
-}
-
-template <int DT, int DK, bool FULL> struct Meeting {
-    bf16x8 states[DK / 32][3][64], right[2][3][64], read[2][ChunkOf<DT, DK, FULL>::NY][64], wrote[2][3][64];
+// What the waves of a workgroup need of each other.
+template <int DK, typename T> struct Meeting {
+    static constexpr int PITCH = 20;        // numbers between tokens of 16: the quads' tokens lie in other banks
+    bf16x8 states[DK / 32][3][64], right[2][3][64], wrote[2][3][64];
+    f32x4 corrections[2][4][64];
+    __align__(16) T values[CHUNK][PITCH], results[CHUNK][PITCH];
+    __align__(16) float factors[5][64];
     int first_bad[2][16];
     // A wave's result as half of an operand of the next product.
-    template <int N> static __device__ __forceinline__ void put(bf16x8 (*to)[64], int half, int lane, f32x4 v)
+    static __device__ __forceinline__ void put(bf16x8 (*to)[64], int half, int lane, f32x4 v)
     {
-        const Parts4<N> parts = split4<N>(v);
+        const Parts4<3> parts = split4<3>(v);
 #pragma unroll
-        for (int p = 0; p < N; ++p) reinterpret_cast<u32x2 *>(&to[p][lane])[half] = parts.p[p];
+        for (int p = 0; p < 3; ++p) reinterpret_cast<u32x2 *>(&to[p][lane])[half] = parts.p[p];
     }
 };
 
-// 16 columns of a head's states through the chunks of a sequence: eight waves, each with a part of the states' rows in its registers.  Four of them (SOLVES) solve for D, wave w the rows of token tile w; the
-// other four make y in between.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
+// 16 columns of a head's states through the chunks of a sequence: eight waves, each with a part of the states' rows in its registers.  Four of them (SOLVES) solve for D, wave w the rows of token tile w.  The
+// other four make y, a step behind, and fetch values and factors for all.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
-template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ void go_through(const Delta &d, Meeting<DT, DK, FULL> &m, int tile, int b, int h, int wave)
+// What a chunk is made of is asked for a chunk ahead, each part behind the product that has used the registers: all at once the loads would hold up the wave that issues them (16 cycles of
+// a compute unit's address unit for 16 bytes a lane).
+template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_through(const Delta &d, Meeting<DK, typename Elem<DT>::T> &m, int tile, int b, int h, int wave)
 {
     typedef typename Elem<DT>::T T;
-    typedef ChunkOf<DT, DK, FULL> Chunk;
-    typedef Meeting<DT, DK, FULL> Meet;
-    constexpr bool HOLDS = DK > 64 || !SOLVES;      // a tile of 16 rows of the states
-    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = Chunk::NP, NY = Chunk::NY, SIZE = sizeof(T), NS = SOLVES ? 3 : NY;
+    constexpr bool HOLDS = DK > 64 || !SOLVES;      // a tile of 16 rows of the states, or more
+    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), NY = HeadChunk<DT>::NY, SIZE = sizeof(T), NS = SOLVES ? 3 : NY;
     const xl_delta_args &a = d.a;
     const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, hk = h / (int)(a.heads / a.key_heads);
     const int j = tile * 16 + col, at_column = min(j, DV - 1), w4 = wave % 4, held = DK > 64 ? wave * TW : w4;
@@ -433,69 +425,117 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
 #pragma unroll
         for (int i = 0; i < TW; ++i) settle(S[i]);
     }
-    const T *row_base = SOLVES ? static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head : static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head;
-    const T *v_base = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head;
-    T *y_base = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head;
-    const long long row_step = (SOLVES ? a.k_token : a.q_token) * SIZE, v_step = a.v_token * SIZE, y_step = a.y_token * SIZE;
-    const Chunk *chunks = static_cast<const Chunk *>(a.workspace) + ((long long)b * H + h) * d.chunks - d.first;
-    const int token = dealt(w4, col), rows = dealt(w4, quad * 4);       // of operands and of results
-    const int row_at = token * (int)row_step + quad * 8 * SIZE;
-    int at[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) at[e] = SOLVES ? (rows + e) * (int)v_step + at_column * SIZE : j < DV ? (rows + e) * (int)y_step + j * SIZE : NOWHERE;
-    // What a chunk is made of is asked for as soon as the chunk before has used the registers, most of a chunk's time ahead, and each part behind the product that has used it: all at once
-    // the loads would hold up the wave that issues them (a compute unit's address unit takes 16 cycles for 16 bytes a lane).
+    const HeadChunk<DT> *heads = static_cast<const HeadChunk<DT> *>(d.heads) + ((long long)b * H + h) * d.chunks - d.first;
+    const KeyChunk<DT, DK> *shared = static_cast<const KeyChunk<DT, DK> *>(d.keys) + ((long long)b * a.key_heads + hk) * d.chunks - d.first;
+    const int rows = dealt(w4, quad * 4);       // the four tokens of a lane's results
     Vec<T, 8> row[KS];          // of keys, or of queries
-    T value[4];
-    float row_factor, beta, write_factor, decay;        // of one of the quad's four tokens
     Parts<NS> triangle[2];      // T, or P
-    Parts<NP> keys[TW][2];
-    const auto tokens_of = [&](const T *base, int c, long long step, int width) { return Tokens(base, (long long)c * CHUNK, n - c * CHUNK, step, width * SIZE); };
-    const auto ask_row = [&](const Tokens &tokens, int c, int s) { row[s] = FULL ? tokens.template load8<T>(row_at + s * 32 * SIZE) : chunks[c].padded[FULL ? 0 : !SOLVES][w4][s][lane]; };
-    const auto ask_factors = [&](int c) {
-        row_factor = (SOLVES ? chunks[c].rows.read : chunks[c].rows.query)[rows + col % 4];
-        if constexpr (SOLVES) {
-            const Tokens tokens = tokens_of(v_base, c, v_step, DV);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(at[e]);
-            beta = chunks[c].rows.beta[rows + col % 4];
-            write_factor = chunks[c].rows.write[rows + col % 4];
-        }
-    };
+    Parts<NP> columns[TW][2];
+    const auto ask_row = [&](int c, int s) { row[s] = shared[c].rows[!SOLVES][w4][s][lane]; };
     const auto ask_triangle = [&](int c, int s) {
 #pragma unroll
-        for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? chunks[c].T[piece(w4, s)][p][lane] : chunks[c].P[piece(w4, s)][p][lane];
+        for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? heads[c].T[piece(w4, s)][p][lane] : heads[c].P[piece(w4, s)][p][lane];
     };
-    const auto ask_keys = [&](int c, int i, int s) {
+    const auto ask_columns = [&](int c, int i, int s) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) keys[i][s].p[p] = chunks[c].keys[held + i][s][p][lane];
+        for (int p = 0; p < NP; ++p) columns[i][s].p[p] = shared[c].columns[held + i][s][p][lane];
+    };
+    // The waves that do not solve: tokens' values and factors, on their way into LDS, four neighbours of a token a lane where their places allow it (one by one, in the lanes that compute with
+    // them, the four loads and four stores took a third of a chunk's time).
+    typedef Vec<T, 4> T4;
+    const T *v_base = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + tile * 16;
+    T *y_base = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + tile * 16;
+    const long long v_step = a.v_token * SIZE, y_step = a.y_token * SIZE;
+    const int width = (DV - tile * 16) * SIZE, four_at = lane % 4 * 4;
+    const bool wide_v = (((unsigned long long)v_base | (unsigned long long)v_step) & (4 * SIZE - 1)) == 0 && DV % 4 == 0;
+    const bool wide_y = (((unsigned long long)y_base | (unsigned long long)y_step) & (4 * SIZE - 1)) == 0 && DV % 4 == 0;
+    const int one_token = dealt(w4, lane / 4), v_at = four_at * SIZE < width ? one_token * (int)v_step + four_at * SIZE : NOWHERE,
+              y_at = four_at * SIZE < width ? one_token * (int)y_step + four_at * SIZE : NOWHERE;
+    T4 value;
+    float factor, last_factor;
+    const auto ask_values = [&](int c) {
+        const Tokens tokens(v_base, (long long)c * CHUNK, n - c * CHUNK, v_step, width);
+        if (wide_v) {
+            value = tokens.template load<T4>(v_at);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(j < DV ? (rows + e) * (int)v_step + col * SIZE : NOWHERE);
+        }
+        factor = heads[c].factors[w4][lane];
+        last_factor = heads[c].factors[4][lane];
+    };
+    const auto hand_over = [&] {
+        if (wide_v) {
+            *reinterpret_cast<T4 *>(&m.values[one_token][four_at]) = value;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m.values[rows + e][col] = value[e];
+        }
+        m.factors[w4][lane] = factor;
+        if (w4 == 0) m.factors[4][lane] = last_factor;
+    };
+    // y of a chunk, from Q S0 and where its column is lost
+    const auto finish = [&](int c, f32x4 out, int lost) {
+        const int next = min(c + 1, end - 1);
+        Parts<NY> D[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const f32x4 lo = m.corrections[c % 2][2 * s][lane], hi = m.corrections[c % 2][2 * s + 1][lane];
+            D[s] = split<NY>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s <= w4 / 2) {
+                Parts<NY> P;
+#pragma unroll
+                for (int p = 0; p < NY; ++p) P.p[p] = triangle[s].p[p];
+                out = product(P, D[s], out);
+                in_order();
+                ask_triangle(next, s);
+            }
+        const Tokens tokens(y_base, (long long)c * CHUNK, n - c * CHUNK, y_step, width);
+        T4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (T)(rows + e < lost ? out[e] : __builtin_nanf(""));
+        if (wide_y) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m.results[rows + e][col] = y[e];
+            wave_sync();
+            tokens.store(y_at, *reinterpret_cast<const T4 *>(&m.results[one_token][four_at]));
+            wave_sync();
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tokens.store(j < DV ? (rows + e) * (int)y_step + col * SIZE : NOWHERE, y[e]);
+        }
     };
     if (d.first < end) {
-        const Tokens tokens = tokens_of(row_base, d.first, row_step, DK);
+        if constexpr (!SOLVES) {
+            ask_values(d.first);
+            hand_over();
+            ask_values(min(d.first + 1, end - 1));
+        }
 #pragma unroll
-        for (int s = 0; s < KS; ++s) ask_row(tokens, d.first, s);
-        ask_factors(d.first);
+        for (int s = 0; s < KS; ++s) ask_row(d.first, s);
         ask_triangle(d.first, 0);
         if (w4 >= 2) ask_triangle(d.first, 1);
         if constexpr (HOLDS) {
 #pragma unroll
             for (int i = 0; i < TW; ++i) {
-                ask_keys(d.first, i, 0);
-                ask_keys(d.first, i, 1);
+                ask_columns(d.first, i, 0);
+                ask_columns(d.first, i, 1);
             }
-            decay = chunks[d.first].decay[lane];
         }
     }
+    f32x4 y_states = {};        // Q S0 of the chunk before
+    int lost = CHUNK;
     for (int c = d.first; c < end; ++c) {
         const int odd = c % 2, next = min(c + 1, end - 1);
-        const Tokens next_rows = tokens_of(row_base, next, row_step, DK);
-        f32x4 weight = {};
-        // a wave's numbers that are not finite: noted for their column, and zero from here on
+        // numbers that are not finite: noted for their column, and zero from here on
         const auto clean = [&](f32x4 &v) {
-            bool bad = false;
+            float none = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) bad |= !finite(v[e]);
-            if (__any(bad)) {
+            for (int e = 0; e < 4; ++e) none = __builtin_fmaf(v[e], 0.f, none);
+            if (__any(none != 0.f)) {       // a NaN
 #pragma unroll
                 for (int e = 3; e >= 0; --e)
                     if (!finite(v[e])) {
@@ -506,12 +546,15 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
         };
         if constexpr (HOLDS) {
 #pragma unroll
-            for (int i = 0; i < TW; ++i) Meet::template put<3>(m.states[(held + i) / 2], (held + i) % 2, lane, S[i]);
+            for (int i = 0; i < TW; ++i) m.put(m.states[(held + i) / 2], (held + i) % 2, lane, S[i]);
         }
         __syncthreads();
         f32x4 acc = {};         // K S0, or Q S0
+        const f32x4 row_factor = four(&m.factors[SOLVES ? 0 : 3][rows]), beta = four(&m.factors[1][rows]), write_factor = four(&m.factors[2][rows]);
+        const f32x4 values = {(float)m.values[rows][col], (float)m.values[rows + 1][col], (float)m.values[rows + 2][col], (float)m.values[rows + 3][col]};
+        const float decay = m.factors[4][lane];
         {
-            constexpr int AT_ONCE = KS < 4 ? KS : 4;
+            constexpr int AT_ONCE = KS < 4 ? KS : DK == 256 && NP == 3 ? 2 : 4;
 #pragma unroll
             for (int s0 = 0; s0 < KS; s0 += AT_ONCE) {
                 Parts<NS> S0[AT_ONCE];
@@ -524,24 +567,19 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
                 for (int s = 0; s < AT_ONCE; ++s) {
                     acc = product(parts<DT>(row[s0 + s]), S0[s], acc);
                     in_order();
-                    ask_row(next_rows, next, s0 + s);
+                    ask_row(next, s0 + s);
                     in_order();
                 }
             }
         }
-        acc *= of_tokens(row_factor);
+        acc *= row_factor;
         if constexpr (SOLVES) {
-            f32x4 side = of_tokens(beta) * (f32x4{(float)value[0], (float)value[1], (float)value[2], (float)value[3]} - acc);
-            settle(side);
-            weight = of_tokens(write_factor);
-            settle(weight);
-            ask_factors(next);
+            f32x4 side = beta * (values - acc);
             if (threadIdx.x < 16) m.first_bad[!odd][col] = CHUNK;
             clean(side);
-            Meet::template put<3>(m.right[w4 / 2], w4 % 2, lane, side);
+            m.put(m.right[w4 / 2], w4 % 2, lane, side);
         } else {
             settle(acc);
-            ask_factors(next);
         }
         __syncthreads();
         if constexpr (SOLVES) {
@@ -560,26 +598,22 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
                 ask_triangle(next, 1);
             }
             clean(D);
-            const f32x4 weighted = weight * D;
-            Meet::template put<3>(m.wrote[w4 / 2], w4 % 2, lane, weighted);
-            Meet::template put<NY>(m.read[w4 / 2], w4 % 2, lane, D);
+            m.put(m.wrote[w4 / 2], w4 % 2, lane, write_factor * D);
+            m.corrections[odd][w4][lane] = D;
+        } else {
+            hand_over();
+            ask_values(min(c + 2, end - 1));
+            if (c > d.first) finish(c - 1, y_states, lost);
+            y_states = acc;
         }
         __syncthreads();
-        const int lost = m.first_bad[odd][col];
-        Parts<3> wrote[2];
-        Parts<NY> read[2];
+        lost = m.first_bad[odd][col];
+        if constexpr (HOLDS) {
+            Parts<3> wrote[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if constexpr (HOLDS) {
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int p = 0; p < 3; ++p) wrote[s].p[p] = m.wrote[s][p][lane];
-            }
-            if constexpr (!SOLVES) {
-#pragma unroll
-                for (int p = 0; p < NY; ++p) read[s].p[p] = m.read[s][p][lane];
-            }
-        }
-        if constexpr (HOLDS) {
 #pragma unroll
             for (int i = 0; i < TW; ++i) S[i] *= decay;
             in_order();
@@ -587,12 +621,11 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < TW; ++i) {
-                    S[i] = product(keys[i][s], wrote[s], S[i]);
+                    S[i] = product(columns[i][s], wrote[s], S[i]);
                     in_order();
-                    ask_keys(next, i, s);
+                    ask_columns(next, i, s);
                     in_order();
                 }
-            decay = chunks[next].decay[lane];
             if (lost < CHUNK) {
 #pragma unroll
                 for (int i = 0; i < TW; ++i) S[i] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
@@ -600,20 +633,9 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
 #pragma unroll
             for (int i = 0; i < TW; ++i) settle(S[i]);
         }
-        if constexpr (!SOLVES) {
-            f32x4 out = product(triangle[0], read[0], acc);
-            in_order();
-            ask_triangle(next, 0);
-            if (w4 >= 2) {
-                out = product(triangle[1], read[1], out);
-                in_order();
-                ask_triangle(next, 1);
-            }
-            settle(out);
-            const Tokens tokens(y_base, (long long)c * CHUNK, n - c * CHUNK, y_step, DV * SIZE);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tokens.store(at[e], (T)(rows + e < lost ? out[e] : __builtin_nanf("")));
-        }
+    }
+    if constexpr (!SOLVES) {
+        if (d.first < end) finish(end - 1, y_states, lost);
     }
     if constexpr (HOLDS) {
         if (to && j < DV) {
@@ -628,11 +650,11 @@ template <int DT, int DK, bool FULL, bool SOLVES> __device__ __forceinline__ voi
     }
 }
 
-template <int DT, int DK, bool FULL>
+template <int DT, int DK>
 __global__ __launch_bounds__(512) void chunks_kernel(const Delta d, int tiles)
 {
     typedef typename Elem<DT>::T T;
-    __shared__ Meeting<DT, DK, FULL> m;
+    __shared__ Meeting<DK, T> m;
     const xl_delta_args &a = d.a;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = (int)a.heads, length = (int)a.length;
     const int u = neighbours_together(blockIdx.x, gridDim.x), tile = u % tiles, h = u / tiles % H, b = u / tiles / H, j = tile * 16 + threadIdx.x % 16;
@@ -642,40 +664,42 @@ __global__ __launch_bounds__(512) void chunks_kernel(const Delta d, int tiles)
     if (absent) return;
     if (threadIdx.x < 32) m.first_bad[threadIdx.x / 16][threadIdx.x % 16] = CHUNK;
     // the two halves of the waves meet at the same three barriers a chunk, each from a loop of its own: registers and loads on their way are its own too
-    if (wave < 4) go_through<DT, DK, FULL, true>(d, m, tile, b, h, wave);
-    else go_through<DT, DK, FULL, false>(d, m, tile, b, h, wave);
+    if (wave < 4) go_through<DT, DK, true>(d, m, tile, b, h, wave);
+    else go_through<DT, DK, false>(d, m, tile, b, h, wave);
 }
 
 static constexpr int FEW_TOKENS = 16;
 static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
 
-template <int DT, int DK, bool FULL> struct Chunked {
-    static constexpr long long EACH = sizeof(ChunkOf<DT, DK, FULL>);
-    long long chunks, at_once, carried;     // of a sequence, in one launch, bytes of states between launches
+template <int DT, int DK> struct Chunked {
+    long long chunks, at_once, of_keys, of_heads, carried;     // of a sequence, in one launch; bytes of a launch's chunks, of states between launches
     Chunked() {}
     explicit Chunked(const xl_delta_args &a)
     {
-        const long long heads = a.batch * a.heads;
+        const long long keys = a.batch * a.key_heads * (long long)sizeof(KeyChunk<DT, DK>), heads = a.batch * a.heads * (long long)sizeof(HeadChunk<DT>);
         chunks = (a.length + CHUNK - 1) / CHUNK;
-        at_once = MOST_BYTES / (heads * EACH);
+        at_once = MOST_BYTES / (keys + heads);
         at_once = at_once < 1 ? 1 : at_once > chunks ? chunks : at_once;
-        carried = at_once < chunks ? heads * a.dk * a.dv * 4 : 0;
+        of_keys = at_once * keys;
+        of_heads = at_once * heads;
+        carried = at_once < chunks ? (a.batch * a.heads * a.dk * a.dv * 4 + 15) / 16 * 16 : 0;
     }
     static long long bytes(const xl_delta_args &a)
     {
         const Chunked plan(a);
-        return plan.at_once * a.batch * a.heads * EACH + (plan.carried + 15) / 16 * 16;
+        return plan.of_keys + plan.of_heads + plan.carried;
     }
     static hipError_t launch(const xl_delta_args &a, hipStream_t s)
     {
         const Chunked plan(a);
         const int tiles = (int)((a.dv + 15) / 16);
-        float *carried = plan.carried ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + plan.at_once * a.batch * a.heads * EACH) : nullptr;
+        char *w = static_cast<char *>(a.workspace);
+        float *carried = plan.carried ? reinterpret_cast<float *>(w + plan.of_keys + plan.of_heads) : nullptr;
         for (long long first = 0; first < plan.chunks; first += plan.at_once) {
             const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
-            const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr};
-            hipError_t e = launch_kernel(prepare_kernel<DT, DK, FULL>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
-            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK, FULL>, dim3((unsigned)(a.batch * a.heads * tiles)), 512, s, d, tiles);
+            const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr, w, w + plan.of_keys};
+            hipError_t e = launch_kernel(prepare_kernel<DT, DK>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
+            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 512, s, d, tiles);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;
@@ -685,18 +709,10 @@ template <int DT, int DK, bool FULL> struct Chunked {
 // Rows of a chunk lie within 2 GB of each other.
 static constexpr long long FURTHEST = 1ll << 22;
 
-// f with the chunks of these arguments.  Keys that do not fill their place, lie at odd addresses or far apart are laid out anew.
+// f with the chunks of these arguments
 template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
 {
-    const int size = sizeof(typename Elem<DT>::T);
-    const auto readable = [&](const void *p, long long batch, long long token, long long head) {
-        return (reinterpret_cast<uintptr_t>(p) | batch * size | token * size | head * size) % 4 == 0 && token <= FURTHEST;
-    };
-    const bool direct = readable(a.k, a.k_batch, a.k_token, a.k_head) && readable(a.q, a.q_batch, a.q_token, a.q_head);
-    if (a.dk == 64 && direct) return f(Chunked<DT, 64, true>());
-    if (a.dk == 128 && direct) return f(Chunked<DT, 128, true>());
-    if (a.dk == 256 && direct) return f(Chunked<DT, 256, true>());
-    return a.dk <= 64 ? f(Chunked<DT, 64, false>()) : a.dk <= 128 ? f(Chunked<DT, 128, false>()) : f(Chunked<DT, 256, false>());
+    return a.dk <= 64 ? f(Chunked<DT, 64>()) : a.dk <= 128 ? f(Chunked<DT, 128>()) : f(Chunked<DT, 256>());
 }
 
 // Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
