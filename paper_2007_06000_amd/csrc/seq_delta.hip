@@ -136,10 +136,16 @@ struct Delta {
     void *keys, *heads;         // chunks [batch, key heads, chunks] and [batch, heads, chunks]
 };
 
-template <int DK, typename T> __device__ __forceinline__ void load_keys(const Delta &d, const T *row, int quad, Vec<T, 8> (&out)[DK / 32])
+// A row's numbers from quad * 8 on, eight of every 32.  Keys that fill their place are read without comparisons: all loads are on their way at once.
+template <int DK, typename T> __device__ __forceinline__ void load_keys(const T *row, int dk, int quad, Vec<T, 8> (&out)[DK / 32])
 {
+    if (dk == DK) {
 #pragma unroll
-    for (int s = 0; s < DK / 32; ++s) out[s] = load_some<T, 8>(row + s * 32 + quad * 8, (int)d.a.dk - (s * 32 + quad * 8));
+        for (int s = 0; s < DK / 32; ++s) out[s] = load_vec<T, 8>(row + s * 32 + quad * 8);
+    } else {
+#pragma unroll
+        for (int s = 0; s < DK / 32; ++s) out[s] = load_some<T, 8>(row + s * 32 + quad * 8, dk - (s * 32 + quad * 8));
+    }
 }
 
 template <typename V> __device__ __forceinline__ float squares(V v)
@@ -156,14 +162,19 @@ __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_in
 // A chunk of a head.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
 // Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
 template <int DT, int DK>
-__global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
+__global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>() * DK < 512 ? 2 : 1) void prepare_kernel(const Delta d)
 {
     typedef typename Elem<DT>::T T;
     typedef HeadChunk<DT> Chunk;
     constexpr int KS = DK / 32, PITCH = CHUNK + 4, NP = parts_of<DT>();
+    constexpr int KEYS_PITCH = DK + 16 / sizeof(T);
     __shared__ __align__(16) float A[CHUNK][PITCH];
-    __shared__ __align__(16) float X[CHUNK][PITCH];
-    __shared__ __align__(16) T keys[CHUNK][DK + 2];
+    __shared__ __align__(16) union {            // T is made when the keys have been used
+        T keys[CHUNK][KEYS_PITCH];
+        float X[CHUNK][PITCH];
+    } room;
+    auto &keys = room.keys;
+    auto &X = room.X;
     __shared__ double G[CHUNK];
     __shared__ float beta[CHUNK], inverse_k[CHUNK], inverse_q[CHUNK];
     __shared__ int first_bad;
@@ -181,8 +192,8 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
         __syncthreads();        // the unit before is done with
         const int token = dealt(wave, col);
         Vec<T, 8> mine[KS], query[KS];
-        load_keys<DK>(d, k + min(token, n - 1) * a.k_token, quad, mine);
-        load_keys<DK>(d, q + min(token, n - 1) * a.q_token, quad, query);
+        load_keys<DK>(k + min(token, n - 1) * a.k_token, (int)a.dk, quad, mine);
+        load_keys<DK>(q + min(token, n - 1) * a.q_token, (int)a.dk, quad, query);
         if (wave == 0) {
             double g = lane < n ? (double)clamped(a.g[b * a.g_batch + (t0 + lane) * a.g_token + h]) : 0.;
 #pragma unroll
@@ -203,8 +214,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
             }
             kk += squares(mine[s]);
             qq += squares(query[s]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) keys[token][s * 32 + quad * 8 + i] = mine[s][i];
+            *reinterpret_cast<Vec<T, 8> *>(&keys[token][s * 32 + quad * 8]) = mine[s];
         }
         kk += __shfl_xor(kk, 16);
         qq += __shfl_xor(qq, 16);
@@ -214,6 +224,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
             inverse_k[token] = a.normalize ? __builtin_amdgcn_rsqf(kk + NORM_EPS) : 1.f;
             inverse_q[token] = (a.normalize ? __builtin_amdgcn_rsqf(qq + NORM_EPS) : 1.f) * (float)a.scale;
         }
+        __syncthreads();
         // dot products of this tile's tokens with those of tile j
         f32x4 with_k[4] = {}, with_q[4] = {};
         Parts<NP> mine_parts[KS], query_parts[KS];
@@ -225,16 +236,13 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Delta d)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (j > (wave | 1)) continue;
-            Vec<T, 8> other[KS];
-            load_keys<DK>(d, k + min(dealt(j, col), n - 1) * a.k_token, quad, other);
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const Parts<NP> o = parts<DT>(other[s]);
+                const Parts<NP> o = parts<DT>(*reinterpret_cast<const Vec<T, 8> *>(&keys[dealt(j, col)][s * 32 + quad * 8]));
                 with_k[j] = product(o, mine_parts[s], with_k[j]);
                 with_q[j] = product(o, query_parts[s], with_q[j]);
             }
         }
-        __syncthreads();
         const double Gi = G[token];
         const float ki = inverse_k[token] * beta[token], qi = inverse_q[token];
         bool bad = false;
