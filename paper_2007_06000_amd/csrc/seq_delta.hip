@@ -402,16 +402,19 @@ template <int DK, typename T> struct Meeting {
     }
 };
 
-// 16 columns of a head's states through the chunks of a sequence: eight waves, each with a part of the states' rows in its registers.  Four of them (SOLVES) solve for D, wave w the rows of token tile w.  The
-// other four make y, a step behind, and fetch values and factors for all.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of the system, and D.
+// 16 columns of a head's states through the chunks of a sequence: twelve waves, a third of them for each part.  SOLVE: for D, wave w the rows of token tile w.  FETCH: tokens' values and factors, on their way into LDS.
+// Both also have parts of the states' rows in their registers (FETCH alone where DK is 64).  RESULT: y, a step behind.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of
+// the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
 // What a chunk is made of is asked for a chunk ahead, each part behind the product that has used the registers: all at once the loads would hold up the wave that issues them (16 cycles of
 // a compute unit's address unit for 16 bytes a lane).
-template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_through(const Delta &d, Meeting<DK, typename Elem<DT>::T> &m, int tile, int b, int h, int wave)
+enum { SOLVE, FETCH, RESULT };
+template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(const Delta &d, Meeting<DK, typename Elem<DT>::T> &m, int tile, int b, int h, int wave)
 {
     typedef typename Elem<DT>::T T;
-    constexpr bool HOLDS = DK > 64 || !SOLVES;      // a tile of 16 rows of the states, or more
-    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), NY = HeadChunk<DT>::NY, SIZE = sizeof(T), NS = SOLVES ? 3 : NY;
+    typedef Vec<T, 4> T4;
+    constexpr bool HOLDS = ROLE == FETCH || (ROLE == SOLVE && DK > 64), READS = ROLE != FETCH;      // a tile of 16 rows of the states, or more; the states
+    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), NY = HeadChunk<DT>::NY, SIZE = sizeof(T), NS = ROLE == SOLVE ? 3 : NY;
     const xl_delta_args &a = d.a;
     const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, hk = h / (int)(a.heads / a.key_heads);
     const int j = tile * 16 + col, at_column = min(j, DV - 1), w4 = wave % 4, held = DK > 64 ? wave * TW : w4;
@@ -439,32 +442,29 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
     Vec<T, 8> row[KS];          // of keys, or of queries
     Parts<NS> triangle[2];      // T, or P
     Parts<NP> columns[TW][2];
-    const auto ask_row = [&](int c, int s) { row[s] = shared[c].rows[!SOLVES][w4][s][lane]; };
+    const auto ask_row = [&](int c, int s) { row[s] = shared[c].rows[ROLE == RESULT][w4][s][lane]; };
     const auto ask_triangle = [&](int c, int s) {
 #pragma unroll
-        for (int p = 0; p < NS; ++p) triangle[s].p[p] = SOLVES ? heads[c].T[piece(w4, s)][p][lane] : heads[c].P[piece(w4, s)][p][lane];
+        for (int p = 0; p < NS; ++p) triangle[s].p[p] = ROLE == SOLVE ? heads[c].T[piece(w4, s)][p][lane] : heads[c].P[piece(w4, s)][p][lane];
     };
     const auto ask_columns = [&](int c, int i, int s) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) columns[i][s].p[p] = shared[c].columns[held + i][s][p][lane];
     };
-    // The waves that do not solve: tokens' values and factors, on their way into LDS, four neighbours of a token a lane where their places allow it (one by one, in the lanes that compute with
-    // them, the four loads and four stores took a third of a chunk's time).
-    typedef Vec<T, 4> T4;
+    // Values and results go four neighbours of a token a lane where their places allow it (one by one, in the lanes that compute with them, four loads and four stores took a third of a
+    // chunk's time).
     const T *v_base = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + tile * 16;
     T *y_base = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + tile * 16;
     const long long v_step = a.v_token * SIZE, y_step = a.y_token * SIZE;
-    const int width = (DV - tile * 16) * SIZE, four_at = lane % 4 * 4;
+    const int width = (DV - tile * 16) * SIZE, four_at = lane % 4 * 4, one_token = dealt(w4, lane / 4);
     const bool wide_v = (((unsigned long long)v_base | (unsigned long long)v_step) & (4 * SIZE - 1)) == 0 && DV % 4 == 0;
     const bool wide_y = (((unsigned long long)y_base | (unsigned long long)y_step) & (4 * SIZE - 1)) == 0 && DV % 4 == 0;
-    const int one_token = dealt(w4, lane / 4), v_at = four_at * SIZE < width ? one_token * (int)v_step + four_at * SIZE : NOWHERE,
-              y_at = four_at * SIZE < width ? one_token * (int)y_step + four_at * SIZE : NOWHERE;
     T4 value;
     float factor, last_factor;
     const auto ask_values = [&](int c) {
         const Tokens tokens(v_base, (long long)c * CHUNK, n - c * CHUNK, v_step, width);
         if (wide_v) {
-            value = tokens.template load<T4>(v_at);
+            value = tokens.template load<T4>(four_at * SIZE < width ? one_token * (int)v_step + four_at * SIZE : NOWHERE);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(j < DV ? (rows + e) * (int)v_step + col * SIZE : NOWHERE);
@@ -482,9 +482,8 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
         m.factors[w4][lane] = factor;
         if (w4 == 0) m.factors[4][lane] = last_factor;
     };
-    // y of a chunk, from Q S0 and where its column is lost
-    const auto finish = [&](int c, f32x4 out, int lost) {
-        const int next = min(c + 1, end - 1);
+    // y of a chunk, from Q S0
+    const auto result = [&](int c, f32x4 out) {
         Parts<NY> D[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -499,8 +498,12 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
                 for (int p = 0; p < NY; ++p) P.p[p] = triangle[s].p[p];
                 out = product(P, D[s], out);
                 in_order();
-                ask_triangle(next, s);
+                ask_triangle(min(c + 1, end - 1), s);
             }
+        settle(out);
+        return out;
+    };
+    const auto store = [&](int c, f32x4 out, int lost) {
         const Tokens tokens(y_base, (long long)c * CHUNK, n - c * CHUNK, y_step, width);
         T4 y;
 #pragma unroll
@@ -509,7 +512,7 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
 #pragma unroll
             for (int e = 0; e < 4; ++e) m.results[rows + e][col] = y[e];
             wave_sync();
-            tokens.store(y_at, *reinterpret_cast<const T4 *>(&m.results[one_token][four_at]));
+            tokens.store(four_at * SIZE < width ? one_token * (int)y_step + four_at * SIZE : NOWHERE, *reinterpret_cast<const T4 *>(&m.results[one_token][four_at]));
             wave_sync();
         } else {
 #pragma unroll
@@ -517,15 +520,17 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
         }
     };
     if (d.first < end) {
-        if constexpr (!SOLVES) {
+        if constexpr (ROLE == FETCH) {
             ask_values(d.first);
             hand_over();
             ask_values(min(d.first + 1, end - 1));
         }
+        if constexpr (READS) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) ask_row(d.first, s);
-        ask_triangle(d.first, 0);
-        if (w4 >= 2) ask_triangle(d.first, 1);
+            for (int s = 0; s < KS; ++s) ask_row(d.first, s);
+            ask_triangle(d.first, 0);
+            if (w4 >= 2) ask_triangle(d.first, 1);
+        }
         if constexpr (HOLDS) {
 #pragma unroll
             for (int i = 0; i < TW; ++i) {
@@ -534,7 +539,7 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
             }
         }
     }
-    f32x4 y_states = {};        // Q S0 of the chunk before
+    f32x4 y_before = {};        // of the chunk before: Q S0, then y
     int lost = CHUNK;
     for (int c = d.first; c < end; ++c) {
         const int odd = c % 2, next = min(c + 1, end - 1);
@@ -558,10 +563,11 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
         }
         __syncthreads();
         f32x4 acc = {};         // K S0, or Q S0
-        const f32x4 row_factor = four(&m.factors[SOLVES ? 0 : 3][rows]), beta = four(&m.factors[1][rows]), write_factor = four(&m.factors[2][rows]);
-        const f32x4 values = {(float)m.values[rows][col], (float)m.values[rows + 1][col], (float)m.values[rows + 2][col], (float)m.values[rows + 3][col]};
         const float decay = m.factors[4][lane];
-        {
+        const f32x4 write_factor = four(&m.factors[2][rows]);
+        if constexpr (READS) {
+            const f32x4 row_factor = four(&m.factors[ROLE == SOLVE ? 0 : 3][rows]), beta = four(&m.factors[1][rows]);
+            const f32x4 values = {(float)m.values[rows][col], (float)m.values[rows + 1][col], (float)m.values[rows + 2][col], (float)m.values[rows + 3][col]};
             constexpr int AT_ONCE = KS < 4 ? KS : DK == 256 && NP == 3 ? 2 : 4;
 #pragma unroll
             for (int s0 = 0; s0 < KS; s0 += AT_ONCE) {
@@ -579,18 +585,18 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
                     in_order();
                 }
             }
-        }
-        acc *= row_factor;
-        if constexpr (SOLVES) {
-            f32x4 side = beta * (values - acc);
-            if (threadIdx.x < 16) m.first_bad[!odd][col] = CHUNK;
-            clean(side);
-            m.put(m.right[w4 / 2], w4 % 2, lane, side);
-        } else {
-            settle(acc);
+            acc *= row_factor;
+            if constexpr (ROLE == SOLVE) {
+                f32x4 side = beta * (values - acc);
+                if (threadIdx.x < 16) m.first_bad[!odd][col] = CHUNK;
+                clean(side);
+                m.put(m.right[w4 / 2], w4 % 2, lane, side);
+            } else {
+                settle(acc);
+            }
         }
         __syncthreads();
-        if constexpr (SOLVES) {
+        if constexpr (ROLE == SOLVE) {
             Parts<3> right[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -608,13 +614,17 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
             clean(D);
             m.put(m.wrote[w4 / 2], w4 % 2, lane, write_factor * D);
             m.corrections[odd][w4][lane] = D;
-        } else {
+        } else if constexpr (ROLE == FETCH) {
             hand_over();
             ask_values(min(c + 2, end - 1));
-            if (c > d.first) finish(c - 1, y_states, lost);
-            y_states = acc;
+        } else if (c > d.first) {
+            y_before = result(c - 1, y_before);
         }
         __syncthreads();
+        if constexpr (ROLE == RESULT) {
+            if (c > d.first) store(c - 1, y_before, lost);
+            y_before = acc;
+        }
         lost = m.first_bad[odd][col];
         if constexpr (HOLDS) {
             Parts<3> wrote[2];
@@ -642,8 +652,8 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
             for (int i = 0; i < TW; ++i) settle(S[i]);
         }
     }
-    if constexpr (!SOLVES) {
-        if (d.first < end) finish(end - 1, y_states, lost);
+    if constexpr (ROLE == RESULT) {
+        if (d.first < end) store(end - 1, result(end - 1, y_before), lost);
     }
     if constexpr (HOLDS) {
         if (to && j < DV) {
@@ -659,7 +669,7 @@ template <int DT, int DK, bool SOLVES> __device__ __forceinline__ void go_throug
 }
 
 template <int DT, int DK>
-__global__ __launch_bounds__(512) void chunks_kernel(const Delta d, int tiles)
+__global__ __launch_bounds__(768) void chunks_kernel(const Delta d, int tiles)
 {
     typedef typename Elem<DT>::T T;
     __shared__ Meeting<DK, T> m;
@@ -668,12 +678,13 @@ __global__ __launch_bounds__(512) void chunks_kernel(const Delta d, int tiles)
     const int u = neighbours_together(blockIdx.x, gridDim.x), tile = u % tiles, h = u / tiles % H, b = u / tiles / H, j = tile * 16 + threadIdx.x % 16;
     const bool absent = slot_of(a.slots, a.nslots, b) < 0;
     if (d.first == 0 && j < a.dv)
-        for (int t = (absent ? 0 : length_of(a.lengths, b, length)) + threadIdx.x / 16; t < length; t += 32) static_cast<T *>(a.y)[b * a.y_batch + t * a.y_token + h * a.y_head + j] = (T)0.f;
+        for (int t = (absent ? 0 : length_of(a.lengths, b, length)) + threadIdx.x / 16; t < length; t += 48) static_cast<T *>(a.y)[b * a.y_batch + t * a.y_token + h * a.y_head + j] = (T)0.f;
     if (absent) return;
     if (threadIdx.x < 32) m.first_bad[threadIdx.x / 16][threadIdx.x % 16] = CHUNK;
-    // the two halves of the waves meet at the same three barriers a chunk, each from a loop of its own: registers and loads on their way are its own too
-    if (wave < 4) go_through<DT, DK, true>(d, m, tile, b, h, wave);
-    else go_through<DT, DK, false>(d, m, tile, b, h, wave);
+    // the thirds meet at the same three barriers a chunk, each from a loop of its own: registers and loads on their way are its own too
+    if (wave < 4) go_through<DT, DK, SOLVE>(d, m, tile, b, h, wave);
+    else if (wave < 8) go_through<DT, DK, FETCH>(d, m, tile, b, h, wave);
+    else go_through<DT, DK, RESULT>(d, m, tile, b, h, wave);
 }
 
 static constexpr int FEW_TOKENS = 16;
@@ -707,7 +718,7 @@ template <int DT, int DK> struct Chunked {
             const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
             const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr, w, w + plan.of_keys};
             hipError_t e = launch_kernel(prepare_kernel<DT, DK>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
-            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 512, s, d, tiles);
+            if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 768, s, d, tiles);
             if (e != hipSuccess) return e;
         }
         return hipSuccess;
