@@ -27,84 +27,119 @@ __device__ __forceinline__ float clamped(float g)
 // One pass over them gives both S^T k and S^T q, from which y follows without the new states:  S'^T q = S^T q + (k.q) beta (v - S^T k).
 static constexpr int COLS = 32;
 
+// The sum over lanes whose number is the same modulo 8, without a way through LDS.
 __device__ __forceinline__ float over_rows(float s)
 {
+    s += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, s), 0x128, 0xf, 0xf, true));      // eight lanes round, of sixteen
+    unsigned at = __builtin_bit_cast(unsigned, s);
+    const auto rows = __builtin_amdgcn_permlane16_swap(at, at, false, false);
+    const unsigned r0 = rows[0], r1 = rows[1];
+    at = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1));
+    const auto halves = __builtin_amdgcn_permlane32_swap(at, at, false, false);
+    const unsigned h0 = halves[0], h1 = halves[1];
+    return __builtin_bit_cast(float, h0) + __builtin_bit_cast(float, h1);
+}
+
+// FULL: the states fill their registers, and nothing is compared.
+template <int DT, int R, bool FULL> __device__ __forceinline__ void step_through(const xl_delta_args &a, int tile, int b, int h)
+{
+    typedef typename Elem<DT>::T T;
+    typedef Vec<T, 8> T8;
+    typedef Vec<T, 4> T4;
+    const int lane = threadIdx.x % 64, DK = (int)a.dk, DV = (int)a.dv, H = (int)a.heads, length = (int)a.length, first = lane / 8 * R, hk = h / (int)(a.heads / a.key_heads);
+    const int j = tile * COLS + lane % 8 * 4, live = FULL ? 4 : DV - j;
+    const long long slot = slot_of(a.slots, a.nslots, b);
+    const int n = slot < 0 ? 0 : length_of(a.lengths, b, length);
+    T *y = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + j;
+    if (lane < 8 && live > 0)
+        for (int t = n; t < length; ++t) store_some<T, 4>(y + t * a.y_token, live, T4{});
+    if (slot < 0) return;
+    const long long at = (slot * H + h) * DK * DV + j + (long long)first * DV;
+    const T *kp = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head + first, *qp = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head + first;
+    const T *vp = static_cast<const T *>(a.v) + b * a.v_batch + h * a.v_head + j;
+    // a token's numbers are asked for a token ahead
+    T8 k8[R / 8], q8[R / 8];
+    T4 v4;
+    float g, beta;
+    const auto ask = [&](int t) {
 #pragma unroll
-    for (int o = 8; o < 64; o *= 2) s += __shfl_xor(s, o);
-    return s;
+        for (int r = 0; r < R / 8; ++r) {
+            k8[r] = FULL ? load_vec<T, 8>(kp + t * a.k_token + r * 8) : load_some<T, 8>(kp + t * a.k_token + r * 8, DK - first - r * 8);
+            q8[r] = FULL ? load_vec<T, 8>(qp + t * a.q_token + r * 8) : load_some<T, 8>(qp + t * a.q_token + r * 8, DK - first - r * 8);
+        }
+        v4 = FULL ? load_vec<T, 4>(vp + t * a.v_token) : load_some<T, 4>(vp + t * a.v_token, live);
+        g = a.g[b * a.g_batch + t * a.g_token + h];
+        beta = a.beta[b * a.beta_batch + t * a.beta_token + h];
+    };
+    if (n > 0) ask(0);
+    f32x4 S[R] = {};
+    if (a.state) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (FULL) S[r] = load_vec<float, 4>(a.state + at + (long long)r * DV);
+            else if (first + r < DK) S[r] = load_some<float, 4>(a.state + at + (long long)r * DV, live);
+        }
+    }
+    for (int t = 0; t < n; ++t) {
+        float k[R], q[R], v[4];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            k[r] = (float)k8[r / 8][r % 8];
+            q[r] = (float)q8[r / 8][r % 8];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = (float)v4[c];
+        const float decay = exp_fast(clamped(g)), step = beta;
+        if (t + 1 < n) ask(t + 1);
+        float kk = 0.f, qq = 0.f, kq = 0.f;
+        f32x4 kS = {}, qS = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            kk = __builtin_fmaf(k[r], k[r], kk);
+            qq = __builtin_fmaf(q[r], q[r], qq);
+            kq = __builtin_fmaf(k[r], q[r], kq);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                S[r][c] *= decay;
+                kS[c] = __builtin_fmaf(k[r], S[r][c], kS[c]);
+                qS[c] = __builtin_fmaf(q[r], S[r][c], qS[c]);
+            }
+        }
+        kq = over_rows(kq);
+        float nk = 1.f, nq = (float)a.scale;
+        if (a.normalize) {
+            nk = __builtin_amdgcn_rsqf(over_rows(kk) + NORM_EPS);
+            nq *= __builtin_amdgcn_rsqf(over_rows(qq) + NORM_EPS);
+        }
+        f32x4 add;
+        T4 out;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            add[c] = step * (v[c] - nk * over_rows(kS[c])) * nk;
+            out[c] = (T)(nq * __builtin_fmaf(kq, add[c], over_rows(qS[c])));
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) S[r][c] = __builtin_fmaf(k[r], add[c], S[r][c]);
+        if (lane < 8 && live > 0) store_some<T, 4>(y + t * a.y_token, live, out);
+    }
+    if (a.new_state && live > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (FULL || first + r < DK) store_some<float, 4>(a.new_state + at + (long long)r * DV, live, S[r]);
+    }
 }
 
 template <int DT, int R>
 __global__ __launch_bounds__(256) void token_kernel(const xl_delta_args a, int tiles)
 {
-    typedef typename Elem<DT>::T T;
-    const int lane = threadIdx.x % 64, DK = (int)a.dk, DV = (int)a.dv, H = (int)a.heads, length = (int)a.length, first = lane / 8 * R;
+    const int H = (int)a.heads, waves = blockDim.x / 64;
     const long long units = a.batch * a.heads * tiles;
-    for (long long unit = (long long)blockIdx.x * 4 + threadIdx.x / 64; unit < units; unit += (long long)gridDim.x * 4) {
-        const int tile = (int)(unit % tiles), h = (int)(unit / tiles % H), b = (int)(unit / tiles / H), hk = h / (int)(a.heads / a.key_heads);
-        const int j = tile * COLS + lane % 8 * 4, live = DV - j;
-        const long long slot = slot_of(a.slots, a.nslots, b);
-        const int n = slot < 0 ? 0 : length_of(a.lengths, b, length);
-        T *y = static_cast<T *>(a.y) + b * a.y_batch + h * a.y_head + j;
-        if (lane < 8 && live > 0)
-            for (int t = n; t < length; ++t) store_some<T, 4>(y + t * a.y_token, live, Vec<T, 4>{});
-        if (slot < 0) continue;
-        const long long at = (slot * H + h) * DK * DV + j;
-        f32x4 S[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) S[r] = a.state && first + r < DK ? load_some<float, 4>(a.state + at + (long long)(first + r) * DV, live) : f32x4{};
-        for (int t = 0; t < n; ++t) {
-            const T *kp = static_cast<const T *>(a.k) + b * a.k_batch + t * a.k_token + hk * a.k_head + first;
-            const T *qp = static_cast<const T *>(a.q) + b * a.q_batch + t * a.q_token + hk * a.q_head + first;
-            float k[R], q[R];
-#pragma unroll
-            for (int r = 0; r < R; r += 8) {
-                const Vec<T, 8> kv = load_some<T, 8>(kp + r, DK - first - r), qv = load_some<T, 8>(qp + r, DK - first - r);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    k[r + i] = (float)kv[i];
-                    q[r + i] = (float)qv[i];
-                }
-            }
-            const float decay = exp_fast(clamped(a.g[b * a.g_batch + t * a.g_token + h])), beta = a.beta[b * a.beta_batch + t * a.beta_token + h];
-            const Vec<T, 4> v = load_some<T, 4>(static_cast<const T *>(a.v) + b * a.v_batch + t * a.v_token + h * a.v_head + j, live);
-            float kk = 0.f, qq = 0.f, kq = 0.f;
-            f32x4 kS = {}, qS = {};
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                kk = __builtin_fmaf(k[r], k[r], kk);
-                qq = __builtin_fmaf(q[r], q[r], qq);
-                kq = __builtin_fmaf(k[r], q[r], kq);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    S[r][c] *= decay;
-                    kS[c] = __builtin_fmaf(k[r], S[r][c], kS[c]);
-                    qS[c] = __builtin_fmaf(q[r], S[r][c], qS[c]);
-                }
-            }
-            kq = over_rows(kq);
-            float nk = 1.f, nq = (float)a.scale;
-            if (a.normalize) {
-                nk = __builtin_amdgcn_rsqf(over_rows(kk) + NORM_EPS);
-                nq *= __builtin_amdgcn_rsqf(over_rows(qq) + NORM_EPS);
-            }
-            f32x4 add;
-            Vec<T, 4> out;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                add[c] = beta * ((float)v[c] - nk * over_rows(kS[c])) * nk;
-                out[c] = (T)(nq * __builtin_fmaf(kq, add[c], over_rows(qS[c])));
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) S[r][c] = __builtin_fmaf(k[r], add[c], S[r][c]);
-            if (lane < 8 && live > 0) store_some<T, 4>(y + t * a.y_token, live, out);
-        }
-        if (a.new_state && live > 0)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (first + r < DK) store_some<float, 4>(a.new_state + at + (long long)(first + r) * DV, live, S[r]);
+    for (long long unit = (long long)blockIdx.x * waves + threadIdx.x / 64; unit < units; unit += (long long)gridDim.x * waves) {
+        const int tile = (int)(unit % tiles), h = (int)(unit / tiles % H), b = (int)(unit / tiles / H);
+        if (a.dk == 8 * R && (tile + 1) * COLS <= a.dv) step_through<DT, R, true>(a, tile, b, h);
+        else step_through<DT, R, false>(a, tile, b, h);
     }
 }
 
@@ -414,6 +449,7 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
     typedef typename Elem<DT>::T T;
     typedef Vec<T, 4> T4;
     constexpr bool HOLDS = ROLE == FETCH || (ROLE == SOLVE && DK > 64), READS = ROLE != FETCH;      // a tile of 16 rows of the states, or more; the states
+    constexpr bool AHEAD = parts_of<DT>() * DK < 384, COLUMNS_AHEAD = parts_of<DT>() * DK < 768;       // there are registers for the next chunk's rows, columns
     constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), NY = HeadChunk<DT>::NY, SIZE = sizeof(T), NS = ROLE == SOLVE ? 3 : NY;
     const xl_delta_args &a = d.a;
     const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, hk = h / (int)(a.heads / a.key_heads);
@@ -527,11 +563,11 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
         }
         if constexpr (READS) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) ask_row(d.first, s);
+            for (int s = 0; s < (AHEAD ? KS : 0); ++s) ask_row(d.first, s);
             ask_triangle(d.first, 0);
             if (w4 >= 2) ask_triangle(d.first, 1);
         }
-        if constexpr (HOLDS) {
+        if constexpr (HOLDS && COLUMNS_AHEAD) {
 #pragma unroll
             for (int i = 0; i < TW; ++i) {
                 ask_columns(d.first, i, 0);
@@ -568,20 +604,22 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
         if constexpr (READS) {
             const f32x4 row_factor = four(&m.factors[ROLE == SOLVE ? 0 : 3][rows]), beta = four(&m.factors[1][rows]);
             const f32x4 values = {(float)m.values[rows][col], (float)m.values[rows + 1][col], (float)m.values[rows + 2][col], (float)m.values[rows + 3][col]};
-            constexpr int AT_ONCE = KS < 4 ? KS : DK == 256 && NP == 3 ? 2 : 4;
+            constexpr int AT_ONCE = DK == 256 || NP == 3 ? 2 : KS;
 #pragma unroll
             for (int s0 = 0; s0 < KS; s0 += AT_ONCE) {
                 Parts<NS> S0[AT_ONCE];
 #pragma unroll
-                for (int s = 0; s < AT_ONCE; ++s)
+                for (int s = 0; s < AT_ONCE; ++s) {
 #pragma unroll
                     for (int p = 0; p < NS; ++p) S0[s].p[p] = m.states[s0 + s][p][lane];
+                    if (!AHEAD) ask_row(c, s0 + s);
+                }
                 in_order();
 #pragma unroll
                 for (int s = 0; s < AT_ONCE; ++s) {
                     acc = product(parts<DT>(row[s0 + s]), S0[s], acc);
                     in_order();
-                    ask_row(next, s0 + s);
+                    if (AHEAD) ask_row(next, s0 + s);
                     in_order();
                 }
             }
@@ -639,9 +677,10 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < TW; ++i) {
+                    if (!COLUMNS_AHEAD) ask_columns(c, i, s);
                     S[i] = product(columns[i][s], wrote[s], S[i]);
                     in_order();
-                    ask_columns(next, i, s);
+                    if (COLUMNS_AHEAD) ask_columns(next, i, s);
                     in_order();
                 }
             if (lost < CHUNK) {
@@ -687,7 +726,8 @@ __global__ __launch_bounds__(768) void chunks_kernel(const Delta d, int tiles)
     else go_through<DT, DK, RESULT>(d, m, tile, b, h, wave);
 }
 
-static constexpr int FEW_TOKENS = 16;
+// Token by token a few heads take 0.5 (64 x 64) to 1 us (128 x 128) a token, in chunks 14 to 20 us up to 64 tokens; 64 sequences of 16 heads of 128 x 128 take 23 + 2.9 us a token, in chunks 150.
+static int few_tokens(const xl_delta_args &a) { return a.batch * a.heads >= 512 ? 40 : 12; }
 static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
 
 template <int DT, int DK> struct Chunked {
@@ -737,17 +777,19 @@ template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
 // Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
 static bool in_chunks(const xl_delta_args &a)
 {
-    return a.length > FEW_TOKENS && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 22 && a.v_token <= FURTHEST && a.y_token <= FURTHEST && a.dv <= FURTHEST;
+    return a.length > few_tokens(a) && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 22 && a.v_token <= FURTHEST && a.y_token <= FURTHEST && a.dv <= FURTHEST;
 }
 
 template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStream_t s)
 {
     if (in_chunks(a)) return with_keys<DT>(a, [&](auto chunked) { return chunked.launch(a, s); });
     const int tiles = (int)((a.dv + COLS - 1) / COLS);
-    const long long groups = (a.batch * a.heads * tiles + 3) / 4;
+    // few waves have a compute unit each
+    const long long units = a.batch * a.heads * tiles, waves = units <= 1024 ? 1 : 4, groups = (units + waves - 1) / waves;
     const dim3 grid((unsigned)(groups < 1 << 20 ? groups : 1 << 20));
-    return a.dk <= 64 ? launch_kernel(token_kernel<DT, 8>, grid, 256, s, a, tiles)
-         : a.dk <= 128 ? launch_kernel(token_kernel<DT, 16>, grid, 256, s, a, tiles) : launch_kernel(token_kernel<DT, 32>, grid, 256, s, a, tiles);
+    const unsigned threads = (unsigned)waves * 64;
+    return a.dk <= 64 ? launch_kernel(token_kernel<DT, 8>, grid, threads, s, a, tiles)
+         : a.dk <= 128 ? launch_kernel(token_kernel<DT, 16>, grid, threads, s, a, tiles) : launch_kernel(token_kernel<DT, 32>, grid, threads, s, a, tiles);
 }
 
 template <int DT> static long long workspace_of(const xl_delta_args &a)
