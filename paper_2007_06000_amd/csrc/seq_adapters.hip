@@ -2,9 +2,9 @@
 //
 //   out[b,t] = y[b,t] + scales[e] * up[e] (down[e] x[b,t]),  e = index[b]
 //
-// Bound by memory: x and y are read and out is written once, the adapter's matrices come from the caches.  One kernel does both products, so that the numbers between them stay in LDS: a workgroup takes
-// MT x 16 tokens of a sequence and a slice of out's columns.  Where the tiles of tokens alone do not fill the chip out is cut into slices, and each slice's workgroup makes down x again: reading x and
-// down from the cache once more on a compute unit that would have had nothing to do costs less than a second launch.
+// Bound by memory: x and y are read and out is written once, the adapter's matrices come from the caches.  A few tokens of a sequence go through one kernel, where the numbers between the products stay in LDS: out
+// is cut into slices until they fill the chip, and each slice's workgroup makes down x again, which costs less than a second launch.  More tokens take two kernels, so that both can be cut into as many parts
+// as the chip wants: of k, and of out's columns.  (In one, 2 x 12321 tokens are 386 tiles for 256 compute units: 176 us instead of 141, of which the second round half empty.)
 #include "seq_parts.h"
 
 namespace xls {
@@ -16,129 +16,299 @@ __device__ __forceinline__ long long adapter_of(const xl_adapters_args &a, int b
     return e >= 0 && e < a.adapters ? e : -1;
 }
 
-// The rows of the first product are RT x 16 ranks, its columns tokens: a lane (token, quad) gets four ranks.  Its operands are read as runs of eight numbers a lane, eight lanes' runs
-// of 64 numbers of a row behind each other: which of them meet in which operation does not matter, as long as both operands agree.
-// The second product's rows are columns of out, its columns the same tokens.  Its four row tiles of a strip of 64 are dealt so that a lane's results are 16 neighbours of a row.
-template <int DT, int MT, int RT, int W>
-__global__ __launch_bounds__(64 * W) void adapters_kernel(const xl_adapters_args a, int tiles, int slices, int strips)
-{
+// Which tokens a workgroup has: MT x 16 of sequence b from t0 on, of which the first `live` of the sequence count; and their adapter, or -1.
+struct Tile {
+    int b, t0, live;
+    long long adapter;
+    bool adapted;
+    __device__ __forceinline__ Tile(const xl_adapters_args &a, long long at, int tiles, int tokens) : b((int)(at / tiles)), t0((int)(at % tiles) * tokens)
+    {
+        live = length_of(a.lengths, b, (int)a.length);
+        adapter = adapter_of(a, b);
+        adapted = adapter >= 0 && t0 < live;
+    }
+};
+
+// The rows of the first product are RT x 16 ranks, its columns tokens: a lane (token, quad) gets four ranks.  Waves take runs of 64 numbers of k in turn; their sums meet in LDS.
+template <int DT, int MT, int RT, int W> struct First {
     typedef typename Elem<DT>::T T;
     typedef Vec<T, 8> T8;
-    constexpr int NP = parts_of<DT>(), NT = DT == XL_F32 ? 3 : 2, R = RT * 16, RK = (RT + 1) / 2, PITCH = R + 4;
-    __shared__ float part[W][MT * 16][PITCH];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16;
-    const int K = (int)a.k, N = (int)a.n, rank = (int)a.rank, length = (int)a.length;
-    const long long units = a.batch * tiles * slices;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-        const int slice = (int)(u % slices), b = (int)(u / slices / tiles), t0 = (int)(u / slices % tiles) * (MT * 16);
-        const int live = length_of(a.lengths, b, length);
-        const long long e = adapter_of(a, b);
-        Parts<NT> inner[MT][RK];
-        if (e >= 0 && t0 < live) {
-            const T *x = static_cast<const T *>(a.x) + b * a.x_batch, *down = static_cast<const T *>(a.down) + e * a.rank * a.k;
-            const T *xrow[MT], *drow[RT];
+    static constexpr int NP = parts_of<DT>(), PITCH = RT * 16 + 4;
+    float part[W][MT * 16][PITCH];
+
+    __device__ __forceinline__ void run(const xl_adapters_args &a, const Tile &tile, int begin, int end)
+    {
+        const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, rank = (int)a.rank;
+        const T *x = static_cast<const T *>(a.x) + tile.b * a.x_batch, *down = static_cast<const T *>(a.down) + tile.adapter * a.rank * a.k;
+        const T *xrow[MT], *drow[RT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) xrow[m] = x + min(t0 + m * 16 + col, live - 1) * a.x_token;
+        for (int m = 0; m < MT; ++m) xrow[m] = x + min(tile.t0 + m * 16 + col, tile.live - 1) * a.x_token;
 #pragma unroll
-            for (int r = 0; r < RT; ++r) drow[r] = down + (long long)min(r * 16 + col, rank - 1) * K;
-            f32x4 acc[MT][RT] = {};
-            const auto step = [&](auto load) {
+        for (int r = 0; r < RT; ++r) drow[r] = down + min(r * 16 + col, rank - 1) * a.k;
+        f32x4 acc[MT][RT] = {};
+        // Each half of a run is asked for again as soon as it has been used: one half's products hide the other's loads.
+        T8 xs[2][MT], ds[2][RT];
+        const auto ask = [&](int k, int half) {
+            const int at = k + half * 32 + quad * 8;
+            if (k + 64 <= end) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    Parts<NP> xs[MT];
+                for (int m = 0; m < MT; ++m) xs[half][m] = load_vec<T, 8>(xrow[m] + at);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) xs[m] = parts<DT>(load(xrow[m], half));
+                for (int r = 0; r < RT; ++r) ds[half][r] = load_vec<T, 8>(drow[r] + at);
+            } else {
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const Parts<NP> d = parts<DT>(load(drow[r], half));
+                for (int m = 0; m < MT; ++m) xs[half][m] = load_some<T, 8>(xrow[m] + at, end - at);
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) acc[m][r] = product(d, xs[m], acc[m][r]);
-                    }
-                }
-            };
-            int k = wave * 64;
-            for (; k + 64 <= K; k += W * 64) step([&](const T *row, int half) { return load_vec<T, 8>(row + k + quad * 16 + half * 8); });
-            if (k < K) step([&](const T *row, int half) { return load_some<T, 8>(row + k + quad * 16 + half * 8, K - (k + quad * 16 + half * 8)); });
-            __syncthreads();        // the unit before has been read
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&part[wave][m * 16 + col][r * 16 + quad * 4]) = acc[m][r];
-            __syncthreads();
-            const float scale = a.scales ? a.scales[e] : 1.f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < RK; ++r) {
-                    const int at = r * 32 + quad * 8;
-                    f32x8 s = {};
-                    if (at < R)
-#pragma unroll
-                        for (int w = 0; w < W; ++w) {
-                            const f32x4 *p = reinterpret_cast<const f32x4 *>(&part[w][m * 16 + col][at]);
-                            s += __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                        }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i] = at + i < rank ? s[i] * scale : 0.f;
-                    inner[m][r] = split<NT>(s);
-                }
+                for (int r = 0; r < RT; ++r) ds[half][r] = load_some<T, 8>(drow[r] + at, end - at);
+            }
+        };
+        const int first = begin + wave * 64;
+        if (first < end) {
+            ask(first, 0);
+            ask(first, 1);
         }
-        const T *up = static_cast<const T *>(a.up) + (e >= 0 ? e : 0) * a.rank * a.n;
-        for (int strip = slice * strips + wave; strip < min((slice + 1) * strips, (N + 63) / 64); strip += W) {
-            const int j = strip * 64 + quad * 16;
-            f32x4 acc[MT][4] = {};
-            T8 y[MT][2];
+        for (int k = first; k < end; k += W * 64) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                Parts<NP> x[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) x[m] = parts<DT>(xs[half][m]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const Parts<NP> d = parts<DT>(ds[half][r]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[m][r] = product(d, x[m], acc[m][r]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (k + W * 64 < end) ask(k + W * 64, half);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();        // what was there has been read
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4 *>(&part[wave][m * 16 + col][r * 16 + quad * 4]) = acc[m][r];
+        __syncthreads();
+    }
+    __device__ __forceinline__ f32x4 sum(int token, int at) const
+    {
+        f32x4 s = {};
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += *reinterpret_cast<const f32x4 *>(&part[w][token][at]);
+        return s;
+    }
+};
+
+// The second product's rows are columns of out, its columns the tokens.  Its four row tiles of a strip of 64 are dealt so that a lane's results are twice eight neighbours of a row, behind those of the quad before.
+template <int DT, int MT, int RT, int W> struct Second {
+    typedef typename Elem<DT>::T T;
+    typedef Vec<T, 8> T8;
+    static constexpr int NP = parts_of<DT>(), NT = DT == XL_F32 ? 3 : 2, RK = (RT + 1) / 2;
+    Parts<NT> inner[MT][RK];
+
+    // The sum over `parts` of of(part, token, rank): four neighbours of down x.  The numbers of a part are asked for together.
+    template <typename F> __device__ __forceinline__ void take(const xl_adapters_args &a, const Tile &tile, int parts, F of)
+    {
+        const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16;
+        const float scale = a.scales ? a.scales[tile.adapter] : 1.f;
+        f32x8 s[MT][RK] = {};
+        for (int p = 0; p < parts; ++p)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < RK; ++r)
+                    if (RT > 1 || quad < 2) s[m][r] += __builtin_shufflevector(of(p, m * 16 + col, r * 32 + quad * 8), of(p, m * 16 + col, r * 32 + quad * 8 + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < RK; ++r) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[m][r][i] = r * 32 + quad * 8 + i < a.rank ? s[m][r][i] * scale : 0.f;
+                inner[m][r] = split<NT>(s[m][r]);
+            }
+    }
+
+    // Strips begin to end.  `first` makes what `inner` is made of: their first numbers are on their way meanwhile.
+    template <typename F> __device__ __forceinline__ void run(const xl_adapters_args &a, const Tile &tile, int begin, int end, F first)
+    {
+        const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16;
+        const int N = (int)a.n, rank = (int)a.rank, length = (int)a.length, t0 = tile.t0, live = tile.live;
+        const T *up = static_cast<const T *>(a.up) + (tile.adapted ? tile.adapter : 0) * a.rank * a.n;
+        // Each strip is asked for while the one before is worked on.
+        T8 ys[MT][2], us[4][RK];
+        const auto inside = [&](int strip) { return (strip + 1) * 64 <= N; };
+        const auto ask_y = [&](int strip) {
+            const int j = strip * 64 + quad * 8;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const int t = t0 + m * 16 + col;
-                const T *row = static_cast<const T *>(a.y) + b * a.y_batch + t * a.y_token;
-                y[m][0] = t < live ? load_some<T, 8>(row + j, N - j) : T8{};
-                y[m][1] = t < live ? load_some<T, 8>(row + j + 8, N - j - 8) : T8{};
+                const T *row = static_cast<const T *>(a.y) + tile.b * a.y_batch + min(t0 + m * 16 + col, live - 1) * a.y_token + j;
+                if (inside(strip)) {
+                    ys[m][0] = load_vec<T, 8>(row);
+                    ys[m][1] = load_vec<T, 8>(row + 32);
+                } else {
+                    ys[m][0] = load_some<T, 8>(row, N - j);
+                    ys[m][1] = load_some<T, 8>(row + 32, N - j - 32);
+                }
             }
-            if (e >= 0 && t0 < live) {
+        };
+        const auto ask_up = [&](int strip) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    // row i of tile c is column 16 (i / 4) + 4 c + i % 4 of the strip
-                    const T *row = up + (long long)min(strip * 64 + col / 4 * 16 + c * 4 + col % 4, N - 1) * rank;
+            for (int c = 0; c < 4; ++c) {
+                // row i of tiles 2 s and 2 s + 1 is column 32 s + 8 (i / 4) + i % 4 (+ 4 in the second) of the strip
+                const T *row = up + (long long)min(strip * 64 + c / 2 * 32 + col / 4 * 8 + c % 2 * 4 + col % 4, N - 1) * rank;
+                if (rank == RK * 32) {
+#pragma unroll
+                    for (int r = 0; r < RK; ++r) us[c][r] = load_vec<T, 8>(row + r * 32 + quad * 8);
+                } else if (RT == 1 && rank == 16) {
+                    us[c][0] = load_vec<T, 8>(row + quad % 2 * 8);      // the upper quads' numbers meet zeros ...
+                    if (quad >= 2) us[c][0] = T8{};                     // ... and may not be infinite
+                } else {
+#pragma unroll
+                    for (int r = 0; r < RK; ++r) us[c][r] = load_some<T, 8>(row + r * 32 + quad * 8, rank - (r * 32 + quad * 8));
+                }
+            }
+        };
+        int strip = begin + wave;
+        if (strip < end && live > 0) {
+            ask_y(strip);
+            if (tile.adapted) ask_up(strip);
+        }
+        if (tile.adapted) first();
+        for (; strip < end; strip += W) {
+            const int j = strip * 64 + quad * 8, next = strip + W;
+            f32x4 acc[MT][4] = {};
+            if (tile.adapted) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int r = 0; r < RK; ++r) {
-                        const Parts<NP> w = parts<DT>(load_some<T, 8>(row + r * 32 + quad * 8, rank - (r * 32 + quad * 8)));
+                        const Parts<NP> w = parts<DT>(us[c][r]);
 #pragma unroll
                         for (int m = 0; m < MT; ++m) acc[m][c] = product(w, inner[m][r], acc[m][c]);
                     }
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (next < end) ask_up(next);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            T8 out[MT][2];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const T y = ys[m][c / 2][c % 2 * 4 + i];
+                        out[m][c / 2][c % 2 * 4 + i] = t0 + m * 16 + col >= live ? (T)0.f : tile.adapted ? (T)((float)y + acc[m][c][i]) : y;
+                    }
+            if (next < end && live > 0) ask_y(next);        // of other columns: out may be y
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const int t = t0 + m * 16 + col;
                 if (t >= length) continue;
-                T *row = static_cast<T *>(a.out) + b * a.out_batch + t * a.out_token;
-                if (e >= 0 && t < live)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[m][c / 2][c % 2 * 4 + i] = (T)((float)y[m][c / 2][c % 2 * 4 + i] + acc[m][c][i]);
-                store_some<T, 8>(row + j, N - j, y[m][0]);
-                store_some<T, 8>(row + j + 8, N - j - 8, y[m][1]);
+                T *row = static_cast<T *>(a.out) + tile.b * a.out_batch + t * a.out_token + j;
+                if (inside(strip)) {
+                    store_vec<T, 8>(row, out[m][0]);
+                    store_vec<T, 8>(row + 32, out[m][1]);
+                } else {
+                    store_some<T, 8>(row, N - j, out[m][0]);
+                    store_some<T, 8>(row + 32, N - j - 32, out[m][1]);
+                }
             }
         }
     }
+};
+
+// Few tokens: both products, for `strips` strips of out.
+template <int DT, int RT, int W>
+__global__ __launch_bounds__(64 * W) void both_kernel(const xl_adapters_args a, int slices, int strips)
+{
+    __shared__ First<DT, 1, RT, W> first;
+    for (long long u = blockIdx.x; u < a.batch * slices; u += gridDim.x) {
+        const Tile tile(a, u / slices, 1, 16);
+        const int begin = (int)(u % slices) * strips;
+        Second<DT, 1, RT, W> second;
+        second.run(a, tile, begin, min(begin + strips, ((int)a.n + 63) / 64), [&] {
+            first.run(a, tile, 0, (int)a.k);
+            second.take(a, tile, 1, [&](int, int token, int at) { return first.sum(token, at); });
+        });
+    }
 }
 
-template <int DT, int MT, int RT, int W> static hipError_t launch_tile(const xl_adapters_args &a, hipStream_t s)
+// More: the sums over `run` numbers of k of every token into the workspace [parts of k][token][rank], ...
+template <int DT, int MT, int RT, int W>
+__global__ __launch_bounds__(64 * W) void first_kernel(const xl_adapters_args a, int tiles, int parts, int run)
 {
-    const long long tiles = (a.length + MT * 16 - 1) / (MT * 16), all = (a.n + 63) / 64, most = (all + W - 1) / W;
-    long long slices = 512 / (a.batch * tiles);
-    slices = slices < 1 ? 1 : slices > most ? most : slices;
-    const long long strips = (all + slices - 1) / slices;
-    slices = (all + strips - 1) / strips;
-    const long long units = a.batch * tiles * slices;
-    return launch_kernel(adapters_kernel<DT, MT, RT, W>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 64 * W, s, a, (int)tiles, (int)slices, (int)strips);
+    __shared__ First<DT, MT, RT, W> first;
+    const int length = (int)a.length;
+    for (long long u = blockIdx.x; u < a.batch * tiles * parts; u += gridDim.x) {
+        const Tile tile(a, u / parts, tiles, MT * 16);
+        const int p = (int)(u % parts);
+        if (!tile.adapted) continue;
+        first.run(a, tile, p * run, min((p + 1) * run, (int)a.k));
+        float *out = static_cast<float *>(a.workspace) + (p * a.batch * length + (long long)tile.b * length + tile.t0) * (RT * 16);
+        for (int i = threadIdx.x; i < MT * 16 * RT * 4; i += 64 * W)
+            if (tile.t0 + i / (RT * 4) < length) *reinterpret_cast<f32x4 *>(out + i * 4) = first.sum(i / (RT * 4), i % (RT * 4) * 4);
+    }
 }
+
+// ... and the second product of what is there.
+template <int DT, int MT, int RT, int W>
+__global__ __launch_bounds__(64 * W) void second_kernel(const xl_adapters_args a, int tiles, int parts, int slices, int strips)
+{
+    const int length = (int)a.length;
+    for (long long u = blockIdx.x; u < a.batch * tiles * slices; u += gridDim.x) {
+        const Tile tile(a, u / slices, tiles, MT * 16);
+        const int begin = (int)(u % slices) * strips;
+        Second<DT, MT, RT, W> second;
+        second.run(a, tile, begin, min(begin + strips, ((int)a.n + 63) / 64), [&] {
+            second.take(a, tile, parts, [&](int p, int token, int at) {
+                return *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.workspace) + (p * a.batch * length + (long long)tile.b * length + min(tile.t0 + token, tile.live - 1)) * (RT * 16) + at);
+            });
+        });
+    }
+}
+
+static unsigned grid_of(long long units) { return (unsigned)(units < 1 << 20 ? units : 1 << 20); }
+static long long up_to(long long most, long long v) { return v < 1 ? 1 : v > most ? most : v; }
+
+// Tiles of 64 tokens, or of what the registers hold; k and out's columns in as many parts as give the chip some 1000 and 2000 workgroups, with two turns at least for each wave.
+template <int DT, int RT> struct Many {
+    static constexpr int W = 4, MT1 = DT == XL_F32 || RT == 8 ? 2 : 4, MT2 = DT == XL_F32 || RT == 8 ? 1 : 2;
+    long long tiles1, tiles2, parts, run, slices, strips;
+    explicit Many(const xl_adapters_args &a)
+    {
+        tiles1 = (a.length + MT1 * 16 - 1) / (MT1 * 16);
+        tiles2 = (a.length + MT2 * 16 - 1) / (MT2 * 16);
+        const long long turn = W * 64, all = (a.n + 63) / 64;
+        parts = up_to(up_to(16, a.k / (2 * turn)), 1024 / (a.batch * tiles1));
+        run = (a.k + parts * turn - 1) / (parts * turn) * turn;
+        parts = run > 0 ? (a.k + run - 1) / run : 0;
+        slices = up_to(up_to(all, all / (2 * W)), 4096 / (a.batch * tiles2));
+        strips = (all + slices - 1) / slices;
+        slices = (all + strips - 1) / strips;
+    }
+    static long long bytes(const xl_adapters_args &a) { return Many(a).parts * a.batch * a.length * RT * 16 * 4; }
+    static hipError_t launch(const xl_adapters_args &a, hipStream_t s)
+    {
+        const Many m(a);
+        if (m.parts > 0) {
+            const hipError_t e = launch_kernel(first_kernel<DT, MT1, RT, W>, dim3(grid_of(a.batch * m.tiles1 * m.parts)), 64 * W, s, a, (int)m.tiles1, (int)m.parts, (int)m.run);
+            if (e != hipSuccess) return e;
+        }
+        return launch_kernel(second_kernel<DT, MT2, RT, W>, dim3(grid_of(a.batch * m.tiles2 * m.slices)), 64 * W, s, a, (int)m.tiles2, (int)m.parts, (int)m.slices, (int)m.strips);
+    }
+};
 
 template <int DT, int RT> static hipError_t launch_rank(const xl_adapters_args &a, hipStream_t s)
 {
-    return a.length <= 16 ? launch_tile<DT, 1, RT, 8>(a, s) : launch_tile<DT, RT == 8 ? 2 : 4, RT, 4>(a, s);
+    if (a.length > 16) return Many<DT, RT>::launch(a, s);
+    constexpr int W = DT == XL_F32 && RT >= 4 ? 4 : 8;         // fp32's registers
+    const long long all = (a.n + 63) / 64;
+    long long slices = up_to((all + W - 1) / W, 256 / a.batch);
+    const long long strips = (all + slices - 1) / slices;
+    slices = (all + strips - 1) / strips;
+    return launch_kernel(both_kernel<DT, RT, W>, dim3(grid_of(a.batch * slices)), 64 * W, s, a, (int)slices, (int)strips);
 }
 
 template <int DT> static hipError_t launch_type(const xl_adapters_args &a, hipStream_t s)
@@ -146,7 +316,14 @@ template <int DT> static hipError_t launch_type(const xl_adapters_args &a, hipSt
     return a.rank <= 16 ? launch_rank<DT, 1>(a, s) : a.rank <= 32 ? launch_rank<DT, 2>(a, s) : a.rank <= 64 ? launch_rank<DT, 4>(a, s) : launch_rank<DT, 8>(a, s);
 }
 
-long long adapters_workspace(const xl_adapters_args &) { return 0; }
+template <int DT> static long long workspace_of(const xl_adapters_args &a)
+{
+    return a.rank <= 16 ? Many<DT, 1>::bytes(a) : a.rank <= 32 ? Many<DT, 2>::bytes(a) : a.rank <= 64 ? Many<DT, 4>::bytes(a) : Many<DT, 8>::bytes(a);
+}
+long long adapters_workspace(const xl_adapters_args &a)
+{
+    return a.length <= 16 ? 0 : a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
+}
 
 hipError_t launch_add_adapters(const xl_adapters_args &a, hipStream_t s)
 {
