@@ -2,9 +2,10 @@
 //
 //   out[b,t] = y[b,t] + scales[e] * up[e] (down[e] x[b,t]),  e = index[b]
 //
-// Bound by memory: x and y are read and out is written once, the adapter's matrices come from the caches.  A few tokens of a sequence go through one kernel, where the numbers between the products stay in LDS: out
+// Bound by memory: x and y are read and out is written once, the adapter's matrices come from the caches.  Few tokens go through one kernel, where the numbers between the products stay in LDS: out
 // is cut into slices until they fill the chip, and each slice's workgroup makes down x again, which costs less than a second launch.  More tokens take two kernels, so that both can be cut into as many parts
-// as the chip wants: of k, and of out's columns.  (In one, 2 x 12321 tokens are 386 tiles for 256 compute units: 176 us instead of 141, of which the second round half empty.)
+// as the chip wants: of k, and of out's columns.  (In one, 2 x 12321 tokens were 386 tiles of 64 for 256 compute units, the second round of them half empty: 176 us instead of 165.)
+// What is left is the way of the operands: sixteen rows at a time, 64 bytes of each, where a run of memory would be read at four times the rate.
 #include "seq_parts.h"
 
 namespace xls {
@@ -221,11 +222,11 @@ template <int DT, int MT, int RT, int W> struct Second {
 
 // Few tokens: both products, for `strips` strips of out.
 template <int DT, int RT, int W>
-__global__ __launch_bounds__(64 * W) void both_kernel(const xl_adapters_args a, int slices, int strips)
+__global__ __launch_bounds__(64 * W) void both_kernel(const xl_adapters_args a, int tiles, int slices, int strips)
 {
     __shared__ First<DT, 1, RT, W> first;
-    for (long long u = blockIdx.x; u < a.batch * slices; u += gridDim.x) {
-        const Tile tile(a, u / slices, 1, 16);
+    for (long long u = blockIdx.x; u < a.batch * tiles * slices; u += gridDim.x) {
+        const Tile tile(a, u / slices, tiles, 16);
         const int begin = (int)(u % slices) * strips;
         Second<DT, 1, RT, W> second;
         second.run(a, tile, begin, min(begin + strips, ((int)a.n + 63) / 64), [&] {
@@ -272,9 +273,10 @@ __global__ __launch_bounds__(64 * W) void second_kernel(const xl_adapters_args a
 static unsigned grid_of(long long units) { return (unsigned)(units < 1 << 20 ? units : 1 << 20); }
 static long long up_to(long long most, long long v) { return v < 1 ? 1 : v > most ? most : v; }
 
-// Tiles of 64 tokens, or of what the registers hold; k and out's columns in as many parts as give the chip some 1000 and 2000 workgroups, with two turns at least for each wave.
+// Tiles of 64 and 32 tokens, or of what the registers hold; k and out's columns in as many parts as give the chip some 1000 and 4000 workgroups, with two turns at least for each wave (four along out's columns in
+// 16 bits: each workgroup begins with the sums of its tokens).
 template <int DT, int RT> struct Many {
-    static constexpr int W = 4, MT1 = DT == XL_F32 || RT == 8 ? 2 : 4, MT2 = DT == XL_F32 || RT == 8 ? 1 : 2;
+    static constexpr int W = 4, MT1 = DT == XL_F32 ? 1 : RT == 8 ? 2 : 4, MT2 = DT == XL_F32 || RT == 8 ? 1 : 2;
     long long tiles1, tiles2, parts, run, slices, strips;
     explicit Many(const xl_adapters_args &a)
     {
@@ -284,7 +286,7 @@ template <int DT, int RT> struct Many {
         parts = up_to(up_to(16, a.k / (2 * turn)), 1024 / (a.batch * tiles1));
         run = (a.k + parts * turn - 1) / (parts * turn) * turn;
         parts = run > 0 ? (a.k + run - 1) / run : 0;
-        slices = up_to(up_to(all, all / (2 * W)), 4096 / (a.batch * tiles2));
+        slices = up_to(up_to(all, all / ((DT == XL_F32 ? 2 : 4) * W)), 4096 / (a.batch * tiles2));
         strips = (all + slices - 1) / slices;
         slices = (all + strips - 1) / strips;
     }
@@ -300,15 +302,19 @@ template <int DT, int RT> struct Many {
     }
 };
 
+// One kernel where tiles of 16 tokens do not fill the chip, and for sequences of no more: 5 x up to 729 tokens, 520 to 1000, rank 13 in fp32 take 13 us in one and 17 in two, 3136 tokens, 1024 to 4096, rank 64 in fp16
+// 35 and 38.
+static bool in_one(const xl_adapters_args &a) { return a.length <= 16 || a.batch * ((a.length + 15) / 16) <= 256; }
+
 template <int DT, int RT> static hipError_t launch_rank(const xl_adapters_args &a, hipStream_t s)
 {
-    if (a.length > 16) return Many<DT, RT>::launch(a, s);
+    if (!in_one(a)) return Many<DT, RT>::launch(a, s);
     constexpr int W = DT == XL_F32 && RT >= 4 ? 4 : 8;         // fp32's registers
-    const long long all = (a.n + 63) / 64;
-    long long slices = up_to((all + W - 1) / W, 256 / a.batch);
+    const long long all = (a.n + 63) / 64, tiles = (a.length + 15) / 16;
+    long long slices = up_to((all + W - 1) / W, 256 / (a.batch * tiles));
     const long long strips = (all + slices - 1) / slices;
     slices = (all + strips - 1) / strips;
-    return launch_kernel(both_kernel<DT, RT, W>, dim3(grid_of(a.batch * slices)), 64 * W, s, a, (int)slices, (int)strips);
+    return launch_kernel(both_kernel<DT, RT, W>, dim3(grid_of(a.batch * tiles * slices)), 64 * W, s, a, (int)tiles, (int)slices, (int)strips);
 }
 
 template <int DT> static hipError_t launch_type(const xl_adapters_args &a, hipStream_t s)
@@ -322,7 +328,7 @@ template <int DT> static long long workspace_of(const xl_adapters_args &a)
 }
 long long adapters_workspace(const xl_adapters_args &a)
 {
-    return a.length <= 16 ? 0 : a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
+    return in_one(a) ? 0 : a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
 }
 
 hipError_t launch_add_adapters(const xl_adapters_args &a, hipStream_t s)

@@ -31,7 +31,8 @@ def check(p, got, what, lengths=None):
 
 SIZES = [  # batch, length, k, n, rank, adapters
     (1, 1, 1, 1, 1, 1), (3, 1, 64, 64, 8, 2), (32, 1, 256, 512, 16, 40), (5, 1, 100, 77, 3, 4), (2, 2, 520, 1000, 13, 3), (7, 5, 33, 130, 5, 2), (2, 17, 128, 96, 32, 3), (1, 64, 512, 256, 64, 1),
-    (3, 65, 200, 300, 128, 2), (1, 200, 1024, 160, 16, 1), (4, 130, 72, 520, 127, 2), (2, 300, 48, 16, 1, 2), (16, 3, 1000, 640, 20, 5), (1, 1, 4096, 4096, 16, 1), (2, 33, 31, 17, 96, 2)]
+    (3, 65, 200, 300, 128, 2), (1, 200, 1024, 160, 16, 1), (4, 130, 72, 520, 127, 2), (2, 300, 48, 16, 1, 2), (16, 3, 1000, 640, 20, 5), (1, 1, 4096, 4096, 16, 1), (2, 33, 31, 17, 96, 2),
+    (260, 17, 40, 72, 4, 7), (1, 4200, 600, 100, 16, 1), (2, 2100, 72, 264, 40, 2), (5, 900, 1100, 40, 7, 3), (3, 1500, 33, 65, 100, 2), (300, 18, 8, 30, 20, 2)]
 
 
 @pytest.mark.parametrize("dtype", list(HALF), ids=str)
@@ -44,7 +45,7 @@ def test_against_the_definition(size, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(HALF), ids=str)
-@pytest.mark.parametrize("length", [1, 9, 150])
+@pytest.mark.parametrize("length", [1, 9, 150, 800])
 def test_sequences_without_an_adapter_keep_their_projection(length, dtype):
     p = inputs(6, length, 96, 200, 24, 3, dtype)
     p["index"] = torch.tensor([0, -1, 2, 3, 1 << 30, -(1 << 31)], dtype=torch.int32, device="cuda")
@@ -58,8 +59,9 @@ def test_sequences_without_an_adapter_keep_their_projection(length, dtype):
 
 @pytest.mark.parametrize("dtype", list(HALF), ids=str)
 @pytest.mark.parametrize("lengths", [[0, 1, 2, 63, 150], [150, 0, -5, 1000, 149], [0, 0, 0, 0, 0], [64, 65, 128, 16, 17]])
-def test_sequences_of_their_own_lengths(lengths, dtype):
-    p = inputs(5, 150, 80, 144, 16, 2, dtype)
+@pytest.mark.parametrize("length", [150, 1000])        # in one kernel, in two
+def test_sequences_of_their_own_lengths(length, lengths, dtype):
+    p = inputs(5, length, 80, 144, 16, 2, dtype)
     for b, n in enumerate(lengths):
         p["x"][b, max(n, 0):] = float("nan")
         p["y"][b, max(n, 0):] = float("nan")
@@ -69,7 +71,7 @@ def test_sequences_of_their_own_lengths(lengths, dtype):
         assert not got[b, max(n, 0):].any()
 
 
-@pytest.mark.parametrize("length", [1, 12, 140])
+@pytest.mark.parametrize("length", [1, 12, 140, 1500])
 def test_views_odd_addresses_and_in_place(length):
     g = torch.Generator().manual_seed(1)
     wide = torch.randn(3, length, 300, generator=g).bfloat16().cuda()
@@ -89,7 +91,7 @@ def test_views_odd_addresses_and_in_place(length):
 
 
 @pytest.mark.parametrize("dtype", list(HALF), ids=str)
-@pytest.mark.parametrize("length", [1, 100])
+@pytest.mark.parametrize("length", [1, 100, 2100])
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")], ids=str)
 def test_infinities_and_nan_stay_in_their_row(length, bad, dtype):
     p = inputs(2, length, 70, 90, 9, 2, dtype)
