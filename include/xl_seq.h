@@ -14,7 +14,7 @@
  *   xl_gated_delta_rule  recurrence of matrices that every token decays, corrects and reads
  *
  * Every call takes one struct of 64-bit numbers and DEVICE pointers, enqueues one kernel (a large
- * product and calls with a workspace two, sizes that take 2^32 threads and more several) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
+ * product and calls with a workspace two, a delta rule of more chunks than its workspace holds and sizes that take 2^32 threads and more several) on `stream` and returns without synchronising: it may be recorded into a HIP graph.  The library allocates
  * nothing and keeps nothing between calls.  Calls never throw or abort.  The current HIP device must be a gfx950 (XL_E_DEVICE) that can reach the
  * pointers.  Inference only: there are no gradients.
  *
@@ -177,7 +177,8 @@ xl_status xl_rms_norm(const xl_rms_norm_args *args, void *stream);
  * For every token of sequence b, whose adapter is e = index[b]:
  *   out[b,t] = y[b,t] + scales[e] * up[e] (down[e] x[b,t]),   out[b,t] = y[b,t] where e lies outside [0, adapters)
  * x [batch, length, k], y and out [batch, length, n], down [adapters, rank, k] and up [adapters, n, rank] are of type `dtype`, scales [adapters] fp32 (NULL: ones).
- * rank is 1 to 128; adapters of a smaller one are filled up with zeros.  Sums are fp32, and so is down x, which is never rounded to fewer bits than 16.  Infinities and NaN stay in their token's row.  out may be
+ * rank is 1 to 128; adapters of a smaller one are filled up with zeros.  Sums are fp32, and so is down x, of which 16 bits at least go into the second product (fp32: all).  Infinities and NaN stay in their token's row; fp32 numbers beyond 3.39e38, which is
+ * bf16's end, count as infinite.  out may be
  * y with the same steps and must not overlap x, down or up.
  * The workspace is xl_add_adapters_workspace bytes, aligned to 16; it holds nothing between calls.
  */
@@ -202,8 +203,8 @@ long long xl_add_adapters_workspace(const xl_adapters_args *args);
  *   S <- exp(g[t]) S,   S <- S + beta[t] k[t] (v[t] - S^T k[t])^T,   y[t] = scale * S^T q[t]
  * q and k are [batch, length, key_heads, dk], v and y [batch, length, heads, dv], of type `dtype`; g and beta [batch, length, heads] and the states
  * [nslots, heads, dk, dv] are fp32.  heads is a multiple of key_heads, dk is 1 to 256.  With `normalize` q[t] and k[t] are divided by
- * sqrt(sum of their squares + 1e-6).  g is at most 0: what is greater counts as 0, and below -128 nothing is left of the states, as of exp(-128) in fp32.  Keys longer than one make
- * states that grow; they are followed as far as fp32 goes.  What an infinite or NaN input makes of its states' columns is not finite from its token on; infinity or NaN is not said.
+ * sqrt(sum of their squares + 1e-6), a sum that has to be an fp32 number.  g is at most 0: what is greater counts as 0, and below -128 nothing is left of the states, as of exp(-128) in fp32.  Keys longer than one make
+ * states that grow; they are followed up to 3.39e38, bf16's end.  What an infinite or NaN input makes of its states' columns is not finite from its token on; infinity or NaN is not said.
  * Arithmetic is fp32, also on the matrix units, which get fp32 operands as sums of bf16 parts: three where states come of it, two for what only makes a y of 16 bits.
  * y must not overlap the inputs.  The workspace is xl_gated_delta_rule_workspace bytes, aligned to 16; it holds nothing between calls.
  */

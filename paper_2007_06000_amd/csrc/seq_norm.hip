@@ -3,7 +3,8 @@
 //   r = x + residual,  y = r / sqrt(mean(r^2) + eps) * weight,  and with 8 bits  scale = max(max|y| / 448, 2^-126), q = e4m3(y / scale)
 //
 // Bound by memory.  A row's numbers stay in the registers of the lanes that have loaded them until its sum is known: eight neighbours a lane and load, so that sixteen
-// lanes hold a block of 128 with its scale.
+// lanes hold a block of 128 with its scale.  24642 x 4096 in bf16 with a residual, to 8 bits: 140 us for 713 MB, 5.1 TB/s (a copy of 4 GB: 4.9); 3645 x 1001 in fp32 12.5 us, 4.7 TB/s;
+// 16 x 2048 3.3 us, of which a launch is 1.6 to 1.9.
 #include "seq_e4m3.h"
 #include "seq_internal.h"
 
@@ -67,7 +68,7 @@ template <int W> __device__ __forceinline__ float sum_of_row(float s, float *sha
 // Squares of numbers above 2^64 leave fp32.  Then the sum is taken of numbers that are scaled down: those whose squares vanish, and eps, do not count beside it.
 static constexpr float DOWN = 0x1p-80f;
 
-// y, or q and a scale, of eight neighbours; by = {1 / root, and what r is to be multiplied with before}
+// y, or q and a scale, of eight neighbours: r is multiplied with `down`, the root's inverse and the weight
 template <int DT, bool Q> __device__ __forceinline__ void finish(const xl_rms_norm_args &a, const Row &row, int k, int K, float *v, float down, float inverse)
 {
     float w[8];
@@ -98,7 +99,8 @@ template <int DT, bool Q> __device__ __forceinline__ Row row_of(const xl_rms_nor
             Q ? a.scales + i * a.scale_row : nullptr};
 }
 
-// W waves a row, N times eight numbers a lane: rows of up to 512 W N numbers.
+// W waves a row, N times eight numbers a lane: rows of up to 512 W N numbers.  One wave up to 1024, whose sum needs no other; four up to what their registers hold, so that a row's loads are all on their
+// way at once.
 template <int DT, bool Q, int W, int N>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_kernel(const xl_rms_norm_args a)
 {

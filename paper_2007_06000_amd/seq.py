@@ -1,7 +1,7 @@
 """Sequence operators on torch tensors: causal convolution, selective scan, gated delta rule, norm, block quantisation, block-scaled product, adapters.
 
 The names and the meaning of every argument mirror include/xl_seq.h; the arithmetic runs in the HIP kernels of libxl_seq.so, and there is no
-CPU fallback.  Each call enqueues one kernel (a large product, a long scan of few channels and other calls with a workspace two) on the current stream of its tensors' device and returns without waiting;
+CPU fallback.  Each call enqueues one kernel (a large product, a long scan of few channels, many tokens of adapters or of the delta rule two and more) on the current stream of its tensors' device and returns without waiting;
 what does not fit raises `XlError` before anything is launched.  Inference only: tensors that ask for gradients are refused.
 """
 from __future__ import annotations
