@@ -22,8 +22,9 @@ struct Tile {
     int b, t0, live;
     long long adapter;
     bool adapted;
-    __device__ __forceinline__ Tile(const xl_adapters_args &a, long long at, int tiles, int tokens) : b((int)(at / tiles)), t0((int)(at % tiles) * tokens)
+    __device__ __forceinline__ Tile(const xl_adapters_args &a, long long at, int tiles, int tokens) : b((int)divided(at, tiles))
     {
+        t0 = (int)(at - (long long)b * tiles) * tokens;
         live = length_of(a.lengths, b, (int)a.length);
         adapter = adapter_of(a, b);
         adapted = adapter >= 0 && t0 < live;
@@ -226,8 +227,9 @@ __global__ __launch_bounds__(64 * W) void both_kernel(const xl_adapters_args a, 
 {
     __shared__ First<DT, 1, RT, W> first;
     for (long long u = blockIdx.x; u < a.batch * tiles * slices; u += gridDim.x) {
-        const Tile tile(a, u / slices, tiles, 16);
-        const int begin = (int)(u % slices) * strips;
+        const long long at = divided(u, slices);
+        const Tile tile(a, at, tiles, 16);
+        const int begin = (int)(u - at * slices) * strips;
         Second<DT, 1, RT, W> second;
         second.run(a, tile, begin, min(begin + strips, ((int)a.n + 63) / 64), [&] {
             first.run(a, tile, 0, (int)a.k);
@@ -243,8 +245,9 @@ __global__ __launch_bounds__(64 * W) void first_kernel(const xl_adapters_args a,
     __shared__ First<DT, MT, RT, W> first;
     const int length = (int)a.length;
     for (long long u = blockIdx.x; u < a.batch * tiles * parts; u += gridDim.x) {
-        const Tile tile(a, u / parts, tiles, MT * 16);
-        const int p = (int)(u % parts);
+        const long long at = divided(u, parts);
+        const Tile tile(a, at, tiles, MT * 16);
+        const int p = (int)(u - at * parts);
         if (!tile.adapted) continue;
         first.run(a, tile, p * run, min((p + 1) * run, (int)a.k));
         float *out = static_cast<float *>(a.workspace) + (p * a.batch * length + (long long)tile.b * length + tile.t0) * (RT * 16);
@@ -259,8 +262,9 @@ __global__ __launch_bounds__(64 * W) void second_kernel(const xl_adapters_args a
 {
     const int length = (int)a.length;
     for (long long u = blockIdx.x; u < a.batch * tiles * slices; u += gridDim.x) {
-        const Tile tile(a, u / slices, tiles, MT * 16);
-        const int begin = (int)(u % slices) * strips;
+        const long long at = divided(u, slices);
+        const Tile tile(a, at, tiles, MT * 16);
+        const int begin = (int)(u - at * slices) * strips;
         Second<DT, MT, RT, W> second;
         second.run(a, tile, begin, min(begin + strips, ((int)a.n + 63) / 64), [&] {
             second.take(a, tile, parts, [&](int p, int token, int at) {

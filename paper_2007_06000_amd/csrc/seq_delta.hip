@@ -136,10 +136,11 @@ template <int DT, int R, bool FULL> __device__ __forceinline__ void step_through
 template <int DT, int R>
 __global__ __launch_bounds__(256) void token_kernel(const xl_delta_args a, int tiles)
 {
-    const int H = (int)a.heads, waves = blockDim.x / 64;
+    const int waves = blockDim.x / 64;
     const long long units = a.batch * a.heads * tiles;
     for (long long unit = (long long)blockIdx.x * waves + threadIdx.x / 64; unit < units; unit += (long long)gridDim.x * waves) {
-        const int tile = (int)(unit % tiles), h = (int)(unit / tiles % H), b = (int)(unit / tiles / H);
+        const long long head = divided(unit, tiles);
+        const int tile = (int)(unit - head * tiles), b = (int)divided(head, a.heads), h = (int)(head - b * a.heads);
         if (a.dk == 8 * R && (tile + 1) * COLS <= a.dv) step_through<DT, R, true>(a, tile, b, h);
         else step_through<DT, R, false>(a, tile, b, h);
     }
@@ -220,7 +221,8 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quad = lane / 16, H = (int)a.heads;
     const long long units = a.batch * a.heads * d.chunks;
     for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-        const int c = (int)(u % d.chunks), h = (int)(u / d.chunks % H), b = (int)(u / d.chunks / H), hk = h / (int)(a.heads / a.key_heads), t0 = (d.first + c) * CHUNK;
+        const long long head = divided(u, d.chunks);
+        const int c = (int)(u - head * d.chunks), b = (int)divided(head, H), h = (int)(head - (long long)b * H), hk = h / (int)(a.heads / a.key_heads), t0 = (d.first + c) * CHUNK;
         const int n = (slot_of(a.slots, a.nslots, b) < 0 ? 0 : length_of(a.lengths, b, (int)a.length)) - t0;        // tokens from here on
         if (n <= 0) continue;
         const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head + t0 * a.k_token, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head + t0 * a.q_token;
@@ -229,18 +231,23 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
         KeyChunk<DT, DK> &shared = static_cast<KeyChunk<DT, DK> *>(d.keys)[((long long)b * a.key_heads + hk) * d.chunks + c];       // by the first of the heads that share them
         __syncthreads();        // the unit before is done with
         const int token = dealt(wave, col);
+        float gate = 0.f, step = 0.f;       // in front of the longer loads: the sums over them take longest
+        if (wave == 0 && lane < n) {
+            gate = a.g[b * a.g_batch + (t0 + lane) * a.g_token + h];
+            step = a.beta[b * a.beta_batch + (t0 + lane) * a.beta_token + h];
+        }
         Vec<T, 8> mine[KS], query[KS];
         load_keys<DK>(k + min(token, n - 1) * a.k_token, (int)a.dk, quad, mine);
         load_keys<DK>(q + min(token, n - 1) * a.q_token, (int)a.dk, quad, query);
         if (wave == 0) {
-            double g = lane < n ? (double)clamped(a.g[b * a.g_batch + (t0 + lane) * a.g_token + h]) : 0.;
+            double g = (double)clamped(gate);
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
                 const double more = __shfl_up(g, o);
                 g += lane >= o ? more : 0.;
             }
             G[lane] = g;
-            beta[lane] = lane < n ? a.beta[b * a.beta_batch + (t0 + lane) * a.beta_token + h] : 0.f;
+            beta[lane] = step;
             if (lane == 0) first_bad = CHUNK;
         }
         float kk = 0.f, qq = 0.f;

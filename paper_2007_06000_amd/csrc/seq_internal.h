@@ -137,6 +137,12 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, int length)
     return lengths ? min(max(lengths[b], 0), length) : length;
 }
 
+// u / by of numbers that are not negative.  A division of 64 bits is some hundred instructions, and u hardly ever has more than 32.
+__device__ __forceinline__ long long divided(long long u, long long by)
+{
+    return (u | by) >> 32 ? u / by : (long long)((unsigned)u / (unsigned)by);
+}
+
 // What lanes of this wave have put into LDS can be read by the others.
 __device__ __forceinline__ void wave_sync()
 {
