@@ -197,7 +197,7 @@ template <typename V> __device__ __forceinline__ float squares(V v)
 __device__ __forceinline__ f32x4 four(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
-// A chunk of a head.  2 x 12321 tokens of 16 heads of 128 x 128 (8 of keys) take 137 us for some 540 MB, most of them written; a workgroup's chain of loads, products and the inverse is some 8 us, three of them a compute
+// A chunk of a head.  2 x 12321 tokens of 16 heads of 128 x 128 (8 of keys) take 125 us for some 540 MB, most of them written; a workgroup's chain of loads, products and the inverse is some 8 us, three of them a compute
 // unit.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
 // Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
 template <int DT, int DK>
@@ -452,7 +452,7 @@ template <int DK, typename T> struct Meeting {
 // the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
 // Bound by the chain of chunks: 1 x 3136 tokens of 8 heads of 128 x 128 take 63 us, 1.3 us a chunk, of which K S0 and the right side are some 950 of 2900 cycles, T and D 600, the states 400, what they wait for each other
-// 900.  With a workgroup on each compute unit (2 x 12321 tokens, 16 heads: 359 us, 1.9 us a chunk) what is read, 80 KB a chunk and tile of 16 columns, comes out of the XCD's cache more slowly than the
+// 900.  With a workgroup on each compute unit (2 x 12321 tokens, 16 heads: 354 us, 1.8 us a chunk) what is read, 80 KB a chunk and tile of 16 columns, comes out of the XCD's cache more slowly than the
 // products need it: with one chunk read again and again the same takes 272 us.  Four waves that do all of it took 108 and 498 us, two a tile pair 130 and 594.
 // What a chunk is made of is asked for a chunk ahead, each part behind the product that has used the registers: all at once the loads would hold up the wave that issues them (16 cycles of
 // a compute unit's address unit for 16 bytes a lane).
