@@ -527,8 +527,8 @@ PyObject *rms_norm(const Args &in)          // name, x, weight, residual, new_re
         const auto span = [&](const at::Tensor *t) { return t ? rows_of(*t, a.k * int64_t(t->element_size())) : xls::Span{}; };
         const Named factor = {"weight", block_of(&weight)}, sum = {"new_residual", span(kept)}, numbers = {"scales", quantized ? numbers_of(*scales) : xls::Span{}};
         Named input = {"x (or is it, as a whole)", span(&x)}, old = {"residual (or is it, as a whole)", span(residual)};
-        if (quantized && scales != &made_scales) op.apart("scales", numbers.span, {input, old, sum, factor});
-        if (kept && kept != &made_kept) op.apart("new_residual", sum.span, {input, {old.what, old.span == sum.span ? xls::Span{} : old.span}, factor});
+        if (quantized && scales != &made_scales) op.apart("scales", numbers.span, {{"x", input.span}, {"residual", old.span}, sum, factor});
+        if (kept && kept != &made_kept) op.apart("new_residual", sum.span, {{"x", input.span}, {old.what, old.span == sum.span ? xls::Span{} : old.span}, factor});
         if (out != &made) {
             const xls::Span y = quantized ? rows_of(*out, wide) : span(out);
             if (!quantized && y == input.span) input.span = {};
