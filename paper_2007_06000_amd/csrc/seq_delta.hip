@@ -453,7 +453,7 @@ template <int DK, typename T> struct Meeting {
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
 // Bound by the chain of chunks: 1 x 3136 tokens of 8 heads of 128 x 128 take 63 us, 1.3 us a chunk, of which K S0 and the right side are some 950 of 2900 cycles, T and D 600, the states 400, what they wait for each other
 // 900.  With a workgroup on each compute unit (2 x 12321 tokens, 16 heads: 354 us, 1.8 us a chunk) what is read, 80 KB a chunk and tile of 16 columns, comes out of the XCD's cache more slowly than the
-// products need it: with one chunk read again and again the same takes 272 us.  Four waves that do all of it took 108 and 498 us, two a tile pair 130 and 594.
+// products need it: with one chunk read again and again the same takes 272 us.  Four waves that do all of it took 123 and 528 us, four with two token tiles each 130 and 594, eight (four that solve) 73 and 366.
 // What a chunk is made of is asked for a chunk ahead, each part behind the product that has used the registers: all at once the loads would hold up the wave that issues them (16 cycles of
 // a compute unit's address unit for 16 bytes a lane).
 enum { SOLVE, FETCH, RESULT };
