@@ -234,3 +234,22 @@ def test_more_chunks_than_are_prepared_at_once():
         compare(got[b:b + 1, :, h], new[b:b + 1, h], reference(one, [int(lengths[b])]), f"sequence {b}")
     again, _ = seq.gated_delta_rule(**p, normalize=True, lengths=lengths)
     assert torch.equal(again, got) and np.isfinite(f64(got[0])).all()
+
+
+def test_more_work_than_a_launch_has_workgroups():
+    """A launch has a million workgroups at most; what is more goes round in them."""
+    x, w = torch.randn(5_000_003, 8, device="cuda"), torch.rand(8, device="cuda") + 0.5
+    y, _ = seq.rms_norm(x, w)
+    want = x.double() / (x.double().square().mean(1, keepdim=True) + 1e-6).sqrt() * w.double()
+    assert ((y.double() - want).abs() <= 70 * 2.0 ** -24 * want.abs() + 1e-40).all()        # as the definition's bound
+    q, s, _ = seq.rms_norm_quantized(x, w)
+    assert ((q.float() * s - y).abs() <= 2.0 ** -4 * 1.001 * y.abs() + 2.0 ** -10 * s).all()
+    p = adapter_inputs(1 << 20, 1, 8, 24, 2, 5, torch.float32)
+    got = seq.add_adapters(**p)
+    at = torch.arange(0, 1 << 20, 10007, device="cuda")
+    some = {f: t[at] if f in ("x", "y", "index") else t for f, t in p.items()}
+    check_adapters(some, got[at], "many sequences")
+    d = delta_inputs(4096, 20, 16, 16, 4, 4, torch.float32)         # 65536 heads: token by token
+    y, new = seq.gated_delta_rule(**d, normalize=True)
+    some = {f: t[::1365].contiguous() for f, t in d.items()}
+    compare(y[::1365].contiguous(), new[::1365].contiguous(), reference(some), "many heads")
