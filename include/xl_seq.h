@@ -205,7 +205,7 @@ long long xl_add_adapters_workspace(const xl_adapters_args *args);
  * [nslots, heads, dk, dv] are fp32.  heads is a multiple of key_heads, dk is 1 to 256.  With `normalize` q[t] and k[t] are divided by
  * sqrt(sum of their squares + 1e-6), a sum that has to be an fp32 number.  g is at most 0: what is greater counts as 0, and below -128 nothing is left of the states, as of exp(-128) in fp32.  Keys longer than one make
  * states that grow; they are followed up to 3.39e38, bf16's end.  What an infinite or NaN input makes of its states' columns is not finite from its token on; infinity or NaN is not said.
- * Arithmetic is fp32, also on the matrix units, which get fp32 operands as sums of bf16 parts: three where states come of it, two for what only makes a y of 16 bits.
+ * Arithmetic is fp32, also on the matrix units, which get fp32 operands as sums of three bf16 parts; only y is rounded to its type.
  * y must not overlap the inputs.  The workspace is xl_gated_delta_rule_workspace bytes, aligned to 16; it holds nothing between calls.
  */
 typedef struct xl_delta_args {

@@ -159,9 +159,8 @@ template <int DT, int DK> struct KeyChunk {
     bf16x8 columns[DK / 16][2][parts_of<DT>()][64];                     // keys, by tiles of their numbers
 };
 // T and P: tiles 0 and 1 have numbers for tokens 0 to 31, tiles 2 and 3 for all.
-template <int DT> struct HeadChunk {
-    static constexpr int NY = DT == XL_F32 ? 3 : 2;                     // parts of what only y is made of
-    bf16x8 T[6][3][64], P[6][NY][64];
+struct HeadChunk {
+    bf16x8 T[6][3][64], P[6][3][64];
     float factors[5][64];       // of each token: e^G / |k|, beta, e^(G_64 - G) / |k|, scale e^G / |q|; and e^G_64
 };
 __device__ __forceinline__ int piece(int tile, int s) { return tile < 2 ? tile : 2 * tile - 2 + s; }
@@ -204,7 +203,6 @@ template <int DT, int DK>
 __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>() * DK < 512 ? 2 : 1) void prepare_kernel(const Delta d)
 {
     typedef typename Elem<DT>::T T;
-    typedef HeadChunk<DT> Chunk;
     constexpr int KS = DK / 32, PITCH = CHUNK + 4, NP = parts_of<DT>();
     constexpr int KEYS_PITCH = DK + 16 / sizeof(T);
     __shared__ __align__(16) float A[CHUNK][PITCH];
@@ -226,7 +224,7 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
         const int n = (slot_of(a.slots, a.nslots, b) < 0 ? 0 : length_of(a.lengths, b, (int)a.length)) - t0;        // tokens from here on
         if (n <= 0) continue;
         const T *k = static_cast<const T *>(a.k) + b * a.k_batch + hk * a.k_head + t0 * a.k_token, *q = static_cast<const T *>(a.q) + b * a.q_batch + hk * a.q_head + t0 * a.q_token;
-        Chunk &out = static_cast<Chunk *>(d.heads)[u];
+        HeadChunk &out = static_cast<HeadChunk *>(d.heads)[u];
         const int group = (int)(a.heads / a.key_heads);
         KeyChunk<DT, DK> &shared = static_cast<KeyChunk<DT, DK> *>(d.keys)[((long long)b * a.key_heads + hk) * d.chunks + c];       // by the first of the heads that share them
         __syncthreads();        // the unit before is done with
@@ -309,9 +307,9 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
                 }
                 *reinterpret_cast<f32x4 *>(&A[token][j0]) = row;
             }
-            const Parts<Chunk::NY> split_p = split<Chunk::NY>(p);
+            const Parts<3> split_p = split<3>(p);
 #pragma unroll
-            for (int i = 0; i < Chunk::NY; ++i) out.P[piece(wave, s)][i][lane] = split_p.p[i];
+            for (int i = 0; i < 3; ++i) out.P[piece(wave, s)][i][lane] = split_p.p[i];
         }
         if (bad) atomicMin(&first_bad, token);
         if (wave == 0) {
@@ -463,7 +461,7 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
     typedef Vec<T, 4> T4;
     constexpr bool HOLDS = ROLE == FETCH || (ROLE == SOLVE && DK > 64), READS = ROLE != FETCH;      // a tile of 16 rows of the states, or more; the states
     constexpr bool AHEAD = parts_of<DT>() * DK < 384, COLUMNS_AHEAD = parts_of<DT>() * DK < 768;       // there are registers for the next chunk's rows, columns
-    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), NY = HeadChunk<DT>::NY, SIZE = sizeof(T), NS = ROLE == SOLVE ? 3 : NY;
+    constexpr int KS = DK / 32, TW = DK <= 128 ? 1 : DK / 128, NP = parts_of<DT>(), SIZE = sizeof(T);
     const xl_delta_args &a = d.a;
     const int lane = threadIdx.x % 64, col = lane % 16, quad = lane / 16, H = (int)a.heads, DV = (int)a.dv, hk = h / (int)(a.heads / a.key_heads);
     const int j = tile * 16 + col, at_column = min(j, DV - 1), w4 = wave % 4, held = DK > 64 ? wave * TW : w4;
@@ -485,16 +483,16 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
 #pragma unroll
         for (int i = 0; i < TW; ++i) settle(S[i]);
     }
-    const HeadChunk<DT> *heads = static_cast<const HeadChunk<DT> *>(d.heads) + ((long long)b * H + h) * d.chunks - d.first;
+    const HeadChunk *heads = static_cast<const HeadChunk *>(d.heads) + ((long long)b * H + h) * d.chunks - d.first;
     const KeyChunk<DT, DK> *shared = static_cast<const KeyChunk<DT, DK> *>(d.keys) + ((long long)b * a.key_heads + hk) * d.chunks - d.first;
     const int rows = dealt(w4, quad * 4);       // the four tokens of a lane's results
     Vec<T, 8> row[KS];          // of keys, or of queries
-    Parts<NS> triangle[2];      // T, or P
+    Parts<3> triangle[2];       // T, or P
     Parts<NP> columns[TW][2];
     const auto ask_row = [&](int c, int s) { row[s] = shared[c].rows[ROLE == RESULT][w4][s][lane]; };
     const auto ask_triangle = [&](int c, int s) {
 #pragma unroll
-        for (int p = 0; p < NS; ++p) triangle[s].p[p] = ROLE == SOLVE ? heads[c].T[piece(w4, s)][p][lane] : heads[c].P[piece(w4, s)][p][lane];
+        for (int p = 0; p < 3; ++p) triangle[s].p[p] = ROLE == SOLVE ? heads[c].T[piece(w4, s)][p][lane] : heads[c].P[piece(w4, s)][p][lane];
     };
     const auto ask_columns = [&](int c, int i, int s) {
 #pragma unroll
@@ -533,19 +531,16 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
     };
     // y of a chunk, from Q S0
     const auto result = [&](int c, f32x4 out) {
-        Parts<NY> D[2];
+        Parts<3> D[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const f32x4 lo = m.corrections[c % 2][2 * s][lane], hi = m.corrections[c % 2][2 * s + 1][lane];
-            D[s] = split<NY>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            D[s] = split<3>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             if (s <= w4 / 2) {
-                Parts<NY> P;
-#pragma unroll
-                for (int p = 0; p < NY; ++p) P.p[p] = triangle[s].p[p];
-                out = product(P, D[s], out);
+                out = product(triangle[s], D[s], out);
                 in_order();
                 ask_triangle(min(c + 1, end - 1), s);
             }
@@ -620,11 +615,11 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
             constexpr int AT_ONCE = DK == 256 || NP == 3 ? 2 : KS;
 #pragma unroll
             for (int s0 = 0; s0 < KS; s0 += AT_ONCE) {
-                Parts<NS> S0[AT_ONCE];
+                Parts<3> S0[AT_ONCE];
 #pragma unroll
                 for (int s = 0; s < AT_ONCE; ++s) {
 #pragma unroll
-                    for (int p = 0; p < NS; ++p) S0[s].p[p] = m.states[s0 + s][p][lane];
+                    for (int p = 0; p < 3; ++p) S0[s].p[p] = m.states[s0 + s][p][lane];
                     if (!AHEAD) ask_row(c, s0 + s);
                 }
                 in_order();
@@ -748,7 +743,7 @@ template <int DT, int DK> struct Chunked {
     Chunked() {}
     explicit Chunked(const xl_delta_args &a)
     {
-        const long long keys = a.batch * a.key_heads * (long long)sizeof(KeyChunk<DT, DK>), heads = a.batch * a.heads * (long long)sizeof(HeadChunk<DT>);
+        const long long keys = a.batch * a.key_heads * (long long)sizeof(KeyChunk<DT, DK>), heads = a.batch * a.heads * (long long)sizeof(HeadChunk);
         chunks = (a.length + CHUNK - 1) / CHUNK;
         at_once = MOST_BYTES / (keys + heads);
         at_once = at_once < 1 ? 1 : at_once > chunks ? chunks : at_once;
