@@ -177,7 +177,7 @@ xl_status xl_rms_norm(const xl_rms_norm_args *args, void *stream);
  * For every token of sequence b, whose adapter is e = index[b]:
  *   out[b,t] = y[b,t] + scales[e] * up[e] (down[e] x[b,t]),   out[b,t] = y[b,t] where e lies outside [0, adapters)
  * x [batch, length, k], y and out [batch, length, n], down [adapters, rank, k] and up [adapters, n, rank] are of type `dtype`, scales [adapters] fp32 (NULL: ones).
- * rank is 1 to 128; adapters of a smaller one are filled up with zeros.  Sums are fp32, and so is down x, of which 16 bits at least go into the second product (fp32: all).  Infinities and NaN stay in their token's row; fp32 numbers beyond 3.39e38, which is
+ * rank is 1 to 128; adapters of a smaller one are filled up with zeros.  Sums are fp32, and so is down x.  Infinities and NaN stay in their token's row; fp32 numbers beyond 3.39e38, which is
  * bf16's end, count as infinite.  out may be
  * y with the same steps and must not overlap x, down or up.
  * The workspace is xl_add_adapters_workspace bytes, aligned to 16; it holds nothing between calls.

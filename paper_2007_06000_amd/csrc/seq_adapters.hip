@@ -106,8 +106,8 @@ template <int DT, int MT, int RT, int W> struct First {
 template <int DT, int MT, int RT, int W> struct Second {
     typedef typename Elem<DT>::T T;
     typedef Vec<T, 8> T8;
-    static constexpr int NP = parts_of<DT>(), NT = DT == XL_F32 ? 3 : 2, RK = (RT + 1) / 2;
-    Parts<NT> inner[MT][RK];
+    static constexpr int NP = parts_of<DT>(), RK = (RT + 1) / 2;
+    Parts<3> inner[MT][RK];
 
     // The sum over `parts` of of(part, token, rank): four neighbours of down x.  The numbers of a part are asked for together.
     template <typename F> __device__ __forceinline__ void take(const xl_adapters_args &a, const Tile &tile, int parts, F of)
@@ -127,7 +127,7 @@ template <int DT, int MT, int RT, int W> struct Second {
             for (int r = 0; r < RK; ++r) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[m][r][i] = r * 32 + quad * 8 + i < a.rank ? s[m][r][i] * scale : 0.f;
-                inner[m][r] = split<NT>(s[m][r]);
+                inner[m][r] = split<3>(s[m][r]);
             }
     }
 
