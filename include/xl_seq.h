@@ -153,7 +153,7 @@ xl_status xl_block_matmul(const xl_block_matmul_args *args, void *stream);
  * y[i,j] = r[i,j] / sqrt(sum over j of r[i,j]^2 / k + eps) * weight[j]
  * x [rows, k] is of type `dtype`, residual and new_residual are of type `residual_dtype`: x's or XL_F32.  y is of type `dtype`; with `quantized` it is q and
  * scales as xl_quantize_blocks makes them of the fp32 y with blocks of one row: rows of q begin at multiples of 16 bytes, and the bytes between a row's end and the next multiple of 16
- * are set to zero.  The norm is that of r, not of what is kept of it; sums are fp32, and right also where squares leave its range.  eps is a positive fp32 number, 2^-126 at least.  A row with an
+ * are set to zero.  The norm is that of r, not of what is kept of it; sums are fp32 (of rows of more than 32768 numbers fp64), and right also where squares leave its range.  eps is a positive fp32 number, 2^-126 at least.  A row with an
  * infinity or a NaN comes out as NaN and zeros (q: as the quantiser has them).  new_residual may be residual, and y may be x, each with the same steps; they must not overlap otherwise.
  */
 typedef struct xl_rms_norm_args {
