@@ -142,11 +142,12 @@ __global__ __launch_bounds__(1024) void long_norm_kernel(const xl_rms_norm_args 
 {
     __shared__ double shared[16];
     const int K = (int)a.k, last = (K + 127) / 128 * 128;        // all lanes of a block of 128 take part in its scale
+    // k in 64 bits: a turn is longer than what is left of 32 behind the longest row
     for (long long i = blockIdx.x; i < a.rows; i += gridDim.x) {
         const Row row = row_of<DT, Q>(a, i);
         float r[8];
         double s = 0.;
-        for (int k = threadIdx.x * 8; k < K; k += 8192) {
+        for (long long k = threadIdx.x * 8; k < K; k += 8192) {
             load_sum<DT>(a, row, k, K, r);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s = __builtin_fma((double)r[j], (double)r[j], s);
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(1024) void long_norm_kernel(const xl_rms_norm_args 
         const double mean = sum_of_row<16>(s, shared) / K + a.eps;
         const bool large = !((float)mean < __builtin_inff());
         const float inverse = __builtin_amdgcn_rsqf((float)(large ? mean * DOWN * DOWN : mean));
-        for (int k = threadIdx.x * 8; k < last; k += 8192) {
+        for (long long k = threadIdx.x * 8; k < last; k += 8192) {
             load_sum<DT>(a, row, k, K, r);
             keep<DT>(a, row, k, K, r);
             finish<DT, Q>(a, row, k, K, r, large ? DOWN : 1.f, inverse);

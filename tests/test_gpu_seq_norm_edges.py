@@ -18,3 +18,41 @@ def test_long_rows_of_one_number(value, k):
     v = float(x[0, 0])
     want = v / np.sqrt(v * v + 1e-6)
     assert (np.abs(f64(y) - want) <= 8 * 2.0 ** -24 * want).all()
+
+
+@pytest.mark.parametrize("quantized", [False, True])
+def test_the_longest_row(quantized):
+    """As many numbers as a size may have, 4096 fewer than 32 bits count: a turn of a workgroup goes past them."""
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("not enough memory is free")
+    k, step = (1 << 31) - 1 - 4096, 1 << 26
+    x = torch.empty(1, k, dtype=torch.bfloat16, device="cuda")
+    w = torch.empty(k, device="cuda")
+    g = torch.Generator("cuda").manual_seed(0)
+    squares = 0.0
+    for at in range(0, k, step):
+        n = min(step, k - at)
+        x[0, at:at + n].copy_(torch.randn(n, generator=g, device="cuda"))
+        w[at:at + n].copy_(torch.rand(n, generator=g, device="cuda") + 0.5)
+        squares += float(x[0, at:at + n].double().square().sum())
+    inverse = (squares / k + 1e-6) ** -0.5
+    if quantized:
+        q, scales, _ = seq.rms_norm_quantized(x, w)
+        assert not q.as_strided((1, q.stride(0)), (q.stride(0), 1)).view(torch.uint8)[:, k:].any()
+    else:
+        y, _ = seq.rms_norm(x, w)
+    for at in range(0, k, step):
+        n = min(step, k - at)
+        want = x[0, at:at + n].double() * w[at:at + n].double() * inverse
+        off = 16 * 2.0 ** -24 * want.abs()
+        if quantized:       # half a step of e4m3
+            s = scales[0, at // 128:(at + n + 127) // 128].double().repeat_interleave(128)[:n]
+            got = q[0, at:at + n].float().double() * s
+            off += 2.0 ** -4 * 1.0001 * want.abs() + 2.0 ** -10 * s
+        else:               # of bf16
+            got = y[0, at:at + n].double()
+            off += 2.0 ** -8 * 1.0001 * want.abs() + 2.0 ** -134
+        assert ((got - want).abs() <= off).all(), at
+    del x, w
+    torch.cuda.empty_cache()
