@@ -65,7 +65,7 @@ template <int W, typename S> __device__ __forceinline__ S sum_of_row(S s, S *sha
     return s;
 }
 
-// Squares of numbers above 2^64 leave fp32.  Then the sum is taken of numbers that are scaled down: those whose squares vanish, and eps, do not count beside it.
+// Squares of numbers above 2^64 leave fp32, and so may a mean and eps together.  Then both are taken scaled down: numbers whose squares vanish do not count beside them.
 static constexpr float DOWN = 0x1p-80f;
 
 // y, or q and a scale, of eight neighbours: r is multiplied with `down`, the root's inverse and the weight
@@ -118,15 +118,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_kernel(const xl_rm
 #pragma unroll
             for (int j = 0; j < 8; ++j) s = __builtin_fmaf(r[n][j], r[n][j], s);
         s = sum_of_row<W>(s, shared);
-        float down = 1.f, inverse = __builtin_amdgcn_rsqf(s * k_inverse + eps);
-        if (!(s < __builtin_inff())) {
+        const float mean = s * k_inverse + eps;
+        float down = 1.f, inverse = __builtin_amdgcn_rsqf(mean);
+        if (!(mean < __builtin_inff())) {
             s = 0.f;
             down = DOWN;
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s = __builtin_fmaf(r[n][j] * DOWN, r[n][j] * DOWN, s);
-            inverse = __builtin_amdgcn_rsqf(sum_of_row<W>(s, shared) * k_inverse);
+            inverse = __builtin_amdgcn_rsqf(sum_of_row<W>(s, shared) * k_inverse + eps * DOWN * DOWN);
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) keep<DT>(a, row, (n * 64 * W + lane) * 8, K, r[n]);

@@ -3,8 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import seq as ref
 from paper_2007_06000_amd import seq
-from test_gpu_seq_conv import f64
+from test_gpu_seq_conv import f64, near
+from test_gpu_seq_norm import inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +58,12 @@ def test_the_longest_row(quantized):
         assert ((got - want).abs() <= off).all(), at
     del x, w
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("k", [1, 96, 1500, 9000, 40000])
+def test_an_eps_that_counts_beside_the_largest_squares(k):
+    x, _, w = inputs(3, k, torch.float32, None)
+    for size, eps in ((1e18, 1e38), (1e19, 3e38), (1.5e19, 3.4e38), (1e19, 1e37), (3e38, 3.4e38), (1.0, 3.4e38)):
+        at = x.sign() * size
+        want, bound, _ = ref.rms_norm(f64(at), None, f64(w), eps)
+        near(seq.rms_norm(at, w, eps=eps)[0], want, bound, (size, eps))
