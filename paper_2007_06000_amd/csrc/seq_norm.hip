@@ -68,13 +68,13 @@ template <int W, typename S> __device__ __forceinline__ S sum_of_row(S s, S *sha
 // Squares of numbers above 2^64 leave fp32, and so may a mean and eps together.  Then both are taken scaled down: numbers whose squares vanish do not count beside them.
 static constexpr float DOWN = 0x1p-80f;
 
-// y, or q and a scale, of eight neighbours: r is multiplied with `down`, the root's inverse and the weight
+// y, or q and a scale, of eight neighbours: r is multiplied with the root's inverse, `down` (behind it: small numbers must not leave fp32 on the way) and the weight
 template <int DT, bool Q> __device__ __forceinline__ void finish(const xl_rms_norm_args &a, const Row &row, int k, int K, float *v, float down, float inverse)
 {
     float w[8];
     load8f<XL_F32>(a.weight, k, K, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = v[i] * down * inverse * w[i];
+    for (int i = 0; i < 8; ++i) v[i] = v[i] * inverse * down * w[i];
     if constexpr (Q) {
         unsigned most = 0;
 #pragma unroll

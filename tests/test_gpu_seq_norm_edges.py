@@ -67,3 +67,15 @@ def test_an_eps_that_counts_beside_the_largest_squares(k):
         at = x.sign() * size
         want, bound, _ = ref.rms_norm(f64(at), None, f64(w), eps)
         near(seq.rms_norm(at, w, eps=eps)[0], want, bound, (size, eps))
+
+
+@pytest.mark.parametrize("k", [96, 1500, 9000, 40000])
+def test_small_numbers_beside_the_largest(k):
+    """A result is a number of 24 bits wherever it is one of the normal ones, whatever size the row's largest number has."""
+    x = torch.full((1, k), 2.0 ** -59, device="cuda")
+    x[0, k // 2] = 1.5 * 2.0 ** 66
+    x[0, 1::2] *= 1 + torch.arange(k // 2, device="cuda") * 2.0 ** -23
+    w = torch.ones(k, device="cuda")
+    want, bound, _ = ref.rms_norm(f64(x), None, f64(w), 1e-6)
+    y = f64(seq.rms_norm(x, w)[0])
+    assert (np.abs(want) > 2.0 ** -126).all() and (np.abs(y - want) <= bound + 2.0 ** -149).all()
