@@ -20,4 +20,13 @@ __device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
+// Eight numbers of a row of which the first n exist: zeros behind them, where a row with a NaN or an infinity has 0 / NaN.  The others are shifted out, 4 bits twice for each number.
+// (Compares, as the loads have them, cost a norm of 24642 x 4096 in bf16 6 us of 139, this 1.)
+__device__ __forceinline__ unsigned long long e4m3x8(const float *v, int n)
+{
+    const unsigned long long q = e4m3x4(v[0], v[1], v[2], v[3]) | (unsigned long long)e4m3x4(v[4], v[5], v[6], v[7]) << 32;
+    const int bits = min(max(n, 0), 8) * 4;
+    return q & ~(~0ull << bits << bits);
+}
+
 }  // namespace xls

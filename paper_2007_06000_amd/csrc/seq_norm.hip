@@ -85,7 +85,7 @@ template <int DT, bool Q> __device__ __forceinline__ void finish(const xl_rms_no
         if (threadIdx.x % 16 == 0 && k < K) row.scales[k / XL_SCALE_BLOCK * a.scale_block] = scale;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = v[i] / scale;
-        if (k < (K + 15) / 16 * 16) *reinterpret_cast<u32x2 *>(row.y + k) = u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
+        if (k < (K + 15) / 16 * 16) *reinterpret_cast<unsigned long long *>(row.y + k) = e4m3x8(v, K - k);
     } else if (k < K) {
         store8f<DT>(row.y, k, K, v);
     }

@@ -79,3 +79,13 @@ def test_small_numbers_beside_the_largest(k):
     want, bound, _ = ref.rms_norm(f64(x), None, f64(w), 1e-6)
     y = f64(seq.rms_norm(x, w)[0])
     assert (np.abs(want) > 2.0 ** -126).all() and (np.abs(y - want) <= bound + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("k", [7, 200, 1001, 3001, 40009])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")], ids=str)
+def test_what_lies_behind_a_row_of_eight_bits_is_zero(bad, k):
+    for at in (0, k - 1):
+        x, r, w = inputs(3, k, torch.bfloat16, torch.bfloat16)
+        x[1, at] = bad
+        q, _, _ = seq.rms_norm_quantized(x, w, residual=r)
+        assert not q.as_strided((3, q.stride(0)), (q.stride(0), 1)).view(torch.uint8)[:, k:].any()
