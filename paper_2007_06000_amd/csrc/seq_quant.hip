@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const xl_quantize_args a)
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = v[i] / scale;
     if (k < (K + 15) / 16 * 16)
-        *reinterpret_cast<u32x2 *>(static_cast<char *>(a.q) + row * a.q_row + k) = u32x2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
+        *reinterpret_cast<unsigned long long *>(static_cast<char *>(a.q) + row * a.q_row + k) = e4m3x8(v, K - k);
 }
 
 // A block of 128 rows by 128 columns a workgroup; a thread has 8 columns of every sixteenth row.  Weights are quantised once.
@@ -88,8 +88,7 @@ __global__ __launch_bounds__(256) void blocks_kernel(const xl_quantize_args a)
         if (row < a.rows && k < (K + 15) / 16 * 16) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[r][i] = v[r][i] / scale;
-            *reinterpret_cast<u32x2 *>(static_cast<char *>(a.q) + row * a.q_row + k) =
-                u32x2{e4m3x4(v[r][0], v[r][1], v[r][2], v[r][3]), e4m3x4(v[r][4], v[r][5], v[r][6], v[r][7])};
+            *reinterpret_cast<unsigned long long *>(static_cast<char *>(a.q) + row * a.q_row + k) = e4m3x8(v[r], K - k);
         }
     }
 }

@@ -89,3 +89,14 @@ def test_what_lies_behind_a_row_of_eight_bits_is_zero(bad, k):
         x[1, at] = bad
         q, _, _ = seq.rms_norm_quantized(x, w, residual=r)
         assert not q.as_strided((3, q.stride(0)), (q.stride(0), 1)).view(torch.uint8)[:, k:].any()
+
+
+@pytest.mark.parametrize("k", [7, 200, 1001, 40009])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")], ids=str)
+@pytest.mark.parametrize("quantize", [seq.quantize_rows, seq.quantize_weight], ids=["rows", "weight"])
+def test_what_lies_behind_a_row_of_the_quantiser_is_zero(quantize, bad, k):
+    for at in (0, k - 1):
+        x, _, _ = inputs(3, k, torch.bfloat16, None)
+        x[1, at] = bad
+        q, _ = quantize(x)
+        assert not q.as_strided((3, q.stride(0)), (q.stride(0), 1)).view(torch.uint8)[:, k:].any()
