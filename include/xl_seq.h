@@ -206,7 +206,8 @@ long long xl_add_adapters_workspace(const xl_adapters_args *args);
  * sqrt(sum of their squares + 1e-6), a sum that has to be an fp32 number.  g is at most 0: what is greater counts as 0, and below -128 nothing is left of the states, as of exp(-128) in fp32.  Keys longer than one make
  * states that grow; they are followed up to 3.39e38, bf16's end.  What an infinite or NaN input makes of its states' columns is not finite from its token on; infinity or NaN is not said.
  * Arithmetic is fp32, also on the matrix units, which get fp32 operands as sums of three bf16 parts; only y is rounded to its type.
- * y must not overlap the inputs.  The workspace is xl_gated_delta_rule_workspace bytes, aligned to 16; it holds nothing between calls.
+ * y must not overlap the inputs.  The workspace is xl_gated_delta_rule_workspace bytes, aligned to 16; it holds nothing between calls.  It is 2^29 bytes at most, and where that
+ * does not hold all chunks of a prompt the states of the sequences that are worked on at the same time besides.
  */
 typedef struct xl_delta_args {
     long long batch, length, key_heads, heads, dk, dv;

@@ -738,33 +738,61 @@ __global__ __launch_bounds__(768) void chunks_kernel(const Delta d, int tiles)
 static int few_tokens(const xl_delta_args &a) { return a.batch * a.heads >= 512 ? 40 : 12; }
 static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
 
+// The sequences [first, first + count) of a call by themselves.
+template <int DT> static xl_delta_args piece_of(const xl_delta_args &a, long long first, long long count)
+{
+    const long long size = sizeof(typename Elem<DT>::T);
+    xl_delta_args p = piece_of_states(a, first, count, a.heads * a.dk * a.dv, sizeof(float));
+    p.q = behind(a.q, first * a.q_batch, size);
+    p.k = behind(a.k, first * a.k_batch, size);
+    p.v = behind(a.v, first * a.v_batch, size);
+    p.y = behind(a.y, first * a.y_batch, size);
+    p.g = behind(a.g, first * a.g_batch, sizeof(float));
+    p.beta = behind(a.beta, first * a.beta_batch, sizeof(float));
+    return p;
+}
+
+// Sequences in pieces, and their chunks so many at once, that these take no more than MOST_BYTES.
 template <int DT, int DK> struct Chunked {
-    long long chunks, at_once, of_keys, of_heads, carried;     // of a sequence, in one launch; bytes of a launch's chunks, of states between launches
+    long long sequences, chunks, at_once, of_keys, of_heads, carried;     // of a piece; of a sequence, in one launch; bytes of a launch's chunks, of states between launches
     Chunked() {}
     explicit Chunked(const xl_delta_args &a)
     {
-        const long long keys = a.batch * a.key_heads * (long long)sizeof(KeyChunk<DT, DK>), heads = a.batch * a.heads * (long long)sizeof(HeadChunk);
+        sequences = MOST_BYTES / bytes_of_a_sequence(a);
+        sequences = sequences < 1 ? 1 : sequences > a.batch ? a.batch : sequences;
         chunks = (a.length + CHUNK - 1) / CHUNK;
-        at_once = MOST_BYTES / (keys + heads);
+        at_once = MOST_BYTES / (sequences * bytes_of_a_sequence(a));
         at_once = at_once < 1 ? 1 : at_once > chunks ? chunks : at_once;
-        of_keys = at_once * keys;
-        of_heads = at_once * heads;
-        carried = at_once < chunks ? (a.batch * a.heads * a.dk * a.dv * 4 + 15) / 16 * 16 : 0;
+        of_keys = at_once * sequences * a.key_heads * (long long)sizeof(KeyChunk<DT, DK>);
+        of_heads = at_once * sequences * a.heads * (long long)sizeof(HeadChunk);
+        carried = at_once < chunks ? (sequences * a.heads * a.dk * a.dv * 4 + 15) / 16 * 16 : 0;
+    }
+    static long long bytes_of_a_sequence(const xl_delta_args &a)      // of one chunk of all its heads
+    {
+        return a.key_heads * (long long)sizeof(KeyChunk<DT, DK>) + a.heads * (long long)sizeof(HeadChunk);
     }
     static long long bytes(const xl_delta_args &a)
     {
         const Chunked plan(a);
         return plan.of_keys + plan.of_heads + plan.carried;
     }
-    static hipError_t launch(const xl_delta_args &a, hipStream_t s)
+    static hipError_t launch(const xl_delta_args &all, hipStream_t s)
     {
-        const Chunked plan(a);
+        const Chunked plan(all);
+        for (long long b = 0; b < all.batch; b += plan.sequences) {
+            const hipError_t e = plan.launch_piece(piece_of<DT>(all, b, all.batch - b < plan.sequences ? all.batch - b : plan.sequences), s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    hipError_t launch_piece(const xl_delta_args &a, hipStream_t s) const
+    {
         const int tiles = (int)((a.dv + 15) / 16);
         char *w = static_cast<char *>(a.workspace);
-        float *carried = plan.carried ? reinterpret_cast<float *>(w + plan.of_keys + plan.of_heads) : nullptr;
-        for (long long first = 0; first < plan.chunks; first += plan.at_once) {
-            const long long some = plan.chunks - first < plan.at_once ? plan.chunks - first : plan.at_once, units = a.batch * a.heads * some;
-            const Delta d = {a, (int)first, (int)some, carried, first + some < plan.chunks ? carried : nullptr, w, w + plan.of_keys};
+        float *between = carried ? reinterpret_cast<float *>(w + of_keys + of_heads) : nullptr;
+        for (long long first = 0; first < chunks; first += at_once) {
+            const long long some = chunks - first < at_once ? chunks - first : at_once, units = a.batch * a.heads * some;
+            const Delta d = {a, (int)first, (int)some, between, first + some < chunks ? between : nullptr, w, w + of_keys};
             hipError_t e = launch_kernel(prepare_kernel<DT, DK>, dim3((unsigned)(units < 1 << 20 ? units : 1 << 20)), 256, s, d);
             if (e == hipSuccess) e = launch_kernel(chunks_kernel<DT, DK>, dim3((unsigned)(a.batch * a.heads * tiles)), 768, s, d, tiles);
             if (e != hipSuccess) return e;
@@ -782,15 +810,16 @@ template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
     return a.dk <= 64 ? f(Chunked<DT, 64>()) : a.dk <= 128 ? f(Chunked<DT, 128>()) : f(Chunked<DT, 256>());
 }
 
-// Tens of thousands of heads fill the chip token by token too, and a chunk of each would take gigabytes of workspace.
-static bool in_chunks(const xl_delta_args &a)
+// Tens of thousands of heads fill the chip token by token too, and so do thousands of one sequence, whose chunk alone would take more than MOST_BYTES.
+template <int DT> static bool in_chunks(const xl_delta_args &a)
 {
-    return a.length > few_tokens(a) && a.batch * a.heads < 1 << 16 && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 22 && a.v_token <= FURTHEST && a.y_token <= FURTHEST && a.dv <= FURTHEST;
+    if (a.batch * a.heads >= 1 << 16 || with_keys<DT>(a, [&](auto chunked) { return chunked.bytes_of_a_sequence(a); }) > MOST_BYTES) return false;
+    return a.length > few_tokens(a) && a.batch * a.heads * ((a.dv + 15) / 16) < 1 << 22 && a.v_token <= FURTHEST && a.y_token <= FURTHEST && a.dv <= FURTHEST;
 }
 
 template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStream_t s)
 {
-    if (in_chunks(a)) return with_keys<DT>(a, [&](auto chunked) { return chunked.launch(a, s); });
+    if (in_chunks<DT>(a)) return with_keys<DT>(a, [&](auto chunked) { return chunked.launch(a, s); });
     const int tiles = (int)((a.dv + COLS - 1) / COLS);
     // few waves have a compute unit each
     const long long units = a.batch * a.heads * tiles, waves = units <= 1024 ? 1 : 4, groups = (units + waves - 1) / waves;
@@ -802,11 +831,11 @@ template <int DT> static hipError_t launch_type(const xl_delta_args &a, hipStrea
 
 template <int DT> static long long workspace_of(const xl_delta_args &a)
 {
-    return with_keys<DT>(a, [&](auto chunked) { return chunked.bytes(a); });
+    return in_chunks<DT>(a) ? with_keys<DT>(a, [&](auto chunked) { return chunked.bytes(a); }) : 0;
 }
 long long delta_workspace(const xl_delta_args &a)
 {
-    return !in_chunks(a) ? 0 : a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
+    return a.dtype == XL_F32 ? workspace_of<XL_F32>(a) : a.dtype == XL_F16 ? workspace_of<XL_F16>(a) : workspace_of<XL_BF16>(a);
 }
 
 hipError_t launch_gated_delta_rule(const xl_delta_args &a, hipStream_t s)
