@@ -401,7 +401,7 @@ __device__ __forceinline__ void settle(f32x4 &v)
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// The rows of a chunk that exist, as a buffer: what lies past the last one comes out as zeros and is not written.
+// The rows of a chunk that exist, as a buffer: what lies past the last one's end comes out as zeros and is not written.  (Rows that overlap go on behind the last one in the same memory.)
 struct Tokens {
     __amdgpu_buffer_rsrc_t rsrc;
     __device__ __forceinline__ Tokens(const void *base, long long first, int rows, long long step, int width)      // in bytes
@@ -509,12 +509,13 @@ template <int DT, int DK, int ROLE> __device__ __forceinline__ void go_through(c
     T4 value;
     float factor, last_factor;
     const auto ask_values = [&](int c) {
-        const Tokens tokens(v_base, (long long)c * CHUNK, n - c * CHUNK, v_step, width);
+        const int left = n - c * CHUNK;
+        const Tokens tokens(v_base, (long long)c * CHUNK, left, v_step, width);
         if (wide_v) {
-            value = tokens.template load<T4>(four_at * SIZE < width ? one_token * (int)v_step + four_at * SIZE : NOWHERE);
+            value = tokens.template load<T4>(four_at * SIZE < width && one_token < left ? one_token * (int)v_step + four_at * SIZE : NOWHERE);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(j < DV ? (rows + e) * (int)v_step + col * SIZE : NOWHERE);
+            for (int e = 0; e < 4; ++e) value[e] = tokens.template load<T>(j < DV && rows + e < left ? (rows + e) * (int)v_step + col * SIZE : NOWHERE);
         }
         factor = heads[c].factors[w4][lane];
         last_factor = heads[c].factors[4][lane];

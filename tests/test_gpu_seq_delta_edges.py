@@ -62,3 +62,21 @@ def test_a_sequence_of_more_heads_than_the_workspace_has_room_for():
     got, new = seq.gated_delta_rule(**p, normalize=True)
     some = {f: (t[:, ::700] if f == "state" else t[:, :, ::700]).contiguous() for f, t in p.items()}
     compare(got[:, :, ::700], new[:, ::700], reference(some), "some")
+
+
+@pytest.mark.parametrize("dtype", list(HALF), ids=str)
+@pytest.mark.parametrize("step", [1, 4])                # numbers one by one, four at a time
+@pytest.mark.parametrize("length", [5, 64, 100, 130])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")], ids=str)
+def test_values_that_overlap_are_those_of_tokens_that_exist(bad, length, step, dtype):
+    """Windows of one run of memory: behind the last token's row there are numbers of that row, not of a token."""
+    p = inputs(1, length, 1, 2, 64, 36, dtype)
+    room = torch.randn((length - 1) * step + 72, generator=torch.Generator().manual_seed(2)).to(dtype).cuda()
+    p["v"] = room.as_strided((1, length, 2, 36), (room.numel(), step, 36, 1))
+    y0, s0 = seq.gated_delta_rule(**p, normalize=True)
+    compare(y0, s0, reference(p), "windows", spread(p, [length], True))
+    room[-1] = bad                                      # the last number of the last token and head
+    y, s = seq.gated_delta_rule(**p, normalize=True)
+    assert not torch.isfinite(y[0, -1, 1, 35]) and not torch.isfinite(s[0, 1, :, 35]).any()
+    y[0, -1, 1, 35], s[0, 1, :, 35] = y0[0, -1, 1, 35], s0[0, 1, :, 35]
+    assert torch.equal(y, y0) and torch.equal(s, s0)
