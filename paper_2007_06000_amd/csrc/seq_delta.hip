@@ -198,7 +198,8 @@ __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_in
 
 // A chunk of a head.  2 x 12321 tokens of 16 heads of 128 x 128 (8 of keys) take 125 us for some 540 MB, most of them written; a workgroup's chain of loads, products and the inverse is some 8 us, three of them a compute
 // unit.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
-// Rows from the first token on that has an infinity or a NaN (or overflows) are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.
+// Rows from the first on that has an infinity or a NaN are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.  (A token whose own key is not finite has such a
+// right side, whatever its row.  k.k is no part of A: it may leave fp32.)
 template <int DT, int DK>
 __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>() * DK < 512 ? 2 : 1) void prepare_kernel(const Delta d)
 {
@@ -286,9 +287,10 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
                 with_q[j] = product(o, query_parts[s], with_q[j]);
             }
         }
+        const int before = token < n ? token : 0;       // numbers of the row: behind the last token it would be 0 beta, of products that may be infinite
         const double Gi = G[token];
         const float ki = inverse_k[token] * beta[token], qi = inverse_q[token];
-        bool bad = false;
+        float none = 0.f;       // a NaN if a number of the row is not finite
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if (s > wave / 2) continue;
@@ -301,8 +303,8 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
                 for (int i = 0; i < 4; ++i) {
                     const int j = j0 + i;
                     const float e = exp_fast((float)(Gi - G[j])) * inverse_k[j], v = with_k[2 * s + half][i] * e * ki;
-                    bad |= j <= token && !finite(v);
-                    row[i] = j < token ? v : 0.f;
+                    row[i] = j < before ? v : 0.f;
+                    none = __builtin_fmaf(row[i], 0.f, none);
                     p[half * 4 + i] = j <= token ? with_q[2 * s + half][i] * e * qi : 0.f;
                 }
                 *reinterpret_cast<f32x4 *>(&A[token][j0]) = row;
@@ -311,7 +313,7 @@ __global__ __launch_bounds__(256, parts_of<DT>() * DK <= 192 ? 3 : parts_of<DT>(
 #pragma unroll
             for (int i = 0; i < 3; ++i) out.P[piece(wave, s)][i][lane] = split_p.p[i];
         }
-        if (bad) atomicMin(&first_bad, token);
+        if (none != 0.f) atomicMin(&first_bad, token);
         if (wave == 0) {
             out.factors[0][lane] = exp_fast((float)G[lane]) * inverse_k[lane];
             out.factors[1][lane] = beta[lane];

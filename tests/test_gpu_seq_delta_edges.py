@@ -80,3 +80,29 @@ def test_values_that_overlap_are_those_of_tokens_that_exist(bad, length, step, d
     assert not torch.isfinite(y[0, -1, 1, 35]) and not torch.isfinite(s[0, 1, :, 35]).any()
     y[0, -1, 1, 35], s[0, 1, :, 35] = y0[0, -1, 1, 35], s0[0, 1, :, 35]
     assert torch.equal(y, y0) and torch.equal(s, s0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("length,t", [(5, 4), (5, 1), (64, 63), (100, 99), (100, 30), (130, 64), (130, 63)])
+def test_a_key_whose_square_leaves_fp32(length, t, dtype):
+    """A key of 3e19 writes states of that size; nothing that the formula asks for is larger."""
+    p = inputs(1, length, 1, 2, 64, 24, dtype, normalized=True)
+    p["k"][..., 7] = 0                                  # no other key has this number
+    p["q"][..., 7] = 2.0 ** -64
+    p["state"][:, :, 7] = 0
+    p["k"][0, t] = 0
+    y0, s0 = seq.gated_delta_rule(**p, scale=1.0)       # without the token's key: nothing is written there
+    p["k"][0, t, 0, 7] = 3e19
+    y, s = seq.gated_delta_rule(**p, scale=1.0)
+    size = f64(p["k"])[0, t, 0, 7]
+    after = np.cumsum(f64(p["g"])[0, t:], 0) - f64(p["g"])[0, t]          # [tokens, heads]
+    row = size * f64(p["beta"])[0, t][:, None] * f64(p["v"])[0, t] * np.exp(after)[..., None]      # [tokens, heads, dv]
+    # a factor e^G is off by 2^-24 of G's size and some units, a product by 2^-24, and states before it are what they were
+    off = (32 + np.abs(after).max()) * 2.0 ** -24
+    assert (np.abs(f64(s)[0, :, 7] - row[-1]) <= off * np.abs(row[-1])).all()
+    others = torch.arange(64, device="cuda") != 7
+    assert torch.allclose(s[:, :, others], s0[:, :, others], rtol=1e-5, atol=1e-6)
+    want = f64(y0)[0, t:] + 2.0 ** -64 * row
+    # each of the two results is rounded to its type, and their fp32 sums of 64 products
+    assert (np.abs(f64(y)[0, t:] - want) <= 2 * HALF[dtype] * (np.abs(f64(y0)[0, t:]) + np.abs(want)) + (off + 256 * 2.0 ** -24) * (1 + np.abs(row) * 2.0 ** -64)).all()
+    assert torch.equal(y[:, :t], y0[:, :t])
