@@ -737,8 +737,16 @@ __global__ __launch_bounds__(768) void chunks_kernel(const Delta d, int tiles)
     else go_through<DT, DK, RESULT>(d, m, tile, b, h, wave);
 }
 
-// Token by token a few heads take 0.5 (64 x 64) to 1 us (128 x 128) a token, in chunks 14 to 20 us up to 64 tokens; 64 sequences of 16 heads of 128 x 128 take 23 + 2.9 us a token, in chunks 150.
-static int few_tokens(const xl_delta_args &a) { return a.batch * a.heads >= 512 ? 40 : 12; }
+// How many tokens go one by one.  us of 16 / 24 / 48 / 64 / 128 tokens, keys and values of 128, bf16, one by one | in chunks:
+//   8 heads 19 / 26 / 49 / 64 / 125 | 16 / 16 / 16 / 16 / 18          128 heads 22 / 29 / 53 / 68 / 132 | 34 / 34 / 34 / 34 / 41
+//   512 heads 36 / 48 / 83 / 105 / 196 | 82 / 82 / 83 / 85 / 120      1024 heads 63 / 85 / 150 / 194 / 371 | 152 / 153 / 158 / 161 / 294
+// The ways meet at 16, 25, 52 and 61 tokens with keys and values of 64, at 13, 20, 37 and 42 with keys of 256.  In fp32 a chunk takes twice as many operations, and from 1024 heads on it is never the faster way:
+// 128 tokens of 4096 heads take 506 one by one, 848 in chunks (64 x 64), 1642 and 2105 (128 x 128).
+static long long few_tokens(const xl_delta_args &a)
+{
+    const long long heads = a.batch * a.heads;
+    return heads >= 1024 && a.dtype == XL_F32 ? a.length : heads >= 512 ? 48 : heads >= 128 ? 24 : 14;
+}
 static constexpr long long MOST_BYTES = 1ll << 29;         // of chunks that are prepared at once
 
 // The sequences [first, first + count) of a call by themselves.
@@ -813,7 +821,7 @@ template <int DT, typename F> static auto with_keys(const xl_delta_args &a, F f)
     return a.dk <= 64 ? f(Chunked<DT, 64>()) : a.dk <= 128 ? f(Chunked<DT, 128>()) : f(Chunked<DT, 256>());
 }
 
-// Tens of thousands of heads fill the chip token by token too, and so do thousands of one sequence, whose chunk alone would take more than MOST_BYTES.
+// Tens of thousands of heads go token by token (64 tokens of 65536 heads of 64 x 64 in bf16 take 3.8 ms, of 65520 in chunks 5.1), and so do thousands of one sequence, whose chunk alone would take more than MOST_BYTES.
 template <int DT> static bool in_chunks(const xl_delta_args &a)
 {
     if (a.batch * a.heads >= 1 << 16 || with_keys<DT>(a, [&](auto chunked) { return chunked.bytes_of_a_sequence(a); }) > MOST_BYTES) return false;

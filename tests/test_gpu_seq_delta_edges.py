@@ -33,35 +33,35 @@ def test_a_result_of_16_bits_is_rounded_once(where, dtype, dk, length):
 
 
 @pytest.mark.parametrize("with_slots", [False, True])
-@pytest.mark.parametrize("length", [41, 140])           # one chunk of each sequence, three and the states between them
+@pytest.mark.parametrize("length", [60, 140])           # one chunk of each sequence, three and the states between them
 def test_more_sequences_than_the_workspace_has_room_for(length, with_slots):
-    """2100 heads whose keys and queries take 229 KB a chunk, of 700 sequences: they go in two pieces, the second from about sequence 669 on."""
-    p = inputs(700, length, 3, 3, 129, 8, torch.float32)
-    rows = torch.arange(700)
+    """4200 heads that take 133 KB a chunk, of 1400 sequences: they go in two pieces, the second from about sequence 1311 on."""
+    p = inputs(1400, length, 3, 3, 129, 8, torch.bfloat16)
+    rows = torch.arange(1400)
     if with_slots:
-        rows = (rows * 3 + 5) % 700
-        p["state"] = torch.randn(700, 3, 129, 8, device="cuda") * 0.1
+        rows = (rows * 3 + 5) % 1400
+        p["state"] = torch.randn(1400, 3, 129, 8, device="cuda") * 0.1
     slots = rows.int().cuda() if with_slots else None
-    lengths = (torch.arange(700) * 7 % (length + 1)).int().cuda()
+    lengths = (torch.arange(1400) * 7 % (length + 1)).int().cuda()
     cache = p["state"].clone()
     got, new = seq.gated_delta_rule(**{**p, "state": cache}, normalize=True, slots=slots, lengths=lengths)
-    at = [0, 1, 599, 660, 667, 668, 669, 670, 671, 672, 699]
+    at = [0, 1, 655, 1300, *range(1308, 1316), 1399]
     some = {**{f: t[at].contiguous() for f, t in p.items() if f != "state"}, "state": p["state"][rows[at].cuda()]}
     n = [int(lengths[b]) for b in at]
     compare(got[at], new[rows[at].cuda()], reference(some, n), "some", spread(some, n, True))
     # the others as in calls of their own, which are small enough for one piece
-    for first in range(0, 700, 100):
-        part = slice(first, first + 100)
+    for first in range(0, 1400, 200):
+        part = slice(first, first + 200)
         y, s = seq.gated_delta_rule(**{**{f: t[part] for f, t in p.items() if f != "state"}, "state": p["state"][rows[part].cuda()]}, normalize=True, lengths=lengths[part])
         assert torch.equal(y, got[part]) and torch.equal(s, new[rows[part].cuda()]), first
 
 
 def test_a_sequence_of_more_heads_than_the_workspace_has_room_for():
-    """A chunk of 2100 heads with keys of their own does not fit: token by token."""
-    p = inputs(2, 70, 2100, 2100, 129, 4, torch.float32)
+    """A chunk of 4200 heads with keys of their own does not fit: token by token."""
+    p = inputs(2, 70, 4200, 4200, 129, 4, torch.bfloat16)
     got, new = seq.gated_delta_rule(**p, normalize=True)
-    some = {f: (t[:, ::700] if f == "state" else t[:, :, ::700]).contiguous() for f, t in p.items()}
-    compare(got[:, :, ::700], new[:, ::700], reference(some), "some")
+    some = {f: (t[:, ::1400] if f == "state" else t[:, :, ::1400]).contiguous() for f, t in p.items()}
+    compare(got[:, :, ::1400], new[:, ::1400], reference(some), "some")
 
 
 @pytest.mark.parametrize("dtype", list(HALF), ids=str)
