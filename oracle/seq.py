@@ -107,7 +107,7 @@ def rms_norm(x, residual, weight, eps):
 
 
 def add_adapters(y, x, down, up, scales, index, lengths, parts):
-    """out and its bound; with `parts` down x counts as rounded to 16 bits."""
+    """out and its bound; with `parts` it allows for a down x that is rounded to 16 bits."""
     out, bound = np.array(y, copy=True), np.zeros(y.shape)
     k, rank = x.shape[2], up.shape[2]
     for b, n in enumerate(lengths):
@@ -128,7 +128,7 @@ def gated_delta_rule(q, k, v, g, beta, scale, normalize, state, lengths, parts):
 
     A token multiplies what the columns of the states are off by with exp(g) (I - beta k k^T), whose 2-norm is max(1, |1 - beta k.k|), and adds
     its own rounding: sums over the numbers of a key and over the up to 64 tokens that are worked on together, of the states' and the correction's size.
-    With `parts` the result's own sums are of operands rounded to 16 bits."""
+    With `parts` it allows for operands rounded to 16 bits in the result's own sums."""
     batch, length, heads, dv = v.shape
     dk, group = q.shape[3], heads // q.shape[2]
     if normalize:

@@ -4,7 +4,7 @@
 //
 // Bound by memory: x and y are read and out is written once, the adapter's matrices come from the caches.  Few tokens go through one kernel, where the numbers between the products stay in LDS: out
 // is cut into slices until they fill the chip, and each slice's workgroup makes down x again, which costs less than a second launch.  More tokens take two kernels, so that both can be cut into as many parts
-// as the chip wants: of k, and of out's columns.  (In one, 2 x 12321 tokens were 386 tiles of 64 for 256 compute units, the second round of them half empty: 176 us instead of 168, of
+// as the chip wants: of k, and of out's columns.  (In one, 2 x 12321 tokens were 386 tiles of 64 for 256 compute units, the second round of them half empty: 176 us instead of 168 (170 with other inputs each time), of
 // which the second kernel, y to out, is 98 at 4.1 TB/s.)  Up read as runs of memory and dealt through LDS measured 174 us, and 33 instead of 35 for 3136 tokens in one kernel.
 #include "seq_parts.h"
 
@@ -306,7 +306,7 @@ template <int DT, int RT> struct Many {
     }
 };
 
-// One kernel where tiles of 16 tokens do not fill the chip, and for sequences of no more: 5 x up to 729 tokens, 520 to 1000, rank 13 in fp32 take 13 us in one and 17 in two, 3136 tokens, 1024 to 4096, rank 64 in fp16
+// One kernel where tiles of 16 tokens do not fill the chip, and for sequences of no more: 5 x up to 729 tokens, 520 to 1000, rank 13 in fp32 take 13 us in one and 17 in two (the same inputs each time; with others 16 in one), 3136 tokens, 1024 to 4096, rank 64 in fp16
 // 35 and 38.
 static bool in_one(const xl_adapters_args &a) { return a.length <= 16 || a.batch * ((a.length + 15) / 16) <= 256; }
 

@@ -25,8 +25,8 @@ __device__ __forceinline__ float clamped(float g)
 
 // A wave has 32 columns of a head's states in registers, eight of them rows' parts: lane % 8 names four columns, lane / 8 a run of R = rows / 8 rows.
 // One pass over them gives both S^T k and S^T q, from which y follows without the new states:  S'^T q = S^T q + (k.q) beta (v - S^T k).
-// A token is bound by reading and writing the states: 64 sequences of 16 heads of 128 x 128 take 23.4 us for 135 MB (5.8 TB/s, a part of it from the last-level cache), 16 of 8 heads of 64 x 64 3.9 us.  Sums over
-// lanes through LDS and numbers asked for when they are needed: 26.5 and 5.6 us, and 1.4 instead of 0.5 to 1 us for each further token.
+// A token is bound by reading and writing the states: 64 sequences of 16 heads of 128 x 128 take 27.3 us for 135 MB (4.9 TB/s, as a copy), 16 of 8 heads of 64 x 64 4.1 us.  (With the same states
+// each time, out of the last-level cache, 23.4 and 3.9; then sums over lanes through LDS and numbers asked for when they are needed took 26.5 and 5.6 us, and 1.4 instead of 0.5 to 1 us for each further token.)
 static constexpr int COLS = 32;
 
 // The sum over lanes whose number is the same modulo 8, without a way through LDS.
@@ -196,8 +196,8 @@ template <typename V> __device__ __forceinline__ float squares(V v)
 __device__ __forceinline__ f32x4 four(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
-// A chunk of a head.  2 x 12321 tokens of 16 heads of 128 x 128 (8 of keys) take 125 us for some 540 MB, most of them written; a workgroup's chain of loads, products and the inverse is some 8 us, three of them a compute
-// unit.  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
+// A chunk of a head.  2 x 12321 tokens of 16 heads of 128 x 128 (8 of keys) take 130 us for 514 MB, 387 of them written; a workgroup's chain of loads, products and the inverse is some 8 us, three of them a compute
+// unit.  (One round of workgroups by itself takes 18 us, 1 x 3136 tokens of 8 heads; what the rest of it goes into has not been measured.)  Wave w makes row tile w of A and P.  Their columns' tokens are the operation's rows, so that a lane has eight neighbours of a row.
 // Rows from the first on that has an infinity or a NaN are left out of A, and T's diagonal says so with NaN: tokens before it get their right results.  (A token whose own key is not finite has such a
 // right side, whatever its row.  k.k is no part of A: it may leave fp32.)
 template <int DT, int DK>
@@ -451,9 +451,10 @@ template <int DK, typename T> struct Meeting {
 // Both also have parts of the states' rows in their registers (FETCH alone where DK is 64).  RESULT: y, a step behind.  What the waves need of each other meets in LDS three times a chunk: S0, the right side of
 // the system, and D.
 // Where a token's correction is not finite, zero stands for it, and its column is not finite from that token on: no product spreads it to tokens before.
-// Bound by the chain of chunks: 1 x 3136 tokens of 8 heads of 128 x 128 take 63 us, 1.3 us a chunk, of which K S0 and the right side are some 950 of 2900 cycles, T and D 600, the states 400, what they wait for each other
-// 900.  With a workgroup on each compute unit (2 x 12321 tokens, 16 heads: 354 us, 1.8 us a chunk) what is read, 80 KB a chunk and tile of 16 columns, comes out of the XCD's cache more slowly than the
-// products need it: with one chunk read again and again the same takes 272 us.  Four waves that do all of it took 123 and 528 us, four with two token tiles each 130 and 594, eight (four that solve) 73 and 366.
+// Bound by the chain of chunks: 1 x 3136 tokens of 8 heads of 128 x 128 take 67 us, 1.4 us a chunk, of which K S0 and the right side are some 950 of 2900 cycles, T and D 600, the states 400, what they wait for each other
+// 900.  With a workgroup on each compute unit (2 x 12321 tokens, 16 heads: 384 us, 2.0 us a chunk) what is read, 85 KB a chunk and tile of 16 columns, comes out of the XCD's cache more slowly than the
+// products need it.  These were measured with two parts in what makes y instead of three, 63 and 354 us: the cycles; 272 us with one chunk read again and again; four waves that do all of it 123 and 528 us, four with two
+// token tiles each 130 and 594, eight (four that solve) 73 and 366.
 // What a chunk is made of is asked for a chunk ahead, each part behind the product that has used the registers: all at once the loads would hold up the wave that issues them (16 cycles of
 // a compute unit's address unit for 16 bytes a lane).
 enum { SOLVE, FETCH, RESULT };

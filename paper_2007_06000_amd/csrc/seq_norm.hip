@@ -3,8 +3,8 @@
 //   r = x + residual,  y = r / sqrt(mean(r^2) + eps) * weight,  and with 8 bits  scale = max(max|y| / 448, 2^-126), q = e4m3(y / scale)
 //
 // Bound by memory.  A row's numbers stay in the registers of the lanes that have loaded them until its sum is known: eight neighbours a lane and load, so that sixteen
-// lanes hold a block of 128 with its scale.  24642 x 4096 in bf16 with a residual, to 8 bits: 140 us for 713 MB, 5.1 TB/s (a copy of 4 GB: 4.9); 3645 x 1001 in fp32 12.5 us, 4.7 TB/s;
-// 16 x 2048 3.3 us, of which a launch is 1.6 to 1.9.
+// lanes hold a block of 128 with its scale.  24642 x 4096 in bf16 with a residual, to 8 bits: 141 us for 710 MB, 5.0 TB/s (a copy of 4 GB: 4.9); 3645 x 1001 in fp32 12.8 us, 4.6 TB/s;
+// 16 x 2048 3.5 us, of which a launch is 1.6 to 1.9.
 #include "seq_e4m3.h"
 #include "seq_internal.h"
 
