@@ -106,3 +106,23 @@ def test_a_key_whose_square_leaves_fp32(length, t, dtype):
     # each of the two results is rounded to its type, and their fp32 sums of 64 products
     assert (np.abs(f64(y)[0, t:] - want) <= 2 * HALF[dtype] * (np.abs(f64(y0)[0, t:]) + np.abs(want)) + (off + 256 * 2.0 ** -24) * (1 + np.abs(row) * 2.0 ** -64)).all()
     assert torch.equal(y[:, :t], y0[:, :t])
+
+
+def test_pieces_recorded_and_replayed():
+    """Several launches that share a workspace, three chunks and two pieces: the same from a graph, again and again, with calls of its own kind in between."""
+    p = inputs(1400, 140, 3, 3, 129, 8, torch.bfloat16)
+    static = {f: t.clone() for f, t in p.items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        seq.gated_delta_rule(**static, normalize=True)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        results = seq.gated_delta_rule(**static, normalize=True)
+    for i in range(3):
+        static["v"].copy_(p["v"] * (1 + i))
+        graph.replay()
+        want = seq.gated_delta_rule(**{**p, "v": p["v"] * (1 + i)}, normalize=True)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results, want)), i
